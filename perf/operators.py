@@ -17,7 +17,8 @@ M tokens, D the model width (what a norm runs over), N and K a projection's outp
 H query heads and Hk key heads of dimension d of which the first R elements turn.  8 bits are e4m3
 (float8_e4m3fn) with a scale for each block: of 128 consecutive k of one token, or of 128 x 128 of a
 weight.  Scales are powers of two, held as their exponent (float8_e8m0fnu), the smallest that brings
-the block's magnitudes to at most 448; a row of scales is padded to a multiple of four.  Activations are standard normal times a per-channel gain, weights standard
+the block's magnitudes to at most 448; four blocks' exponents lie side by side, in the shape
+[groups of four blocks][tokens, or weight blocks][4].  Activations are standard normal times a per-channel gain, weights standard
 normal over the square root of their input width, norm weights near 1, output gradients standard
 normal.
 
@@ -181,9 +182,9 @@ def _scales(amax):
 
 
 def _held_scales(e):
-    """Exponents [rows][blocks] as the scale operand, padded with ones."""
-    e = torch.nn.functional.pad(e, (0, -e.shape[1] % 4), value=127)
-    return e.to(torch.uint8).view(torch.float8_e8m0fnu)
+    """Exponents [rows][blocks] as the scale operand [groups][rows][4], padded with ones."""
+    e = torch.nn.functional.pad(e, (0, -e.shape[1] % 4), value=127).to(torch.uint8)
+    return e.unflatten(1, (-1, 4)).transpose(0, 1).contiguous().view(torch.float8_e8m0fnu)
 
 
 def _rows8(x):
@@ -314,9 +315,9 @@ def _norm(x, residual, weight):
 
 
 def _two_to(e, K):
-    """Scales from exponents [rows][blocks], each for the 128 k of its block."""
+    """Scales from exponents [rows][blocks] or a scale operand, each for the 128 k of its block."""
     if e.dtype == torch.float8_e8m0fnu:
-        e = e.view(torch.uint8)
+        e = e.view(torch.uint8).transpose(0, 1).flatten(1)
     return (e.int() << 23).view(torch.float32).repeat_interleave(BLOCK, 1)[:, :K]
 
 
@@ -491,8 +492,8 @@ def exact(case, seed):
             c = slice(j * BLOCK, (j + 1) * BLOCK)
             a, b = t["x8"][:, c].double(), t["w8"][:, c].double()
             if k == "linear":
-                a = a * _two64(t["x_scale"].view(torch.uint8)[:, j].int() - 127)[:, None]
-            by = _two64(t["w_scale"].view(torch.uint8)[:, j].int() - 127)
+                a = a * _two64(t["x_scale"].view(torch.uint8)[j // 4, :, j % 4].int() - 127)[:, None]
+            by = _two64(t["w_scale"].view(torch.uint8)[j // 4, :, j % 4].int() - 127)
             b = b * by.repeat_interleave(BLOCK)[:b.shape[0], None]
             y = a @ b.T if y is None else y.addmm_(a, b.T)
         y = _parts(y, case["parts"])
