@@ -658,6 +658,144 @@ HCMS_API int hcms_layer_forward(hcms_ctx *ctx, const void *x, const void *w_qkv,
                                 int n_chunks, int dtype, int mode, void *main_stream,
                                 void *copy_stream, void *compute_stream);
 
+/* ------------------------------------------------------------------------ */
+/* Operators beside the chunk loop: norm, 8-bit products, rotary positions    */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Root-mean-square norm with the residual's addition, M rows of D elements:
+ *   h[m] = x[m] + residual[m],  y[m] = h[m] / sqrt(mean(h[m]^2) + eps) * weight
+ * h is rounded to the storage type when it is stored; y is computed from the
+ * unrounded sum, in fp32, and rounded once.  Without a residual (NULL, with h
+ * NULL) h is x.
+ *   x, residual : device, rows of D elements ldx and ldr elements apart
+ *   weight      : device, [D] of weight_dtype
+ *   y, h        : device, [M][D], disjoint from the inputs and each other
+ * Buffers need the alignment of their elements only.  8 <= D <= 16384, eps >= 0.
+ * hcms_rms_norm_fp8 gives y in 8 bits instead, as the operand of
+ * hcms_linear_fp8: q [M][D] and its scales, as hcms_quantize_fp8 with
+ * q_block 1 makes them of the fp32 y.  D a multiple of 16.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, ARG (eps), HIP.
+ */
+HCMS_API int hcms_rms_norm(const void *x, const void *residual, const void *weight, void *y, void *h,
+                           int M, int D, int64_t ldx, int64_t ldr, float eps, int dtype,
+                           int weight_dtype, void *stream);
+HCMS_API int hcms_rms_norm_fp8(const void *x, const void *residual, const void *weight, void *q,
+                               void *scale, void *h, int M, int D, int64_t ldx, int64_t ldr,
+                               float eps, int dtype, int weight_dtype, void *stream);
+
+/*
+ * Backward of hcms_rms_norm from its inputs, with the unrounded h = x + residual
+ * (residual NULL: x), n = h / sqrt(mean(h^2) + eps), g = dy weight:
+ *   dx[m] = (g - n mean(g n)) / sqrt(mean(h^2) + eps) + dh[m],  dw = sum_m dy n
+ * dx is the gradient of x and of the residual alike.
+ *   dy, dh : device, [M][D]: the gradients of y and of h (dh NULL: none)
+ *   x, residual, weight : as hcms_rms_norm took them
+ *   dx     : device, [M][D];  dw : device, [D] of weight_dtype (zeros for M = 0)
+ *   partial: device workspace, hcms_rms_norm_partials(M, D) rows of D floats
+ * No atomics: runs are deterministic.  Errors: as hcms_rms_norm.
+ * hcms_rms_norm_partials is host only (errors: SHAPE).
+ */
+HCMS_API int hcms_rms_norm_partials(int M, int D);
+HCMS_API int hcms_rms_norm_backward(const void *dy, const void *x, const void *residual, const void *dh,
+                                    const void *weight, void *dx, void *dw, float *partial, int M, int D,
+                                    int64_t ldx, int64_t ldr, float eps, int dtype, int weight_dtype,
+                                    void *stream);
+
+/*
+ * 8-bit floating point with block scales: e4m3 values (no infinities, largest
+ * 448) and, per block of 128 consecutive elements of a row or of 128 x 128, one
+ * scale, a power of two 2^(b - 127) held as its exponent byte b (e8m0).  The
+ * scale of a block is the smallest one from 2^-126 on that brings its largest
+ * magnitude to at most 448; values are x / scale rounded to nearest even.  A
+ * block that holds an infinity or a NaN gets the scale NaN (byte 255), and
+ * every product with it is NaN.
+ * Scales of an operand of R rows (or blocks of 128 rows) of K elements lie in
+ * groups of four blocks, [ceil(K / 512)][R][4] bytes: byte [g][r][i] belongs to
+ * block 4 g + i.  Bytes of blocks past K are those of a block of zeros (1).
+ *
+ * hcms_quantize_fp8 makes operands of x [M][K] (rows ldx elements apart):
+ *   q : [M][K], NULL for none; q_scale: per row (q_block 1, R = M) or per 128 x
+ *       128 (q_block 128, R = ceil(M / 128))
+ *   t : x transposed, [K][M'] with M' = M rounded up to 16, padded with zeros,
+ *       NULL for none; t_scale: blocks along M, per row of t (t_block 1, R = K)
+ *       or per 128 x 128 (t_block 128, R = ceil(K / 128)): [ceil(M / 512)][R][4]
+ * K a positive multiple of 16, at most 2^20.  Errors: NULL, SHAPE, DTYPE (of
+ * x), ALIGN (outputs 16 bytes), ALIAS, ARG (block), HIP.
+ */
+HCMS_API int hcms_quantize_fp8(const void *x, void *q, void *q_scale, int q_block, void *t,
+                               void *t_scale, int t_block, int M, int K, int64_t ldx, int dtype,
+                               void *stream);
+
+/*
+ * 8-bit product:  y[m][n] = sum_k x[m][k] w[n][k]  with the values x and w
+ * stand for, accumulated in fp32 and rounded once to `dtype`.
+ *   x : device, [M][K] e4m3;  x_scale : per row, [ceil(K / 512)][M][4]
+ *   w : device, [N][K] e4m3;  w_scale : per 128 x 128, [ceil(K / 512)][ceil(N / 128)][4]
+ *   y : device, [parts][M][N / parts]: column n in part n / (N / parts) (3 parts
+ *       of a QKV projection are its q, k and v as hcms_forward takes them)
+ * K a positive multiple of 16 and N of 8 parts, each at most 2^20; M >= 0.
+ * Deterministic.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, HIP.
+ */
+HCMS_API int hcms_linear_fp8(const void *x, const void *x_scale, const void *w, const void *w_scale,
+                             void *y, int M, int N, int K, int parts, int dtype, void *stream);
+
+/*
+ * Rotary positions of query and key heads, apart from the projection (where a
+ * norm of queries and keys stands between), forward and backward.  The first
+ * R = 2 sum(axis_pairs) <= d elements of every head vector turn by `table`
+ * (hcms_rope_table or hcms_rope_table_freqs of the same grid and axis_pairs):
+ * pair p, the elements (2p, 2p + 1) or, in the layout of halves, (p, p + R / 2),
+ *   (a, b) -> (a cos - b sin, a sin + b cos)      inverse: sin -> -sin
+ * for the token's coordinates; elements past R are copied.  The inverse is the
+ * transpose: the gradient's rotation, with a scaled table's magnitude kept.
+ *   q, k      : heads of a side (k may be NULL): input x and output y at
+ *               x + t x_token + h x_head (strides in elements); the output may be
+ *               the input itself (same address and strides)
+ *   positions : NULL (token t at place t of the row-major grid; S at most its
+ *               size) or device [S][n_axes] of position_bytes 4 (int32) or 8
+ *               (int64).  A token with a position outside the grid gets NaN.
+ * 2 <= d <= 512.  Buffers need the alignment of their elements only.
+ * Errors: NULL, SHAPE (sizes, strides, outputs that overlap themselves), DTYPE,
+ * ALIGN, ALIAS, ARG (layout, position_bytes, n_axes), HIP.
+ *
+ * hcms_rope_frequencies: the frequencies of `pairs` pairs, base^(-i / pairs),
+ *   scaled for contexts `factor` times longer than the trained ones:
+ *   HCMS_ROPE_LINEAR divides all by factor; HCMS_ROPE_NTK raises the base to
+ *   base factor^(pairs / (pairs - 1)), so that the slowest pair is slowed by
+ *   factor and the fastest not at all; HCMS_ROPE_YARN keeps pairs that turn at
+ *   least beta_fast times over original_length, slows those that turn at most
+ *   beta_slow times by factor and mixes linearly between, and gives the table
+ *   the magnitude 0.1 ln(factor) + 1.  Host only.  Errors: NULL, SHAPE (pairs
+ *   outside 1..256), ARG.
+ * hcms_rope_table_freqs: hcms_rope_table with given frequencies (freqs: host,
+ *   sum(axis_pairs) <= 256 doubles) and magnitude: entries magnitude (cos, sin).
+ */
+#define HCMS_ROPE_INTERLEAVED 0
+#define HCMS_ROPE_HALF 1
+
+#define HCMS_ROPE_UNSCALED 0
+#define HCMS_ROPE_LINEAR 1
+#define HCMS_ROPE_NTK 2
+#define HCMS_ROPE_YARN 3
+
+typedef struct hcms_rope_heads {
+    const void *x;
+    void *y;
+    int64_t x_token, x_head, y_token, y_head;
+    int heads;
+} hcms_rope_heads;
+
+HCMS_API int hcms_rope(const hcms_rope_heads *q, const hcms_rope_heads *k, const float *table,
+                       const int *grid, const int *axis_pairs, int n_axes, const void *positions,
+                       int position_bytes, int S, int d, int layout, int inverse, int dtype,
+                       void *stream);
+HCMS_API int hcms_rope_frequencies(int pairs, double base, int scaling, double factor,
+                                   double original_length, double beta_fast, double beta_slow,
+                                   double *freqs, double *magnitude);
+HCMS_API int hcms_rope_table_freqs(float *table, const int *grid, const int *axis_pairs, int n_axes,
+                                   const double *freqs, double magnitude, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

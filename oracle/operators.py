@@ -1,0 +1,121 @@
+"""Oracle for the operators beside the chunk loop: the root-mean-square norm with
+its gradients, 8-bit block quantisation and product, and rotary positions.
+
+TEST INFRASTRUCTURE ONLY.  Everything is float64 on the stored input values, from
+the definitions in ``include/hcms.h``; this module never imports the product path.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+
+BLOCK = 128
+
+
+# ---------------------------------------------------------------------------
+# Norm
+# ---------------------------------------------------------------------------
+def rms_norm(x, weight, eps, residual=None):
+    """(y, h) of rows: h = x + residual, y = h / sqrt(mean(h^2) + eps) weight."""
+    h = x if residual is None else x + residual
+    return h / np.sqrt((h * h).mean(axis=1, keepdims=True) + eps) * weight, h
+
+
+def rms_norm_backward(dy, x, weight, eps, residual=None, dh=None):
+    """(dx, dw): the gradients of sum(dy y) + sum(dh h)."""
+    h = x if residual is None else x + residual
+    r = 1.0 / np.sqrt((h * h).mean(axis=1, keepdims=True) + eps)
+    n, g = h * r, dy * weight
+    dx = r * (g - n * (g * n).mean(axis=1, keepdims=True))
+    return dx if dh is None else dx + dh, (dy * n).sum(axis=0)
+
+
+# ---------------------------------------------------------------------------
+# 8 bits
+# ---------------------------------------------------------------------------
+def e4m3(x):
+    """Nearest e4m3 value, ties to the even one: 3 bits behind the leading one
+    down to 2^-6, steps of 2^-9 below; |x| <= 448 is taken for granted."""
+    x = np.asarray(x, dtype=np.float64)
+    _, e = np.frexp(x)
+    step = np.ldexp(1.0, np.maximum(e - 1, -6) - 3)
+    return np.rint(x / step) * step
+
+
+def scale_exponent(amax: float) -> int:
+    """The smallest e >= -126 with amax <= 448 * 2^e; 128 (NaN) if amax is not finite."""
+    if not math.isfinite(amax):
+        return 128
+    e = -126
+    while amax > math.ldexp(448.0, e):
+        e += 1
+    return e
+
+
+def quantize(x, rows: int):
+    """(values on the e4m3 grid, exponents [blocks of rows][blocks of 128]) of x
+    [M][K], blocks of ``rows`` x 128."""
+    M, K = x.shape
+    q = np.zeros((M, K))
+    exps = np.zeros((-(-M // rows), -(-K // BLOCK)), dtype=np.int64)
+    for i in range(exps.shape[0]):
+        for j in range(exps.shape[1]):
+            b = x[i * rows:(i + 1) * rows, j * BLOCK:(j + 1) * BLOCK]
+            e = scale_exponent(float(np.abs(b).max()) if np.isfinite(b).all() else math.inf)
+            exps[i, j] = e
+            q[i * rows:(i + 1) * rows, j * BLOCK:(j + 1) * BLOCK] = \
+                e4m3(np.ldexp(b, -e)) if e < 128 else np.nan
+    return q, exps
+
+
+def held(x, rows: int):
+    """The values that x's 8-bit form stands for."""
+    q, e = quantize(x, rows)
+    s = np.repeat(np.repeat(np.where(e < 128, np.ldexp(1.0, np.minimum(e, 127)), np.nan), rows, 0),
+                  BLOCK, 1)
+    return q * s[:x.shape[0], :x.shape[1]]
+
+
+def scale_bytes(exps):
+    """Exponents [rows][blocks] as the bytes [groups of four][rows][4], the fill of
+    the last group being the scale of a block of zeros."""
+    rows, blocks = exps.shape
+    out = np.ones((-(-blocks // 4), rows, 4), dtype=np.uint8)
+    for b in range(blocks):
+        out[b // 4, :, b % 4] = exps[:, b] + 127
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions
+# ---------------------------------------------------------------------------
+def frequencies(pairs, base=10000.0, scaling="none", factor=1.0, original_length=0.0,
+                beta_fast=32.0, beta_slow=1.0):
+    """(frequencies, magnitude) from the wavelengths: pair i turns
+    original_length * f_i / (2 pi) times over the original length."""
+    i = np.arange(pairs, dtype=np.float64)
+    f = base ** (-i / pairs)
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling == "ntk":
+        return (f if pairs == 1 else (base * factor ** (pairs / (pairs - 1))) ** (-i / pairs)), 1.0
+    if scaling == "none":
+        return f, 1.0
+    # index (not rounded) of a pair that turns `beta` times
+    at = [pairs * math.log(original_length / (beta * 2 * math.pi)) / math.log(base)
+          for beta in (beta_fast, beta_slow)]
+    lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), pairs - 1)
+    slow = np.array([min(max((k - lo) / max(hi - lo, 1e-3), 0.0), 1.0) for k in range(pairs)])
+    return f * (1 - slow) + f / factor * slow, 0.1 * math.log(factor) + 1.0
+
+
+def rotate(x, angles, magnitude=1.0, layout="interleaved", inverse=False):
+    """x [S][H][d] with its first 2 * angles.shape[1] elements turned by angles
+    [S][pairs], by complex multiplication."""
+    x = np.array(x, dtype=np.float64)
+    P = angles.shape[1]
+    a, b = (slice(0, 2 * P, 2), slice(1, 2 * P, 2)) if layout == "interleaved" else (slice(0, P), slice(P, 2 * P))
+    z = (x[..., a] + 1j * x[..., b]) * (magnitude * np.exp((-1j if inverse else 1j) * angles))[:, None, :]
+    x[..., a], x[..., b] = z.real, z.imag
+    return x

@@ -99,6 +99,15 @@ def load():
         "hcms_rope_table_entries": ([ip, ip, i], i),
         "hcms_rope_table": ([vp, ip, ip, i, d, vp], i),
         "hcms_qkv_projection": ([vp, vp, vp, ip, ip, i, vp, vp, vp, i, i, i, i, i, vp], i),
+        "hcms_rms_norm": ([vp, vp, vp, vp, vp, i, i, i64, i64, f, i, i, vp], i),
+        "hcms_rms_norm_fp8": ([vp, vp, vp, vp, vp, vp, i, i, i64, i64, f, i, i, vp], i),
+        "hcms_rms_norm_partials": ([i, i], i),
+        "hcms_rms_norm_backward": ([vp, vp, vp, vp, vp, vp, vp, vp, i, i, i64, i64, f, i, i, vp], i),
+        "hcms_quantize_fp8": ([vp, vp, vp, i, vp, vp, i, i, i, i64, i, vp], i),
+        "hcms_linear_fp8": ([vp, vp, vp, vp, vp, i, i, i, i, i, vp], i),
+        "hcms_rope": ([vp, vp, vp, ip, ip, i, vp, i, i, i, i, i, i, vp], i),
+        "hcms_rope_frequencies": ([i, d, i, d, d, d, d, dp, dp], i),
+        "hcms_rope_table_freqs": ([vp, ip, ip, i, dp, d, vp], i),
         "hcms_layer_forward": ([vp, vp, vp, vp, vp, ip, ip, i, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                 i, i, i, i, i, f, ip, i, i, i, vp, vp, vp], i),
     }
@@ -745,3 +754,8 @@ class HcmsAttention(torch.autograd.Function):
         ctx, P, scale, sizes, mode, ws, lse = fctx.hcms
         dq, dk, dv = ctx.backward(dout.contiguous(), P, scale, sizes, ws, lse, mode=mode)
         return dq, dk, dv, None, None, None, None, None
+
+
+from .operators import (E4M3, E8M0, SCALE_BLOCK, Fp8Linear, RmsNorm, Rope, linear_fp8,  # noqa: E402,F401
+                        quantize_fp8, rms_norm, rms_norm_backward, rms_norm_fp8, rope,
+                        rope_frequencies, rope_table_freqs)

@@ -20,7 +20,8 @@ LIB = os.path.join(PKG, "libhcms.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-SOURCES = ["api.cpp", "model.cpp", "pack.hip", "attention.hip", "attention_bwd.hip", "linear.hip"]
+SOURCES = ["api.cpp", "ops.cpp", "model.cpp", "pack.hip", "attention.hip", "attention_bwd.hip", "linear.hip",
+           "linear_fp8.hip", "quantize.hip", "rmsnorm.hip", "rope.hip"]
 
 COMMON = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

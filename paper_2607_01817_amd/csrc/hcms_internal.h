@@ -139,4 +139,52 @@ hipError_t launch_qkv_projection(const void *x, const void *w, void *q, void *k,
 // Fills the rotation table of `ax` (fp32 (cos, sin) pairs).
 hipError_t launch_rope_table(float *table, const RopeAxes &ax, double base, hipStream_t stream);
 
+// Rotary positions of queries and keys: one side's heads, strides in elements.
+struct RopeSide {
+    const void *x;
+    void *y;
+    int64_t x_token, x_head, y_token, y_head;
+    int H;
+};
+// The first R = 2 * (pairs of ax) elements of each head vector of d turn;
+// positions: NULL (row-major on the grid) or [S][n_axes] int32 or int64.
+hipError_t launch_rope(const RopeSide &q, const RopeSide &k, const float *table, const RopeAxes &ax,
+                       const void *positions, bool pos64, int S, int d, int R, bool half, bool inverse,
+                       int dtype, hipStream_t stream);
+inline constexpr int kRopeMaxPairs = 256;
+struct RopeFreqs {
+    double f[kRopeMaxPairs];
+};
+hipError_t launch_rope_table_freqs(float *table, const RopeAxes &ax, const RopeFreqs &freqs, double magnitude,
+                                   hipStream_t stream);
+
+// Largest D of the norm and its backward (rows are held in registers).
+int rms_norm_max_width();
+// RMS norm of rows of h = x + r (r NULL: h = x, not stored), in the storage
+// type into y or, q not NULL, in 8 bits into q and scale (fp8.h).
+hipError_t launch_rms_norm(const void *x, const void *r, const void *w, bool w_f32, void *y, void *q,
+                           void *scale, void *h, int64_t M, int D, int64_t ldx, int64_t ldr, float eps,
+                           int dtype, hipStream_t stream);
+// Its backward; partial: rms_norm_partials(M, D) rows of D floats.
+int rms_norm_partials(int64_t M, int D);
+hipError_t launch_rms_norm_backward(const void *dy, const void *x, const void *r, const void *dh, const void *w,
+                                    bool w_f32, void *dx, void *dw, float *partial, int64_t M, int D, int64_t ldx,
+                                    int64_t ldr, float eps, int dtype, hipStream_t stream);
+
+// Operands of the 8-bit product from x [M][K] (either may be NULL): q by rows,
+// t transposed; *_square: one scale per 128 x 128 instead of per row and 128.
+struct QuantizeOut {
+    unsigned char *q, *q_scale;
+    bool q_square;
+    unsigned char *t, *t_scale;
+    bool t_square;
+};
+hipError_t launch_quantize_fp8(const void *x, int64_t ldx, const QuantizeOut &out, int64_t M, int K, int dtype,
+                               hipStream_t stream);
+
+// 8-bit product Y[M][N] = X[M][K] W[N][K]^T of e4m3 operands, X's scales per
+// row and 128 k, W's per 128 x 128; y in `parts` tensors [M][N / parts].
+hipError_t launch_linear_fp8(const void *x, const void *x_scale, const void *w, const void *w_scale, void *y,
+                             int M, int N, int K, int parts, int dtype, hipStream_t stream);
+
 }  // namespace hcms

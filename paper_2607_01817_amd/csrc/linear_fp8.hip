@@ -1,0 +1,400 @@
+// 8-bit product for gfx950 (MI355X), scaled MFMA with fp32 accumulation:
+//   Y[m][n] = sum_b 2^(sx[m][b] + sw[n / 128][b]) sum_{k in b} X[m][k] W[n][k]
+// X [M][K] and W [N][K] e4m3, b the blocks of 128 k, sx and sw the exponents
+// of fp8.h.  v_mfma_scale_f32_32x32x64_f8f6f4 takes the exponents as operands,
+// so the scales cost no arithmetic and the sum over blocks stays in the MFMA's
+// accumulators.
+//
+// Work decomposition
+//   * one workgroup computes a BM x BN tile of Y, its waves WM x WN rectangles
+//     of 32 x 32 MFMA tiles of Y^T: D[n][m], W rows as the A operand, X rows
+//     as the B operand, each lane holding one row m.  Whatever the tile, every
+//     element sums its products in the order of k, so all tiles give the same
+//     bits;
+//   * k advances in stages of 128 bytes per row, one block of the scales,
+//     which go from global memory straight into one of ST LDS buffers, as the
+//     stage's scales do (one dword, a group of four blocks, per row of X and
+//     per 128 rows of W);
+//   * one barrier per stage, placed where the operands of the stage's last
+//     k-step are already in registers: past it the stage's buffer is free and
+//     the next stage is in LDS;
+//   * workgroups are persistent, their tiles form one stream of stages, and
+//     the tile order gives each XCD a contiguous range of each round (groups
+//     of 8 row tiles), so that its L2 serves shared panels.
+//
+// Tails: rows past M or N and k past K are read as zeros through buffer
+// resources; rows past M and columns past N are not stored.  K is a multiple
+// of 16 and N / parts of 8 (checked by the caller).
+#include "attention_tiles.h"
+#include "fp8.h"
+#include "hcms_internal.h"
+#include "linear_fp8_tiles.h"
+
+namespace hcms {
+namespace {
+
+using namespace tiles;
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kGroupM = 8;   // row tiles per group of the tile order
+
+template <int BM_, int BN_, int WM_, int WN_, int ST_, int PER_CU_>
+struct Tile {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_, PER_CU = PER_CU_;
+    static constexpr int W = WM * WN, THREADS = 64 * W;
+    static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;   // 32 x 32 tiles per wave
+    static constexpr int XL = BM / 8 / W, WL = BN / 8 / W;       // operand loads per wave and stage
+    static constexpr int SCALE_B = (BM + 64) * 4;                // scales of a stage: X rows, W blocks
+    static constexpr int STAGE_B = (BM + BN) * 128 + SCALE_B;
+    static constexpr int OUT_B = 2048;                           // output staging per wave
+    static constexpr int LDS_B = ST * STAGE_B + W * OUT_B;
+    static_assert(XL * 8 * W == BM && WL * 8 * W == BN && W % 2 == 0, "whole loads per wave");
+    static_assert(BM % 64 == 0 && BM / 64 < W, "one scale load per wave");
+    static_assert(BN >= 128 ? BN % 128 == 0 : 128 % BN == 0, "tiles hold whole scale blocks or lie in one");
+    static_assert(128 % (NT * 32) == 0, "a wave's columns lie in one scale block");
+    static_assert(LDS_B * PER_CU <= 160 * 1024 && ST >= 2, "LDS of a CU");
+};
+
+// Resource over `bytes` bytes (at most 2^28) from base on.
+__device__ inline __amdgpu_buffer_rsrc_t span(const void *base, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000);
+}
+
+// A wave's MT x NT tiles at rows mb .., columns nb .. of Y.  Lane (li, g)
+// holds row mb + 32 mt + li and, per 32 x 32 tile, runs of 4 consecutive
+// columns 8 rb + 4 g; they pass through a private 2 KiB of LDS, 32 rows by 64
+// bytes at a time, to leave as 16 bytes per lane and 64 per row.  Chunk c of
+// staged row r sits at position c ^ (r / 4 % 4).  Column n of Y lies in part
+// n / np (np is a multiple of 8, so no chunk crosses parts).
+template <typename T, typename C>
+__device__ inline void store_tile(f32x16 (&acc)[C::NT][C::MT], char *stage, T *y, int np, int mb, int nb, int M,
+                                  int N, int lane) {
+    constexpr int SEG = sizeof(T) == 2 ? 1 : 2;          // segments per 32 columns
+    constexpr int E = 16 / static_cast<int>(sizeof(T));  // elements per chunk
+    const int li = lane & 31, g = lane >> 5;
+#pragma unroll
+    for (int mt = 0; mt < C::MT; ++mt) {
+#pragma unroll
+        for (int sg = 0; sg < C::NT * SEG; ++sg) {
+            const f32x16 &t = acc[sg / SEG][mt];
+#pragma unroll
+            for (int i = 0; i < 4 / SEG; ++i) {
+                const int rb = (sg % SEG) * 2 + i;
+                const f32x4 v = {t[rb * 4 + 0], t[rb * 4 + 1], t[rb * 4 + 2], t[rb * 4 + 3]};
+                if constexpr (sizeof(T) == 2)
+                    *reinterpret_cast<bf16x4 *>(stage + li * 64 + ((i ^ ((li >> 2) & 3)) << 4) + g * 8) =
+                        __builtin_convertvector(v, bf16x4);
+                else
+                    *reinterpret_cast<f32x4 *>(stage + li * 64 + (((i * 2 + g) ^ ((li >> 2) & 3)) << 4)) = v;
+            }
+            const int ch = lane & 3;
+            const int n = nb + sg * (32 / SEG) + ch * E;
+            const int part = n / np;
+            T *col = y + static_cast<int64_t>(part) * M * np + (n - part * np);
+            u32x4 o[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int row = q * 16 + (lane >> 2);
+                o[q] = *reinterpret_cast<const u32x4 *>(stage + row * 64 + ((ch ^ ((row >> 2) & 3)) << 4));
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int mm = mb + mt * 32 + q * 16 + (lane >> 2);
+                if (mm < M && n < N) *reinterpret_cast<u32x4 *>(col + static_cast<int64_t>(mm) * np) = o[q];
+            }
+        }
+    }
+}
+
+template <typename T, typename C>
+__global__ __launch_bounds__(C::THREADS, C::PER_CU *C::W / 4) void linear_fp8_kernel(
+    const unsigned char *__restrict__ x, const unsigned *__restrict__ xs, const unsigned char *__restrict__ w,
+    const unsigned *__restrict__ ws, T *__restrict__ y, int M, int N, int K, int np, int tiles_m, int tiles_n) {
+    constexpr int MT = C::MT, NT = C::NT, ST = C::ST, W = C::W;
+    constexpr int LPW = C::XL + C::WL + 1;   // loads per wave and stage, the last one of scales
+    constexpr int kHalf = (LPW + 1) / 2;     // of them right behind the barrier
+    __shared__ __attribute__((aligned(1024))) char lds[C::LDS_B];
+
+    const int G = gridDim.x, b = blockIdx.x;
+    const int xcd = b & 7, per = G >> 3, rem = G & 7;
+    const int slot = xcd * per + min(xcd, rem) + (b >> 3);
+    const int n_tiles = tiles_m * tiles_n;
+    if (slot >= n_tiles) return;
+    const int n_mine = (n_tiles - 1 - slot) / G + 1;
+    auto origin = [&](int r, int &m0, int &n0) {
+        const int L = r * G + slot;
+        const int group = L / (kGroupM * tiles_n);
+        const int first_m = group * kGroupM;
+        const int gm = min(tiles_m - first_m, kGroupM);
+        const int in_group = L - group * kGroupM * tiles_n;
+        m0 = (first_m + in_group % gm) * C::BM;
+        n0 = (in_group / gm) * C::BN;
+    };
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int li = lane & 31, g = lane >> 5;
+    const int wm = wave / C::WN, wn = wave % C::WN;
+    const int nkb = (K + 127) / 128, n_blocks = (N + 127) / 128;
+
+    // Load i of a wave brings rows 8 (i W + wave) + lane / 8 of the stage's X
+    // rows (then of its W rows), 16 bytes per lane; the lane at position
+    // lane % 8 of its row fetches chunk (lane % 8) ^ (row / 2 % 8), so that 16
+    // rows of one chunk lie in 16 different groups of 4 banks.  A chunk past K
+    // is fetched from past the resource: zeros.
+    const unsigned chunk = ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) << 4;
+    const unsigned voff_in = (8 * wave + (lane >> 3)) * static_cast<unsigned>(K) + chunk;
+    const unsigned voff_end = (nkb - 1) * 128u + chunk < static_cast<unsigned>(K) ? voff_in : 0x80000000u;
+    const unsigned pass_bytes = 8u * W * K;
+    const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(lds));
+
+    // The stages of the workgroup's tiles form one stream.  A stage past its
+    // end is loaded through empty resources: zeros into a buffer that nobody
+    // reads, so that every step issues the same number of loads.
+    int ld_r = 0, ld_kb = 0;
+    int lm0, ln0;
+    unsigned voff;
+    __amdgpu_buffer_rsrc_t lxs, lws, lss;
+    // Scales of stage ld_kb: the first BM / 64 waves bring X's, 64 rows each,
+    // the others (all alike) W's.
+    const bool scale_of_x = wave < C::BM / 64;
+    auto scales = [&]() {
+        const int64_t grp = ld_kb >> 2;
+        lss = scale_of_x ? span(xs + grp * M + lm0, min(M - lm0, C::BM) * 4)
+                         : span(ws + grp * n_blocks + ln0 / 128, min(n_blocks - ln0 / 128, 64) * 4);
+    };
+    auto panels = [&]() {
+        origin(ld_r, lm0, ln0);
+        lxs = span(x + static_cast<int64_t>(lm0) * K, min(M - lm0, C::BM) * K);
+        lws = span(w + static_cast<int64_t>(ln0) * K, min(N - ln0, C::BN) * K);
+        scales();
+    };
+    panels();
+    voff = nkb == 1 ? voff_end : voff_in;
+    const unsigned scale_voff = (scale_of_x ? wave * 64 + lane : lane) * 4;
+    const unsigned scale_dst = (C::BM + C::BN) * 128 + (scale_of_x ? wave : C::BM / 64) * 256;
+    auto load_one = [&](int i, int buf) {
+        const unsigned base = lds0 + buf * C::STAGE_B;
+        if (i == LPW - 1) {
+            load_lds_b32(base + scale_dst, lss, scale_voff, 0);
+            return;
+        }
+        const unsigned dst = base + (i * W + wave) * 1024;
+        const unsigned soff = ld_kb * 128;
+        if (i < C::XL) load_lds(dst, lxs, voff, soff + i * pass_bytes);
+        else load_lds(dst, lws, voff, soff + (i - C::XL) * pass_bytes);
+    };
+    auto advance = [&]() {
+        if (++ld_kb < nkb) {
+            if ((ld_kb & 3) == 0 && ld_r < n_mine) scales();
+            voff = ld_kb == nkb - 1 ? voff_end : voff_in;
+            return;
+        }
+        ld_kb = 0;
+        voff = nkb == 1 ? voff_end : voff_in;
+        if (++ld_r < n_mine) {
+            panels();
+        } else {
+            lxs = span(x, 0);
+            lws = span(w, 0);
+            lss = span(xs, 0);
+        }
+    };
+
+    const unsigned rd = li * 128 + ((g ^ ((li >> 1) & 7)) << 4);
+    const char *const xrd = lds + wm * MT * 32 * 128;
+    const char *const wrd = lds + C::BM * 128 + wn * NT * 32 * 128;
+    const char *const xsrd = lds + (C::BM + C::BN) * 128 + (wm * MT * 32 + li) * 4;
+    const char *const wsrd = lds + (C::BM + C::BN) * 128 + C::BM * 4 + (wn * NT / 4) * 4;
+
+    // fp32 output: the 8-bit MFMA aligns groups of 8 products to the largest and
+    // cuts each 13 binary places below that one's leading digit (relative error
+    // 1.4e-5 on normal operands, a hundredth of the rounding to bf16), so for
+    // fp32 output the operands are widened to bf16, exactly, scales included,
+    // and multiplied at the bf16 rate, whose MFMA keeps fp32 sums (6e-8).
+    constexpr bool kWide = sizeof(T) == 4;
+    f32x16 acc[NT][MT];
+    i32x8 a[2][NT], bx[2][MT];
+    int sx[MT], sw, sx_next[MT], sw_next;
+    // Operand of k-step ks (64 k, 4 chunks of a staged row): lane half g takes
+    // chunks g and 2 + g of them, of both operands alike.
+    auto operand = [&](const char *p, int ks) {
+        const i32x4 lo = *reinterpret_cast<const i32x4 *>(p + (rd ^ (ks << 6)));
+        const i32x4 hi = *reinterpret_cast<const i32x4 *>(p + (rd ^ (ks << 6) ^ 32));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    auto read_ops = [&](int set, int ks, int buf) {
+        const int base = buf * C::STAGE_B;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) a[set][nt] = operand(wrd + base + nt * 32 * 128, ks);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) bx[set][mt] = operand(xrd + base + mt * 32 * 128, ks);
+    };
+    auto read_scales = [&](int buf) {
+        const int base = buf * C::STAGE_B;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sx_next[mt] = *reinterpret_cast<const int *>(xsrd + base + mt * 32 * 4);
+        sw_next = *reinterpret_cast<const int *>(wsrd + base);
+    };
+    // The stage's byte of the group's four into the lowest place.
+    auto take_scales = [&](int kb) {
+        const int sh = (kb & 3) * 8;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sx[mt] = static_cast<unsigned>(sx_next[mt]) >> sh;
+        sw = static_cast<unsigned>(sw_next) >> sh;
+        if constexpr (kWide) {   // as fp32 exponents
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) sx[mt] = (sx[mt] & 255) << 23;
+            sw = (sw & 255) << 23;
+        }
+    };
+    // 8 values of a k-step, quarter t, widened and scaled.
+    auto widened = [&](const i32x8 &v, int t, int s) {
+        const float by = __builtin_bit_cast(float, s);
+        const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * t], by, false);
+        const bf16x2 p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * t], by, true);
+        const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * t + 1], by, false);
+        const bf16x2 p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * t + 1], by, true);
+        return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+    };
+    auto mfma = [&](int set, int i) {
+        const int nt = i / MT, mt = i % MT;
+        acc[nt][mt] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[set][nt], bx[set][mt], acc[nt][mt], 0, 0, 0,
+                                                                      sw, 0, sx[mt]);
+    };
+
+#pragma unroll
+    for (int st = 0; st < ST; ++st) {
+        const int n = st < ST - 1 ? LPW : kHalf;
+#pragma unroll
+        for (int i = 0; i < LPW; ++i)
+            if (i < n) load_one(i, st);
+        if (st < ST - 1) advance();
+    }
+    wait_vm<(ST - 2) * LPW + kHalf>();
+    __syncthreads();
+    read_ops(0, 0, 0);
+    read_scales(0);
+
+    // MFMAs of operand set `set` with the loads l0 .. l1 - 1 into `into`.
+    auto phase = [&](int set, int l0, int l1, int into) {
+        constexpr int kMf = NT * MT * (kWide ? 4 : 1);
+        bf16x8 aw[NT], bw[MT];
+#pragma unroll
+        for (int i = 0; i < kMf; ++i) {
+            if constexpr (kWide) {
+                const int t = i / (NT * MT), nt = i % (NT * MT) / MT, mt = i % MT;
+                if (i % (NT * MT) == 0) {
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) aw[k] = widened(a[set][k], t, sw);
+#pragma unroll
+                    for (int k = 0; k < MT; ++k) bw[k] = widened(bx[set][k], t, sx[k]);
+                }
+                acc[nt][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(aw[nt], bw[mt], acc[nt][mt], 0, 0, 0);
+            } else {
+                mfma(set, i);
+            }
+#pragma unroll
+            for (int l = 0; l < LPW; ++l)
+                if (l >= l0 && l < l1 && (l - l0) * kMf / (l1 - l0) == i) load_one(l, into);
+            if (l0 < l1) __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int buf = 0, prev = ST - 1;
+    for (int r = 0; r < n_mine; ++r) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = f32x16{};
+        // End the scalar loads of the code before the loop (simm16: lgkmcnt 0,
+        // the others open).
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+        take_scales(0);
+        for (int kb = 0; kb < nkb; ++kb) {
+            // The first k-step, beside the operand reads of the second; it
+            // also issues the second half of the loads into the buffer that
+            // the step before freed.
+            read_ops(1, 1, buf);
+            __builtin_amdgcn_sched_barrier(0);
+            phase(0, kHalf, LPW, prev);
+            advance();
+            // The second k-step's operands are in registers: past this barrier
+            // the stage's buffer is free and the next stage is in LDS.
+            wait_vm<(ST - 2) * LPW>();
+            __syncthreads();
+            const int next = buf + 1 == ST ? 0 : buf + 1;
+            read_ops(0, 0, next);
+            read_scales(next);
+            __builtin_amdgcn_sched_barrier(0);
+            phase(1, 0, kHalf, buf);
+            if (kb + 1 < nkb) take_scales(kb + 1);
+            prev = buf;
+            buf = next;
+        }
+        int m0, n0;
+        origin(r, m0, n0);
+        store_tile<T, C>(acc, lds + ST * C::STAGE_B + wave * C::OUT_B, y, np, m0 + wm * MT * 32, n0 + wn * NT * 32,
+                         M, N, lane);
+    }
+    wait_vm<0>();   // no load into LDS is pending when the workgroup ends
+}
+
+template <typename T, typename C>
+hipError_t launch_tile(const void *x, const void *xs, const void *w, const void *ws, void *y, int M, int N, int K,
+                       int np, int n_cu, hipStream_t stream) {
+    const int tiles_m = (M + C::BM - 1) / C::BM, tiles_n = (N + C::BN - 1) / C::BN;
+    const int64_t tiles = static_cast<int64_t>(tiles_m) * tiles_n;
+    if (tiles < 1 || tiles > 0x3fffffff) return hipErrorInvalidValue;
+    const int64_t slots = static_cast<int64_t>(n_cu) * C::PER_CU;
+    const int64_t blocks = tiles > slots ? slots : tiles;
+    linear_fp8_kernel<T, C><<<static_cast<unsigned>(blocks), C::THREADS, 0, stream>>>(
+        static_cast<const unsigned char *>(x), static_cast<const unsigned *>(xs),
+        static_cast<const unsigned char *>(w), static_cast<const unsigned *>(ws), static_cast<T *>(y), M, N, K, np,
+        tiles_m, tiles_n);
+    return hipGetLastError();
+}
+
+// The tiles in the order of kFp8Tiles.
+using TileA = Tile<256, 256, 4, 2, 2, 1>;
+using TileB = Tile<128, 128, 4, 2, 4, 1>;
+using TileC = Tile<64, 128, 2, 2, 4, 1>;
+using TileD = Tile<64, 64, 2, 2, 4, 2>;
+template <typename C>
+constexpr bool costs_of(const Fp8TileCost &c) {
+    return c.bm == C::BM && c.bn == C::BN && c.per_cu == C::PER_CU;
+}
+static_assert(costs_of<TileA>(kFp8Tiles[0]) && costs_of<TileB>(kFp8Tiles[1]) && costs_of<TileC>(kFp8Tiles[2]) &&
+              costs_of<TileD>(kFp8Tiles[3]));
+
+template <typename T>
+hipError_t launch_typed(const void *x, const void *xs, const void *w, const void *ws, void *y, int M, int N, int K,
+                        int np, hipStream_t stream) {
+    int device = 0, n_cu = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, device);
+    if (e != hipSuccess) return e;
+    if (n_cu < 1) return hipErrorInvalidValue;
+    switch (fp8_tile(M, N, (K + 127) / 128, n_cu, sizeof(T) == 4)) {
+        case 0:
+            if constexpr (sizeof(T) == 2) return launch_tile<T, TileA>(x, xs, w, ws, y, M, N, K, np, n_cu, stream);
+            else break;
+        case 1: return launch_tile<T, TileB>(x, xs, w, ws, y, M, N, K, np, n_cu, stream);
+        case 2: return launch_tile<T, TileC>(x, xs, w, ws, y, M, N, K, np, n_cu, stream);
+        case 3: return launch_tile<T, TileD>(x, xs, w, ws, y, M, N, K, np, n_cu, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_linear_fp8(const void *x, const void *x_scale, const void *w, const void *w_scale, void *y, int M,
+                             int N, int K, int parts, int dtype, hipStream_t stream) {
+    if (M == 0 || N == 0) return hipSuccess;
+    if (dtype == 0) return launch_typed<__bf16>(x, x_scale, w, w_scale, y, M, N, K, N / parts, stream);
+    return launch_typed<float>(x, x_scale, w, w_scale, y, M, N, K, N / parts, stream);
+}
+
+}  // namespace hcms

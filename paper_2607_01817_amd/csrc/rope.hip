@@ -1,0 +1,201 @@
+// Rotary positions: the first R elements of every query and key head vector
+// turn, pair by pair, by the (cos, sin) that the rotation table holds for the
+// token's coordinates:
+//   (a, b) -> (a cos - b sin, a sin + b cos)
+// Pair p is the elements (2p, 2p + 1), or (p, p + R/2) in the layout of
+// halves.  The inverse flag turns by the negative angle with the table's
+// magnitude kept, which is the transpose and so the backward.  Elements past R
+// are copied.
+//
+// What bounds it: bytes, once in and once out.  A thread takes one unit (8
+// elements, in the layout of halves 8 and their partners) of one token and
+// goes through the heads with it, so the table entries and the coordinates
+// are read once for all of them.
+#include "fp8.h"
+#include "hcms_internal.h"
+
+namespace hcms {
+namespace {
+
+constexpr int kAhead = 4;   // heads whose loads are in flight together
+
+template <typename T, int V>
+struct Unit;   // V elements of T in one access
+template <typename T>
+struct Unit<T, 1> {
+    float v[1];
+    __device__ void load(const T *p) { v[0] = static_cast<float>(*p); }
+    __device__ void store(T *p) const { *p = static_cast<T>(v[0]); }
+};
+template <typename T>
+struct Unit<T, 8> {
+    float v[8];
+    __device__ void load(const T *p) {
+        const fp8::f32x8 x = widen(load_raw(p));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = x[i];
+    }
+    __device__ void store(T *p) const {
+        store_8(p, fp8::f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
+    }
+};
+
+// V: elements per access, 8 or 1.  Units of a head vector: the rotated ones,
+// then those that are copied (V or, with V = 1, 2 elements).
+template <typename T, int V, bool HALF>
+__global__ __launch_bounds__(256) void rope_kernel(RopeSide qs, RopeSide ks, const float *__restrict__ table,
+                                                   RopeAxes ax, const void *__restrict__ positions, bool pos64,
+                                                   int S, int d, int R, bool inverse, int heads_per_block) {
+    constexpr int NP = HALF ? V : (V == 1 ? 1 : V / 2);   // pairs per rotated unit
+    constexpr bool TWO = HALF || V == 1;                  // a unit is two accesses
+    constexpr int CP = V == 1 ? 2 : V;                    // elements per copied unit
+    const int turn = R / 2 / NP, units = turn + (d - R + CP - 1) / CP;
+    const int per = 256 / units;                          // tokens per workgroup
+    const int lt = threadIdx.x / units, u = threadIdx.x - lt * units;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * per + lt;
+    if (lt >= per || token >= S) return;
+
+    const bool rotates = u < turn;
+    // First elements of the unit's two accesses.
+    const int p0 = u * NP;
+    const int e0 = rotates ? (HALF ? p0 : 2 * p0) : R + (u - turn) * CP;
+    const int e1 = rotates ? (HALF ? p0 + R / 2 : 2 * p0 + 1) : e0 + 1;
+    const bool second = TWO && (rotates || (V == 1 && e1 < d));
+    float c[NP], s[NP];
+    if (rotates) {
+        int row[kRopeMaxAxes] = {};
+        bool inside = true;
+        if (positions) {
+            for (int a = 0; a < ax.n_axes; ++a) {
+                const int64_t i = token * ax.n_axes + a;
+                const int64_t at = pos64 ? static_cast<const int64_t *>(positions)[i]
+                                         : static_cast<int64_t>(static_cast<const int *>(positions)[i]);
+                const bool ok = at >= 0 && at < ax.grid[a];
+                inside = inside && ok;
+                row[a] = ax.tab_off[a] + (ok ? static_cast<int>(at) : 0) * ax.pairs[a] - ax.pair_start[a];
+            }
+        } else {
+            int rest = static_cast<int>(token);
+            for (int a = ax.n_axes - 1; a >= 0; --a) {
+                const int cc = rest % ax.grid[a];
+                rest /= ax.grid[a];
+                row[a] = ax.tab_off[a] + cc * ax.pairs[a] - ax.pair_start[a];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int p = p0 + i;
+            int at = row[0];
+#pragma unroll
+            for (int a = 1; a < kRopeMaxAxes; ++a)
+                if (a < ax.n_axes && p >= ax.pair_start[a]) at = row[a];
+            const float2 cs = reinterpret_cast<const float2 *>(table)[at + p];
+            // A position outside the grid: NaN, never another position's angle.
+            c[i] = inside ? cs.x : __builtin_nanf("");
+            s[i] = inside ? (inverse ? -cs.y : cs.y) : __builtin_nanf("");
+        }
+    }
+    const int heads = qs.H + ks.H;
+    const int hb = blockIdx.y * heads_per_block, he = min(hb + heads_per_block, heads);
+    for (int h0 = hb; h0 < he; h0 += kAhead) {
+        Unit<T, V> a[kAhead], b[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int h = h0 + k;
+            if (h >= he) break;
+            const RopeSide &side = h < qs.H ? qs : ks;
+            const T *x = static_cast<const T *>(side.x) + token * side.x_token + (h < qs.H ? h : h - qs.H) * side.x_head;
+            a[k].load(x + e0);
+            if (second) b[k].load(x + e1);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int h = h0 + k;
+            if (h >= he) break;
+            if (rotates) {
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    float &x0 = a[k].v[TWO ? i : 2 * i];
+                    float &x1 = TWO ? b[k].v[i] : a[k].v[2 * i + 1];
+                    const float u0 = x0, u1 = x1;
+                    x0 = __builtin_fmaf(u0, c[i], -(u1 * s[i]));
+                    x1 = __builtin_fmaf(u0, s[i], u1 * c[i]);
+                }
+            }
+            const RopeSide &side = h < qs.H ? qs : ks;
+            T *y = static_cast<T *>(side.y) + token * side.y_token + (h < qs.H ? h : h - qs.H) * side.y_head;
+            a[k].store(y + e0);
+            if (second) b[k].store(y + e1);
+        }
+    }
+}
+
+// Rotation table from given frequencies: entry of axis a, coordinate c, pair i
+// of the axis is magnitude * (cos, sin)(c * freq), computed in fp64.
+__global__ __launch_bounds__(256) void rope_table_freqs_kernel(float *table, RopeAxes ax, RopeFreqs f,
+                                                               double magnitude, int total) {
+    const int e = blockIdx.x * 256 + threadIdx.x;
+    if (e >= total) return;
+    int a = 0;
+    while (a + 1 < ax.n_axes && e >= ax.tab_off[a + 1]) ++a;
+    const int rel = e - ax.tab_off[a];
+    const double ang = static_cast<double>(rel / ax.pairs[a]) * f.f[ax.pair_start[a] + rel % ax.pairs[a]];
+    table[2 * e] = static_cast<float>(magnitude * cos(ang));
+    table[2 * e + 1] = static_cast<float>(magnitude * sin(ang));
+}
+
+template <typename T, int V, bool HALF>
+hipError_t run_rope(const RopeSide &q, const RopeSide &k, const float *table, const RopeAxes &ax,
+                    const void *positions, bool pos64, int S, int d, int R, bool inverse, hipStream_t stream) {
+    constexpr int NP = HALF ? V : (V == 1 ? 1 : V / 2), CP = V == 1 ? 2 : V;
+    const int units = R / 2 / NP + (d - R + CP - 1) / CP;
+    if (units < 1 || units > 256) return hipErrorInvalidValue;
+    const int per = 256 / units, heads = q.H + k.H;
+    const int64_t blocks = (S + static_cast<int64_t>(per) - 1) / per;
+    // All heads in one workgroup once the tokens alone make 1024 of them, down
+    // to kAhead heads each for a few tokens.
+    int split = 1;
+    while (split * blocks < 1024 && (heads + split - 1) / split > kAhead) split *= 2;
+    const int each = (heads + split - 1) / split;
+    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>((heads + each - 1) / each));
+    rope_kernel<T, V, HALF><<<grid, 256, 0, stream>>>(q, k, table, ax, positions, pos64, S, d, R, inverse, each);
+    return hipGetLastError();
+}
+
+bool by_eight(const RopeSide &s) {
+    return s.H == 0 || (s.x_token % 8 == 0 && s.x_head % 8 == 0 && s.y_token % 8 == 0 && s.y_head % 8 == 0);
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeSide &q, const RopeSide &k, const float *table, const RopeAxes &ax,
+                       const void *positions, bool pos64, int S, int d, int R, bool half, bool inverse,
+                       int dtype, hipStream_t stream) {
+    if (S == 0 || q.H + k.H == 0) return hipSuccess;
+    // 8 elements per access where no access crosses a boundary of the head's
+    // parts; else one element.
+    const bool wide = d % 8 == 0 && R % (half ? 16 : 8) == 0 && by_eight(q) && by_eight(k);
+#define HCMS_RUN(T, V, HALF) return run_rope<T, V, HALF>(q, k, table, ax, positions, pos64, S, d, R, inverse, stream)
+    if (dtype == 0) {
+        if (wide && half) HCMS_RUN(__bf16, 8, true);
+        if (wide) HCMS_RUN(__bf16, 8, false);
+        if (half) HCMS_RUN(__bf16, 1, true);
+        HCMS_RUN(__bf16, 1, false);
+    }
+    if (wide && half) HCMS_RUN(float, 8, true);
+    if (wide) HCMS_RUN(float, 8, false);
+    if (half) HCMS_RUN(float, 1, true);
+    HCMS_RUN(float, 1, false);
+#undef HCMS_RUN
+}
+
+hipError_t launch_rope_table_freqs(float *table, const RopeAxes &ax, const RopeFreqs &freqs, double magnitude,
+                                   hipStream_t stream) {
+    const int last = ax.n_axes - 1;
+    const int total = ax.tab_off[last] + ax.grid[last] * ax.pairs[last];
+    if (total == 0) return hipSuccess;
+    rope_table_freqs_kernel<<<(total + 255) / 256, 256, 0, stream>>>(table, ax, freqs, magnitude, total);
+    return hipGetLastError();
+}
+
+}  // namespace hcms
