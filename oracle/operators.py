@@ -55,23 +55,29 @@ def scale_exponent(amax: float) -> int:
 
 def quantize(x, rows: int):
     """(values on the e4m3 grid, exponents [blocks of rows][blocks of 128]) of x
-    [M][K], blocks of ``rows`` x 128."""
+    [M][K], blocks of ``rows`` x 128.  Exponents as :func:`scale_exponent`, with 448
+    as 0.875 * 2^9; values of a block with an infinity or a NaN are NaN."""
     M, K = x.shape
-    q = np.zeros((M, K))
-    exps = np.zeros((-(-M // rows), -(-K // BLOCK)), dtype=np.int64)
-    for i in range(exps.shape[0]):
-        for j in range(exps.shape[1]):
-            b = x[i * rows:(i + 1) * rows, j * BLOCK:(j + 1) * BLOCK]
-            e = scale_exponent(float(np.abs(b).max()) if np.isfinite(b).all() else math.inf)
-            exps[i, j] = e
-            q[i * rows:(i + 1) * rows, j * BLOCK:(j + 1) * BLOCK] = \
-                e4m3(np.ldexp(b, -e)) if e < 128 else np.nan
-    return q, exps
+    R, B = -(-M // rows), -(-K // BLOCK)
+    pad = np.zeros((R * rows, B * BLOCK))
+    pad[:M, :K] = np.where(np.isfinite(x), x, np.nan)
+    blocks = pad.reshape(R, rows, B, BLOCK)
+    amax = np.abs(blocks).max(axis=(1, 3))
+    bad = np.isnan(amax)
+    m, e = np.frexp(np.where(bad, 0.0, amax))
+    exps = np.where(bad, 128, np.maximum(e - 9 + (m > 0.875), -126)).astype(np.int64)
+    exps[amax == 0] = -126
+    q = e4m3(np.where(bad[:, None, :, None], 0.0, np.ldexp(np.nan_to_num(blocks), -np.where(bad, 0, exps)[:, None, :, None])))
+    q = np.where(bad[:, None, :, None], np.nan, q)
+    return q.reshape(R * rows, B * BLOCK)[:M, :K], exps
 
 
-def held(x, rows: int):
-    """The values that x's 8-bit form stands for."""
+def held(x, rows: int, least: float = 0.0):
+    """The values that x's 8-bit form stands for; with ``least``, the magnitudes of
+    those that are not zero, taken to be at least ``least`` of their scale."""
     q, e = quantize(x, rows)
+    if least:
+        q = np.where(q != 0, np.maximum(np.abs(q), least), 0.0)
     s = np.repeat(np.repeat(np.where(e < 128, np.ldexp(1.0, np.minimum(e, 127)), np.nan), rows, 0),
                   BLOCK, 1)
     return q * s[:x.shape[0], :x.shape[1]]

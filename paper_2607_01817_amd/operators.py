@@ -10,10 +10,11 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 
 import torch
 
-from . import _check, _dev, _devs, _dtype, _expect, _ints, _stream, _table_rows, load
+from . import _check, _dev, _devs, _dtype, _expect, _ints, load
 
 E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 SCALE_BLOCK = 128
@@ -27,9 +28,22 @@ class RopeHeads(ctypes.Structure):
                 ("heads", ctypes.c_int)]
 
 
+_NO_CONTEXT = contextlib.nullcontext()
+
+
 def _on(stream):
     """Outputs and workspaces belong to the stream that the call runs on."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _NO_CONTEXT if stream is None else torch.cuda.stream(stream)
+
+
+def _stream(stream, x: torch.Tensor) -> int:
+    """The handle of the stream to launch on, x's device being the current one."""
+    if stream is not None:
+        return stream.cuda_stream
+    device = torch._C._cuda_getDevice()
+    if x.device.index != device:
+        raise ValueError(f"the tensors are on {x.device}, the current device is {device}")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _rows(t: torch.Tensor, name: str) -> int:
@@ -41,7 +55,9 @@ def _rows(t: torch.Tensor, name: str) -> int:
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     M, D = t.shape
-    if M > 0 and D > 1 and t.stride(1) != 1:
+    if t.is_contiguous():
+        return D
+    if D > 1 and t.stride(1) != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
     if M > 1 and t.stride(0) < D:
         raise ValueError(f"the rows of {name} overlap")
@@ -75,13 +91,13 @@ def _norm_args(x, weight, residual):
     return M, D, ldx, ldr
 
 
-def _out(t, shape, dtype, device, name):
+def _out(t, shape, dtype, x, name):
+    """The output t, or a new one beside x."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return x.new_empty(shape, dtype=dtype)
     _expect(t, shape, dtype, name)
     _dev(t, name)
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    _one_device(x, ((t, name),))
     return t
 
 
@@ -96,10 +112,10 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6,
     if residual is None and h_out is not None:
         raise ValueError("h_out is given without a residual")
     with _on(stream):
-        y = _out(out, (M, D), x.dtype, x.device, "out")
-        h = None if residual is None else _out(h_out, (M, D), x.dtype, x.device, "h_out")
+        y = _out(out, (M, D), x.dtype, x, "out")
+        h = None if residual is None else _out(h_out, (M, D), x.dtype, x, "h_out")
     _check(load().hcms_rms_norm(x.data_ptr(), _ptr(residual), weight.data_ptr(), y.data_ptr(), _ptr(h),
-                                M, D, ldx, ldr, eps, _dtype(x), _dtype(weight), _stream(stream)))
+                                M, D, ldx, ldr, eps, _dtype(x), _dtype(weight), _stream(stream, x)))
     return y if h is None else (y, h)
 
 
@@ -112,12 +128,12 @@ def rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6,
     if residual is None and h_out is not None:
         raise ValueError("h_out is given without a residual")
     with _on(stream):
-        q = torch.empty((M, D), dtype=E4M3, device=x.device)
-        scale = _scales(M, D, x.device)
-        h = None if residual is None else _out(h_out, (M, D), x.dtype, x.device, "h_out")
+        q = x.new_empty((M, D), dtype=E4M3)
+        scale = _scales(M, D, x)
+        h = None if residual is None else _out(h_out, (M, D), x.dtype, x, "h_out")
     _check(load().hcms_rms_norm_fp8(x.data_ptr(), _ptr(residual), weight.data_ptr(), q.data_ptr(),
                                     scale.data_ptr(), _ptr(h), M, D, ldx, ldr, eps, _dtype(x),
-                                    _dtype(weight), _stream(stream)))
+                                    _dtype(weight), _stream(stream, x)))
     return (q, scale) if h is None else (q, scale, h)
 
 
@@ -131,15 +147,20 @@ def rms_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, e
             _expect(t, (M, D), x.dtype, n)
             _dev(t, n)
     _one_device(x, ((dy, "dy"), (dh, "dh")))
+    return _norm_backward(dy, x, weight, eps, residual, dh, ldx, ldr, stream)
+
+
+def _norm_backward(dy, x, weight, eps, residual, dh, ldx, ldr, stream=None):
+    """The launch of :func:`rms_norm_backward` on tensors that have been checked."""
+    M, D = x.shape
     lib = load()
     with _on(stream):
-        dx = torch.empty((M, D), dtype=x.dtype, device=x.device)
+        dx = x.new_empty((M, D))
         dw = torch.empty_like(weight)
-        partial = torch.empty((_check(lib.hcms_rms_norm_partials(M, D)), D), dtype=torch.float32,
-                              device=x.device)
+        partial = x.new_empty((_check(lib.hcms_rms_norm_partials(M, D)), D), dtype=torch.float32)
     _check(lib.hcms_rms_norm_backward(dy.data_ptr(), x.data_ptr(), _ptr(residual), _ptr(dh),
                                       weight.data_ptr(), dx.data_ptr(), dw.data_ptr(), partial.data_ptr(),
-                                      M, D, ldx, ldr, eps, _dtype(x), _dtype(weight), _stream(stream)))
+                                      M, D, ldx, ldr, eps, _dtype(x), _dtype(weight), _stream(stream, x)))
     return dx, dw
 
 
@@ -160,14 +181,17 @@ class RmsNorm(torch.autograd.Function):
         x, weight, residual = fctx.saved_tensors
         if dy is None:   # only h was used
             return dh, None, None, dh
-        dx, dw = rms_norm_backward(dy.contiguous(), x, weight, fctx.hcms, residual,
-                                   None if dh is None else dh.contiguous())
+        # autograd gives gradients of the outputs' shape and type
+        M, D = x.shape
+        dx, dw = _norm_backward(dy.contiguous(), x, weight, fctx.hcms, residual,
+                                None if dh is None else dh.contiguous(), x.stride(0) if M > 1 else D,
+                                D if residual is None or M <= 1 else residual.stride(0))
         return dx, dw, None, None if residual is None else dx
 
 
-def _scales(rows: int, K: int, device) -> torch.Tensor:
+def _scales(rows: int, K: int, x: torch.Tensor) -> torch.Tensor:
     """Room for the scales of ``rows`` rows (or blocks of rows) of K elements."""
-    return torch.empty((-(-K // (4 * SCALE_BLOCK)), rows, 4), dtype=E8M0, device=device)
+    return x.new_empty((-(-K // (4 * SCALE_BLOCK)), rows, 4), dtype=E8M0)
 
 
 def quantize_fp8(x: torch.Tensor, block: int | None = 1, t_block: int | None = None, stream=None):
@@ -180,19 +204,24 @@ def quantize_fp8(x: torch.Tensor, block: int | None = 1, t_block: int | None = N
     if (block is None and t_block is None) or block not in (None, 1, SCALE_BLOCK) \
             or t_block not in (None, 1, SCALE_BLOCK):
         raise ValueError("block and t_block are 1, 128 or None, not both None")
+    return _quantize(x, block, t_block, ldx, stream)
+
+
+def _quantize(x, block, t_block, ldx, stream=None):
+    """The launch of :func:`quantize_fp8` on a tensor that has been checked."""
     M, K = x.shape
     q = scale = t = t_scale = None
     with _on(stream):
         if block is not None:
-            q = torch.empty((M, K), dtype=E4M3, device=x.device)
-            scale = _scales(M if block == 1 else -(-M // SCALE_BLOCK), K, x.device)
+            q = x.new_empty((M, K), dtype=E4M3)
+            scale = _scales(M if block == 1 else -(-M // SCALE_BLOCK), K, x)
         if t_block is not None:
-            t = torch.empty((K, -(-M // 16) * 16), dtype=E4M3, device=x.device)
-            t_scale = _scales(K if t_block == 1 else -(-K // SCALE_BLOCK), M, x.device)
+            t = x.new_empty((K, -(-M // 16) * 16), dtype=E4M3)
+            t_scale = _scales(K if t_block == 1 else -(-K // SCALE_BLOCK), M, x)
     if M > 0:
         _check(load().hcms_quantize_fp8(x.data_ptr(), _ptr(q), _ptr(scale), block or 1, _ptr(t),
                                         _ptr(t_scale), t_block or 1, M, K, ldx, _dtype(x),
-                                        _stream(stream)))
+                                        _stream(stream, x)))
     if t is None:
         return q, scale
     return (t, t_scale) if q is None else (q, scale, t, t_scale)
@@ -224,10 +253,15 @@ def linear_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale:
     _one_device(x, ((x_scale, "x_scale"), (w, "w"), (w_scale, "w_scale")))
     shape = (M, N) if parts == 1 else (parts, M, N // parts)
     with _on(stream):
-        y = _out(out, shape, dtype, x.device, "out")
+        y = _out(out, shape, dtype, x, "out")
+    return _linear(x, x_scale, w, w_scale, y, parts, stream)
+
+
+def _linear(x, x_scale, w, w_scale, y, parts=1, stream=None):
+    """The launch of :func:`linear_fp8` on tensors that have been checked."""
+    M, K = x.shape
     _check(load().hcms_linear_fp8(x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(),
-                                  y.data_ptr(), M, N, K, parts, 0 if dtype == torch.bfloat16 else 1,
-                                  _stream(stream)))
+                                  y.data_ptr(), M, w.shape[0], K, parts, _dtype(y), _stream(stream, x)))
     return y
 
 
@@ -235,21 +269,22 @@ class Fp8Linear(torch.autograd.Function):
     """A projection whose three products run in 8 bits: ``Fp8Linear.apply(x, w)``
     is x [M][K] times w [N][K] in x's dtype, with activations and gradients
     quantised per row and 128 of the contraction, and weights (and the activations
-    of the weight's gradient) per 128 x 128.  K, and N where x needs a gradient,
-    must be multiples of 16.  What the backward needs is kept in 8 bits."""
+    of the weight's gradient) per 128 x 128.  K and N must be multiples of 16 (N of
+    8 without gradients).  What the backward needs is kept in 8 bits."""
 
     @staticmethod
     def forward(fctx, x, w):
         if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x.dtype != w.dtype:
             raise ValueError("x must be [M][K] and w [N][K] of one dtype")
         dx, dw = fctx.needs_input_grad
-        if dx and w.shape[0] % 16:
-            raise ValueError(f"N = {w.shape[0]} must be a multiple of 16 for the gradient of x")
+        if w.shape[0] % (16 if dx or dw else 8):
+            raise ValueError(f"N = {w.shape[0]} must be a multiple of 16, or of 8 without gradients")
+        _one_device(x, ((w, "w"),))
         xq, xs, *xt = quantize_fp8(x, 1, SCALE_BLOCK if dw else None)
         wq, ws, *wt = quantize_fp8(w, SCALE_BLOCK, SCALE_BLOCK if dx else None)
         fctx.save_for_backward(*(xt or (None, None)), *(wt or (None, None)))
         fctx.hcms = (x.shape[0], w.dtype)
-        return linear_fp8(xq, xs, wq, ws, dtype=x.dtype)
+        return _linear(xq, xs, wq, ws, x.new_empty((x.shape[0], w.shape[0])))
 
     @staticmethod
     def backward(fctx, dy):
@@ -260,9 +295,12 @@ class Fp8Linear(torch.autograd.Function):
         if M == 0:
             return (torch.empty((0, wt.shape[0]), dtype=dy.dtype, device=dy.device) if need_x else None,
                     torch.zeros((dy.shape[1], xt.shape[0]), dtype=dtype, device=dy.device) if need_w else None)
-        got = list(quantize_fp8(dy, 1 if need_x else None, 1 if need_w else None))
-        dx = linear_fp8(got[0], got[1], wt, wts, dtype=dy.dtype) if need_x else None
-        dw = linear_fp8(got[-2], got[-1], xt, xts, dtype=dtype) if need_w else None
+        got = _quantize(dy, 1 if need_x else None, 1 if need_w else None, dy.shape[1])
+        dx = dw = None
+        if need_x:
+            dx = _linear(got[0], got[1], wt, wts, dy.new_empty((M, wt.shape[0])))
+        if need_w:
+            dw = _linear(got[-2], got[-1], xt, xts, dy.new_empty((dy.shape[1], xt.shape[0]), dtype=dtype))
         return dx, dw
 
 
@@ -281,32 +319,40 @@ def rope_frequencies(pairs: int, base: float = 10000.0, scaling: str = "none", f
     return list(buf), mag.value
 
 
+@functools.lru_cache(maxsize=256)
+def _axes(grid: tuple, axis_pairs: tuple):
+    """The C arrays of a grid and its pair counts, and the table's entries."""
+    g, na = _ints(grid)
+    p, npairs = _ints(axis_pairs)
+    if na != npairs:
+        raise ValueError("one pair count per grid axis")
+    return g, p, na, _check(load().hcms_rope_table_entries(g, p, na))
+
+
 def rope_table_freqs(grid, axis_pairs, freqs, magnitude: float = 1.0, device="cuda",
                      stream=None) -> torch.Tensor:
     """The rotation table (see :func:`rope_table`) of given frequencies, one per
     pair, with every entry times ``magnitude``: float32 [entries][2]."""
-    n = _table_rows(grid, axis_pairs)
-    g, na = _ints(grid)
-    p, _ = _ints(axis_pairs)
+    g, p, na, n = _axes(tuple(grid), tuple(axis_pairs))
     freqs = [float(f) for f in freqs]
-    if len(freqs) != sum(int(x) for x in axis_pairs):
+    if len(freqs) != sum(p):
         raise ValueError("one frequency per pair")
     with _on(stream):
         table = torch.empty((n, 2), dtype=torch.float32, device=device)
     _check(load().hcms_rope_table_freqs(table.data_ptr(), g, p, na, (ctypes.c_double * len(freqs))(*freqs),
-                                        float(magnitude), _stream(stream)))
+                                        float(magnitude), _stream(stream, table)))
     return table
 
 
-def _heads(x, S, d, dtype, name):
-    """Checks a side's heads [S][heads][d] and gives its token and head strides."""
-    if not isinstance(x, torch.Tensor) or x.dim() != 3 or x.shape[0] != S or x.shape[2] != d or x.dtype != dtype:
-        raise ValueError(f"{name} must be [S][heads][d] of one dtype")
-    if not x.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor")
-    if x.numel() and d > 1 and x.stride(2) != 1:
+def _side(x, y, S, d, dtype, name):
+    """A side's heads as the library takes them: x and y [S][heads][d], any strides of
+    tokens and heads."""
+    if x.shape != y.shape or x.shape[0] != S or x.shape[2] != d or not x.dtype == y.dtype == dtype:
+        raise ValueError(f"{name} and its output must be [S][heads][d] of one dtype")
+    xs, ys = x.stride(), y.stride()
+    if x.numel() and d > 1 and not xs[2] == ys[2] == 1:
         raise ValueError(f"the head vectors of {name} must be contiguous")
-    return x.stride(0), x.stride(1)
+    return RopeHeads(x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], x.shape[1])
 
 
 def rope(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, grid, axis_pairs,
@@ -322,13 +368,13 @@ def rope(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, grid, axi
     to write to, which may be the inputs themselves.  Returns (q, k), or q."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be [S][heads][d]")
+    if k is not None and (not isinstance(k, torch.Tensor) or k.dim() != 3):
+        raise ValueError("k must be [S][heads][d]")
     if layout not in _LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}")
     S, _, d = q.shape
-    _expect(table, (_table_rows(grid, axis_pairs), 2), torch.float32, "table")
-    _dev(table, "table")
-    g, na = _ints(grid)
-    p, _ = _ints(axis_pairs)
+    g, p, na, entries = _axes(tuple(grid), tuple(axis_pairs))
+    _expect(table, (entries, 2), torch.float32, "table")
     pb = 0
     if positions is not None:
         if not isinstance(positions, torch.Tensor) or positions.dtype not in (torch.int32, torch.int64):
@@ -337,31 +383,23 @@ def rope(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, grid, axi
             raise ValueError("positions must be [S] or [S][axes]")
         _dev(positions, "positions")
         pb = positions.element_size()
-    if out is not None and len(out) != 2:
-        raise ValueError("out must be the pair (q, k)")
-    ins, outs, sides = (q, k), [], []
-    _one_device(q, ((k, "k"), (table, "table"), (positions, "positions")))
-    for i, (x, name) in enumerate(zip(ins, ("q", "k"))):
-        if x is None:
-            outs.append(None)
-            sides.append(None)
-            continue
-        xt, xh = _heads(x, S, d, q.dtype, name)
-        if out is None:
-            with _on(stream):
-                y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        else:
-            y = out[i]
-            if not isinstance(y, torch.Tensor) or y.shape != x.shape:
-                raise ValueError(f"out's {name} must match {name}")
-            _one_device(x, ((y, f"out's {name}"),))
-        yt, yh = _heads(y, S, d, q.dtype, f"out's {name}")
-        outs.append(y)
-        sides.append(RopeHeads(x.data_ptr(), y.data_ptr(), xt, xh, yt, yh, x.shape[1]))
-    _check(load().hcms_rope(ctypes.byref(sides[0]), None if k is None else ctypes.byref(sides[1]),
-                            table.data_ptr(), g, p, na, _ptr(positions), pb, S, d, _LAYOUTS[layout],
-                            int(bool(inverse)), _dtype(q), _stream(stream)))
-    return outs[0] if k is None else tuple(outs)
+    _dev(table, "table")
+    if out is None:
+        with _on(stream):
+            yq, yk = q.new_empty(q.shape), None if k is None else k.new_empty(k.shape)
+    else:
+        yq, yk = out
+        if not isinstance(yq, torch.Tensor) or not (k is None or isinstance(yk, torch.Tensor)):
+            raise TypeError("out must be the tensors (q, k)")
+    if not q.is_cuda:
+        raise ValueError("q must be a GPU tensor")
+    _one_device(q, ((yq, "out's q"), (k, "k"), (None if k is None else yk, "out's k"), (table, "table"),
+                    (positions, "positions")))
+    qs = _side(q, yq, S, d, q.dtype, "q")
+    ks = None if k is None else ctypes.byref(_side(k, yk, S, d, q.dtype, "k"))
+    _check(load().hcms_rope(ctypes.byref(qs), ks, table.data_ptr(), g, p, na, _ptr(positions), pb, S, d,
+                            _LAYOUTS[layout], 1 if inverse else 0, _dtype(q), _stream(stream, q)))
+    return yq if k is None else (yq, yk)
 
 
 class Rope(torch.autograd.Function):

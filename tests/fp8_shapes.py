@@ -1,0 +1,29 @@
+"""Shapes of the 8-bit product that take each of its tiles on 256 compute units
+(csrc/linear_fp8_tiles.h), in at most one round of workgroups and in more, with
+ragged rows, columns and last blocks of k.  A host test checks the tiles; the GPU
+tests run the shapes."""
+
+TILES = {"bf16": [(256, 256), (192, 256), (128, 256), (128, 128), (64, 128), (64, 64)],
+         "fp32": [(256, 128), (128, 128), (64, 64)]}
+
+# (output type, tile, more than one round, M, N, K)
+SHAPES = [
+    ("bf16", 0, False, 12391, 776, 272),
+    ("bf16", 0, True, 12321, 1800, 80),
+    ("bf16", 1, False, 513, 13120, 272),
+    ("bf16", 1, True, 13107, 1160, 80),
+    ("bf16", 2, False, 321, 10920, 656),
+    ("bf16", 2, True, 10809, 1288, 272),
+    ("bf16", 3, False, 145, 10888, 656),
+    ("bf16", 3, True, 10903, 520, 272),
+    ("bf16", 4, False, 35, 72, 656),
+    ("bf16", 4, True, 265, 10952, 272),
+    ("bf16", 5, False, 35, 16, 272),
+    ("bf16", 5, True, 521, 7184, 80),
+    ("fp32", 0, False, 321, 10888, 272),
+    ("fp32", 0, True, 13111, 904, 80),
+    ("fp32", 1, False, 145, 10888, 656),
+    ("fp32", 1, True, 529, 10904, 272),
+    ("fp32", 2, False, 35, 16, 656),
+    ("fp32", 2, True, 10889, 264, 272),
+]

@@ -48,6 +48,23 @@ def test_scale_exponent(amax, e):
     assert op.scale_exponent(amax) == e
 
 
+@pytest.mark.parametrize("rows", [1, 128])
+def test_quantize_takes_each_block_by_itself(rows):
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((150, 300)) * np.exp2(rng.integers(-140, 120, (150, 1)))
+    x[7], x[140, 299], x[3, 4] = 0, np.inf, 1e-320
+    q, e = op.quantize(x, rows)
+    for i in range(e.shape[0]):
+        for j in range(e.shape[1]):
+            s = slice(i * rows, (i + 1) * rows), slice(j * 128, (j + 1) * 128)
+            want = op.scale_exponent(np.abs(x[s]).max())
+            assert e[i, j] == want
+            if want < 128:
+                assert np.array_equal(q[s], op.e4m3(x[s] / 2.0 ** want))
+            else:
+                assert np.isnan(q[s]).all()
+
+
 def test_norm_gradient_is_that_of_differences():
     rng = np.random.default_rng(1)
     x, r, dy, dh = rng.standard_normal((4, 3, 10))
