@@ -87,6 +87,14 @@ __device__ inline bf16x8_any load_raw(const __bf16 *p) { return *reinterpret_cas
 __device__ inline raw_f32x8 load_raw(const float *p) {
     return {*reinterpret_cast<const f32x4_any *>(p), *reinterpret_cast<const f32x4_any *>(p + 4)};
 }
+// The same for data that is not read again (a hint to the caches).
+__device__ inline bf16x8_any load_raw_once(const __bf16 *p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const bf16x8_any *>(p));
+}
+__device__ inline raw_f32x8 load_raw_once(const float *p) {
+    return {__builtin_nontemporal_load(reinterpret_cast<const f32x4_any *>(p)),
+            __builtin_nontemporal_load(reinterpret_cast<const f32x4_any *>(p + 4))};
+}
 __device__ inline fp8::f32x8 widen(bf16x8_any v) { return __builtin_convertvector(v, fp8::f32x8); }
 __device__ inline fp8::f32x8 widen(raw_f32x8 v) {
     return fp8::f32x8{v.a[0], v.a[1], v.a[2], v.a[3], v.b[0], v.b[1], v.b[2], v.b[3]};

@@ -73,28 +73,32 @@ __device__ inline void put_scale(unsigned char *scale, int64_t rows, int64_t row
 // Any of q and t, a 128 x 128 tile per workgroup.  Thread (r, c) holds the 8 x
 // 8 elements of rows 8 r .., columns 8 c .., so that 8 rows of a column pack
 // into 8 bytes of t; t's tile passes through LDS to leave as 16-byte pieces of
-// whole rows.
+// whole rows.  Unit u (8 bytes) of t's row k sits at place u ^ (k / 8), so that
+// the lanes of a write, whose rows are 8 apart, spread over the banks.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_tile_kernel(const T *__restrict__ x, int64_t ldx, QuantizeOut o,
                                                             int64_t M, int K, int tiles_k) {
     __shared__ unsigned col_max[16][kTile];
     __shared__ unsigned wave_max[4];
-    __shared__ __attribute__((aligned(16))) unsigned char tile[kTile][kTile + 16];
+    __shared__ __attribute__((aligned(16))) unsigned char tile[kTile][kTile];
     const int tid = threadIdx.x, c = tid & 15, r = tid >> 4;
     const int kb = blockIdx.x % tiles_k, mb = blockIdx.x / tiles_k;
     const int tiles_m = static_cast<int>((M + kTile - 1) / kTile);
     const int64_t m0 = static_cast<int64_t>(mb) * kTile + r * 8;
     const int e = kb * kTile + c * 8;
-    f32x8 v[8];
+    // Kept as stored and widened where they are used: 32 registers, not 64.
+    using Raw = decltype(load_raw(x));
+    Raw v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        v[i] = m0 + i < M && e < K ? widen(load_raw(x + (m0 + i) * ldx + e)) : f32x8{};
+    for (int i = 0; i < 8; ++i) v[i] = m0 + i < M && e < K ? load_raw(x + (m0 + i) * ldx + e) : Raw{};
     unsigned row_max[8], all = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        row_max[i] = fp8::max16(magnitude8(v[i]));
+        row_max[i] = magnitude8(widen(v[i]));
         all = max(all, row_max[i]);
+        if (o.q && !o.q_square) row_max[i] = fp8::max16(row_max[i]);
     }
+    all = fp8::max16(all);
     // Whole-tile maximum, and the maximum of each column.
     unsigned w = max(max(static_cast<unsigned>(__builtin_amdgcn_readlane(all, 0)),
                          static_cast<unsigned>(__builtin_amdgcn_readlane(all, 16))),
@@ -106,7 +110,7 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(const T *__restrict_
         for (int j = 0; j < 8; ++j) {
             unsigned a = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a = max(a, fp8::magnitude(v[i][j]));
+            for (int i = 0; i < 8; ++i) a = max(a, fp8::magnitude(widen(v[i])[j]));
             col_max[r][c * 8 + j] = a;
         }
     }
@@ -117,7 +121,7 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(const T *__restrict_
         for (int i = 0; i < 8; ++i) {
             const unsigned b = o.q_square ? square : fp8::scale_byte(row_max[i]);
             if (m0 + i >= M) continue;
-            if (e < K) *reinterpret_cast<uint2 *>(o.q + (m0 + i) * K + e) = pack8(v[i], fp8::inverse_scale(b));
+            if (e < K) *reinterpret_cast<uint2 *>(o.q + (m0 + i) * K + e) = pack8(widen(v[i]), fp8::inverse_scale(b));
             if (!o.q_square && c == 0) put_scale(o.q_scale, M, m0 + i, kb, tiles_k, b);
         }
         if (o.q_square && tid == 0) put_scale(o.q_scale, tiles_m, mb, kb, tiles_k, square);
@@ -139,18 +143,20 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(const T *__restrict_
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float by = fp8::inverse_scale(o.t_square ? square : col_max[0][c * 8 + j]);
-        const f32x8 col = {v[0][j], v[1][j], v[2][j], v[3][j], v[4][j], v[5][j], v[6][j], v[7][j]};
-        *reinterpret_cast<uint2 *>(&tile[c * 8 + j][r * 8]) = pack8(col, by);
+        const f32x8 col = {widen(v[0])[j], widen(v[1])[j], widen(v[2])[j], widen(v[3])[j],
+                           widen(v[4])[j], widen(v[5])[j], widen(v[6])[j], widen(v[7])[j]};
+        *reinterpret_cast<uint2 *>(&tile[c * 8 + j][(r ^ c) * 8]) = pack8(col, by);
     }
     __syncthreads();
     const int64_t ldt = (M + 15) / 16 * 16;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int k = i * 32 + (tid >> 3), m = (tid & 7) * 16;
-        const int64_t mm = static_cast<int64_t>(mb) * kTile + m;
+        const int k = i * 32 + (tid >> 3), p = tid & 7, f = k >> 3;
+        const int64_t mm = static_cast<int64_t>(mb) * kTile + p * 16;
+        const uint4 u = *reinterpret_cast<const uint4 *>(&tile[k][(p ^ (f >> 1)) * 16]);
         if (kb * kTile + k < K && mm < ldt)
             *reinterpret_cast<uint4 *>(o.t + static_cast<int64_t>(kb * kTile + k) * ldt + mm) =
-                *reinterpret_cast<const uint4 *>(&tile[k][m]);
+                f & 1 ? uint4{u.z, u.w, u.x, u.y} : u;
     }
 }
 

@@ -3,9 +3,8 @@
 // h is the residual stream's next value; it is stored rounded to the storage
 // type, while y is computed from the unrounded sum.  The statistics are fp32.
 //
-// What bounds it: bytes.  A row is read once into registers, summed and
-// written once, by a wave (64 lanes) where that leaves enough rows to fill
-// the CUs, else by 256 or 1024 lanes.
+// What bounds it: bytes.  A row is read once into registers by L lanes (a
+// multiple of 64), NC chunks of 8 elements each, summed and written once.
 #include "fp8.h"
 #include "hcms_internal.h"
 
@@ -14,10 +13,10 @@ namespace {
 
 using fp8::f32x8;
 
-// Lane t of a row's TPR lanes holds the chunks of 8 elements t, t + TPR, ...
-// The chunk that the row's end cuts is read from D - 8 on: its first `dup`
-// elements are another lane's too, which stores the same values; sums take
-// them from that lane alone.
+// Lane t of a row's L lanes holds the chunks of 8 elements t, t + L, ...  The
+// chunk that the row's end cuts is read from D - 8 on: its first `dup` elements
+// are another lane's too, which stores the same values; sums take them from
+// that lane alone.
 struct Chunk {
     int e0, dup;
 };
@@ -26,19 +25,36 @@ __device__ inline Chunk chunk_at(int c, int D) {
     return {e0, e - e0};
 }
 
-// Sum of v over the TPR lanes of a row; `red` holds a float per wave.
-template <int TPR>
-__device__ inline float row_sum(float v, float *red) {
-    v = wave_sum(v);
-    if constexpr (TPR > 64) {
-        __syncthreads();   // the floats of the sum before have been read
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0;
+// The lane's place in a workgroup that takes one row, or with ROWS one for each
+// of its four waves.
+template <bool ROWS>
+struct Lane {
+    static __device__ int t() { return ROWS ? threadIdx.x & 63 : threadIdx.x; }
+    static __device__ int lanes() { return ROWS ? 64 : blockDim.x; }
+    static __device__ int row() { return ROWS ? threadIdx.x >> 6 : 0; }
+    static __device__ int rows() { return ROWS ? 4 : 1; }
+};
+
+// Sums of N values over the lanes of a row, in a fixed order; `red` holds N
+// floats per wave.
+template <bool ROWS, int N>
+__device__ inline void row_sums(float (&v)[N], float (*red)[N]) {
 #pragma unroll
-        for (int i = 0; i < TPR / 64; ++i) v += red[i];
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (!ROWS) {
+        const int waves = blockDim.x >> 6;
+        if (waves == 1) return;
+        __syncthreads();   // the sums before have been read
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[threadIdx.x >> 6][i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = red[0][i];
+        for (int k = 1; k < waves; ++k)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += red[k][i];
     }
-    return v;
 }
 
 __device__ inline f32x8 weights(const void *w, bool w_f32, int e0) {
@@ -47,42 +63,41 @@ __device__ inline f32x8 weights(const void *w, bool w_f32, int e0) {
 }
 
 // F8: y as e4m3 values q [M][D] and scales [D / 512][M][4] (fp8.h).
-template <typename T, bool F8, int TPR, int NC>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(
+template <typename T, bool F8, int NC>
+__global__ __launch_bounds__(1024) void rms_norm_kernel(
     const T *__restrict__ x, const T *__restrict__ r, const void *__restrict__ w, bool w_f32,
     T *__restrict__ y, unsigned char *__restrict__ q, unsigned *__restrict__ scale, T *__restrict__ h_out,
     int64_t M, int D, int64_t ldx, int64_t ldr, float eps) {
-    __shared__ float red[TPR / 64];
-    const int t = threadIdx.x % TPR;
-    const int64_t m = TPR >= 256 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * (256 / TPR) + threadIdx.x / TPR;
-    if (TPR < 256 && m >= M) return;   // whole waves, and no barrier follows for them
+    __shared__ float red[16][1];
+    const int t = threadIdx.x, L = blockDim.x;
+    const int64_t m = blockIdx.x;
     const T *xr = x + m * ldx;
     f32x8 h[NC];
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-        const int c = j * TPR + t;
+        const int c = j * L + t;
         h[j] = c * 8 < D ? widen(load_raw(xr + chunk_at(c, D).e0)) : f32x8{};
     }
     if (r) {
         const T *rr = r + m * ldr;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const int c = j * TPR + t;
+            const int c = j * L + t;
             if (c * 8 < D) h[j] += widen(load_raw(rr + chunk_at(c, D).e0));
         }
     }
-    float sum = 0;
+    float sum[1] = {0};
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-        const int dup = chunk_at(j * TPR + t, D).dup;
+        const int dup = chunk_at(j * L + t, D).dup;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += i >= dup ? h[j][i] * h[j][i] : 0.0f;
+        for (int i = 0; i < 8; ++i) sum[0] += i >= dup ? h[j][i] * h[j][i] : 0.0f;
     }
-    sum = row_sum<TPR>(sum, red);
-    const float rstd = 1.0f / __builtin_sqrtf(sum / static_cast<float>(D) + eps);
+    row_sums<false>(sum, red);
+    const float rstd = 1.0f / __builtin_sqrtf(sum[0] / static_cast<float>(D) + eps);
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-        const int c = j * TPR + t;
+        const int c = j * L + t;
         const bool in = c * 8 < D;
         const int e0 = chunk_at(c, D).e0;
         f32x8 v{};
@@ -117,91 +132,138 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(
 // rounded, dw would be 1.4 times as far from the exact sum in bf16; reading x
 // and r costs one tensor more), n = h rstd, g = dy w,
 //   dx = rstd (g - n mean(g n)) + dh,   dw = sum over rows of dy n.
-// A workgroup takes every gridDim.x-th set of rows and keeps its share of dw
-// in registers; the shares go to partial [gridDim.x][D] and are summed by
-// sum_rows_kernel, so no atomics: the order is fixed.
-template <typename T, int TPR, int NC>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_backward_kernel(
+// A workgroup takes every gridDim.x-th set of rows, its next row's loads issued
+// ahead of this row's sums (AHEAD; rows that 512 lanes do not hold, whose values
+// and next row would not fit the registers, are read twice instead), and keeps its share of dw in registers; the shares
+// go to partial [gridDim.x][D] and are summed by sum_rows_kernel, so no
+// atomics: the order is fixed.
+template <typename T, bool ROWS, int NC, int MAX, bool AHEAD>
+__global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
     const T *__restrict__ dy, const T *__restrict__ x, const T *__restrict__ r, const T *__restrict__ dh,
     const void *__restrict__ w, bool w_f32, T *__restrict__ dx, float *__restrict__ partial, int64_t M, int D,
     int64_t ldx, int64_t ldr, float eps) {
-    constexpr int RB = TPR < 256 ? 256 / TPR : 1;   // rows at once
-    __shared__ float red[TPR / 64];
-    __shared__ float share[RB > 1 ? TPR * NC * 8 : 1];
-    const int t = threadIdx.x % TPR;
+    __shared__ float red[16][2];
+    __shared__ float share[ROWS ? 64 * NC * 8 : 1];
+    using P = Lane<ROWS>;
+    const int t = P::t(), L = P::lanes();
     f32x8 acc[NC];
+    int e0[NC], dup[NC];
+    bool in[NC];
 #pragma unroll
-    for (int j = 0; j < NC; ++j) acc[j] = f32x8{};
-    for (int64_t m = static_cast<int64_t>(blockIdx.x) * RB + threadIdx.x / TPR; m < M;
-         m += static_cast<int64_t>(gridDim.x) * RB) {
-        f32x8 n[NC], g[NC];
+    for (int j = 0; j < NC; ++j) {
+        const Chunk k = chunk_at(j * L + t, D);
+        in[j] = (j * L + t) * 8 < D;
+        e0[j] = k.e0;
+        dup[j] = k.dup;
+        acc[j] = f32x8{};
+    }
+    const int64_t step = static_cast<int64_t>(gridDim.x) * P::rows();
+    int64_t m = static_cast<int64_t>(blockIdx.x) * P::rows() + P::row();
+    const auto add = [&](float (&sums)[2], int j, const f32x8 &n, const f32x8 &g, const f32x8 &wv) {
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            const int c = j * TPR + t;
-            n[j] = c * 8 < D ? widen(load_raw(x + m * ldx + chunk_at(c, D).e0)) : f32x8{};
+        for (int i = 0; i < 8; ++i) {
+            sums[0] += i >= dup[j] ? n[i] * n[i] : 0.0f;
+            sums[1] += i >= dup[j] ? g[i] * wv[i] * n[i] : 0.0f;
         }
-        if (r) {
+    };
+    float rstd, mean;
+    const auto finish_sums = [&](float (&sums)[2]) {
+        row_sums<ROWS>(sums, red);
+        rstd = 1.0f / __builtin_sqrtf(sums[0] / static_cast<float>(D) + eps);
+        mean = sums[1] * rstd / static_cast<float>(D);
+    };
+    // dx without dh, and the chunk's part of dw.
+    const auto gradient = [&](int j, const f32x8 &n, const f32x8 &g, const f32x8 &wv) {
+        const f32x8 nn = n * rstd;
+        acc[j] += g * nn;
+        return (g * wv - nn * mean) * rstd;
+    };
+    using Raw = decltype(load_raw(x));
+    if constexpr (AHEAD) {
+        f32x8 wv[NC];
+        Raw xn[NC], rn[NC], gn[NC];
+        const auto fetch = [&](int64_t at) {
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                const int c = j * TPR + t;
-                if (c * 8 < D) n[j] += widen(load_raw(r + m * ldr + chunk_at(c, D).e0));
+                if (!in[j]) continue;
+                xn[j] = load_raw(x + at * ldx + e0[j]);
+                gn[j] = load_raw(dy + at * D + e0[j]);
+                if (r) rn[j] = load_raw(r + at * ldr + e0[j]);
+            }
+        };
+#pragma unroll
+        for (int j = 0; j < NC; ++j) wv[j] = in[j] ? weights(w, w_f32, e0[j]) : f32x8{};
+        if (m < M) fetch(m);
+        for (; m < M; m += step) {
+            f32x8 n[NC], g[NC];
+            Raw dhr[NC];
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                n[j] = in[j] ? widen(xn[j]) : f32x8{};
+                if (r && in[j]) n[j] += widen(rn[j]);
+                g[j] = in[j] ? widen(gn[j]) : f32x8{};
+                if (dh && in[j]) dhr[j] = load_raw(dh + m * D + e0[j]);
+            }
+            if (m + step < M) fetch(m + step);
+            float sums[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < NC; ++j) add(sums, j, n[j], g[j], wv[j]);
+            finish_sums(sums);
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                if (!in[j]) continue;
+                f32x8 o = gradient(j, n[j], g[j], wv[j]);
+                if (dh) o += widen(dhr[j]);
+                store_8(dx + m * D + e0[j], o);
             }
         }
+    } else {
+        for (; m < M; m += step) {
+            f32x8 n, g, wv;
+            const auto fetch = [&](int j) {
+                asm volatile("" : "+v"(e0[j]));   // the second reading is one: nothing is kept
+                n = widen(load_raw(x + m * ldx + e0[j]));
+                if (r) n += widen(load_raw(r + m * ldr + e0[j]));
+                g = widen(load_raw(dy + m * D + e0[j]));
+                wv = weights(w, w_f32, e0[j]);
+            };
+            float sums[2] = {0, 0};
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            const int c = j * TPR + t;
-            g[j] = c * 8 < D ? widen(load_raw(dy + m * D + chunk_at(c, D).e0)) : f32x8{};
-        }
-        float ss = 0, sg = 0;
-        f32x8 wv[NC];
+            for (int j = 0; j < NC; ++j)
+                if (in[j]) {
+                    fetch(j);
+                    add(sums, j, n, g, wv);
+                }
+            finish_sums(sums);
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            const int c = j * TPR + t;
-            const Chunk k = chunk_at(c, D);
-            wv[j] = c * 8 < D ? weights(w, w_f32, k.e0) : f32x8{};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                ss += i >= k.dup ? n[j][i] * n[j][i] : 0.0f;
-                sg += i >= k.dup ? g[j][i] * wv[j][i] * n[j][i] : 0.0f;
-            }
-        }
-        ss = row_sum<TPR>(ss, red);
-        sg = row_sum<TPR>(sg, red);
-        const float rstd = 1.0f / __builtin_sqrtf(ss / static_cast<float>(D) + eps);
-        const float mean = sg * rstd / static_cast<float>(D);
-#pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            const int c = j * TPR + t;
-            if (c * 8 >= D) continue;
-            const int e0 = chunk_at(c, D).e0;
-            const f32x8 nn = n[j] * rstd;
-            acc[j] += g[j] * nn;
-            f32x8 o = (g[j] * wv[j] - nn * mean) * rstd;
-            if (dh) o += widen(load_raw(dh + m * D + e0));
-            store_8(dx + m * D + e0, o);
+            for (int j = 0; j < NC; ++j)
+                if (in[j]) {
+                    fetch(j);
+                    f32x8 o = gradient(j, n, g, wv);
+                    if (dh) o += widen(load_raw(dh + m * D + e0[j]));
+                    store_8(dx + m * D + e0[j], o);
+                }
         }
     }
-    if constexpr (RB > 1) {
+    if constexpr (ROWS) {
         // The waves' shares, added in the order of the waves.
-        for (int k = 0; k < RB; ++k) {
-            if (static_cast<int>(threadIdx.x) / TPR == k)
+        for (int k = 0; k < 4; ++k) {
+            if (P::row() == k)
 #pragma unroll
                 for (int j = 0; j < NC; ++j)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        float &s = share[(j * 8 + i) * TPR + t];
+                        float &s = share[(j * 8 + i) * 64 + t];
                         s = k == 0 ? acc[j][i] : s + acc[j][i];
-                        if (k == RB - 1) acc[j][i] = s;
+                        if (k == 3) acc[j][i] = s;
                     }
             __syncthreads();
         }
-        if (static_cast<int>(threadIdx.x) / TPR != RB - 1) return;
+        if (P::row() != 3) return;
     }
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        const int c = j * TPR + t;
-        if (c * 8 < D) store_8(partial + static_cast<int64_t>(blockIdx.x) * D + chunk_at(c, D).e0, acc[j]);
-    }
+    for (int j = 0; j < NC; ++j)
+        if (in[j]) store_8(partial + static_cast<int64_t>(blockIdx.x) * D + e0[j], acc[j]);
 }
 
 // out[d] = sum over P rows of partial[P][D]: 16 columns per workgroup, 16 lanes
@@ -213,6 +275,7 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(const float *__restrict__
     const int col = threadIdx.x & 15, k = threadIdx.x >> 4, d = blockIdx.x * 16 + col;
     float s = 0;
     if (d < D)
+#pragma unroll 8
         for (int p = k; p < P; p += 16) s += partial[static_cast<int64_t>(p) * D + d];
     part[k][col] = s;
     __syncthreads();
@@ -232,31 +295,28 @@ struct NormArgs {
     float eps;
 };
 
-template <typename T, bool F8, int TPR, int NC>
+// Lanes of a row of D elements in NC chunks each, in whole waves.
+int lanes_for(int D, int NC) { return ((D + 7) / 8 + 64 * NC - 1) / (64 * NC) * 64; }
+
+template <typename T, bool F8, int NC>
 hipError_t run_norm(const NormArgs &a, hipStream_t s) {
-    constexpr int RB = TPR < 256 ? 256 / TPR : 1;
-    const int64_t blocks = (a.M + RB - 1) / RB;
-    if (blocks < 1 || blocks > 0x7fffffff) return hipErrorInvalidValue;
-    rms_norm_kernel<T, F8, TPR, NC><<<static_cast<unsigned>(blocks), TPR < 256 ? 256 : TPR, 0, s>>>(
+    const int threads = lanes_for(a.D, NC);
+    if (a.M < 1 || a.M > 0x7fffffff || threads > 1024) return hipErrorInvalidValue;
+    rms_norm_kernel<T, F8, NC><<<static_cast<unsigned>(a.M), threads, 0, s>>>(
         static_cast<const T *>(a.x), static_cast<const T *>(a.r), a.w, a.w_f32, static_cast<T *>(a.y),
         static_cast<unsigned char *>(a.q), static_cast<unsigned *>(a.scale), static_cast<T *>(a.h), a.M, a.D,
         a.ldx, a.ldr, a.eps);
     return hipGetLastError();
 }
 
-// A wave per row from 1024 rows on, 256 lanes for fewer or longer rows.
+// One chunk per lane, two for many long rows (bf16 with a residual, 56160 rows:
+// D = 5120 428 us with one, 386 (6.0 TB/s) with two, 450 with ten on one wave;
+// D = 2560 197 and 195; D = 1280 99 and 102; one row of 5120 3.3 and 3.5) and
+// for rows that 1024 lanes do not hold.
 template <typename T, bool F8>
 hipError_t norm_typed(const NormArgs &a, hipStream_t s) {
-    const int D = a.D;
-    if (D <= 512) return run_norm<T, F8, 64, 1>(a, s);
-    if (a.M >= 1024) {
-        if (D <= 1536) return run_norm<T, F8, 64, 3>(a, s);
-        if (D <= 2560) return run_norm<T, F8, 64, 5>(a, s);
-        if (D <= 5120) return run_norm<T, F8, 64, 10>(a, s);
-    }
-    if (D <= 2048) return run_norm<T, F8, 256, 1>(a, s);
-    if (D <= 6144) return run_norm<T, F8, 256, 3>(a, s);
-    return run_norm<T, F8, 256, 8>(a, s);
+    if ((a.M >= 1024 && a.D > 2048) || a.D > 8192) return run_norm<T, F8, 2>(a, s);
+    return run_norm<T, F8, 1>(a, s);
 }
 
 struct BackwardArgs {
@@ -271,9 +331,11 @@ struct BackwardArgs {
     int P;
 };
 
-template <typename T, int TPR, int NC>
+template <typename T, bool ROWS, int NC, int MAX, bool AHEAD>
 hipError_t run_backward(const BackwardArgs &a, hipStream_t s) {
-    rms_norm_backward_kernel<T, TPR, NC><<<a.P, TPR < 256 ? 256 : TPR, 0, s>>>(
+    const int threads = ROWS ? 256 : lanes_for(a.D, NC);
+    if (threads > MAX) return hipErrorInvalidValue;
+    rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD><<<a.P, threads, 0, s>>>(
         static_cast<const T *>(a.dy), static_cast<const T *>(a.x), static_cast<const T *>(a.r),
         static_cast<const T *>(a.dh), a.w, a.w_f32, static_cast<T *>(a.dx), a.partial, a.M, a.D, a.ldx, a.ldr,
         a.eps);
@@ -282,21 +344,26 @@ hipError_t run_backward(const BackwardArgs &a, hipStream_t s) {
 
 template <typename T>
 hipError_t backward_typed(const BackwardArgs &a, hipStream_t s) {
-    if (a.D <= 512) return run_backward<T, 64, 1>(a, s);
-    if (a.D <= 2048) return run_backward<T, 256, 1>(a, s);
-    if (a.D <= 6144) return run_backward<T, 256, 3>(a, s);
-    if (a.D <= 8192) return run_backward<T, 1024, 1>(a, s);
-    return run_backward<T, 1024, 2>(a, s);
+    if (a.D <= 512) return run_backward<T, true, 1, 256, true>(a, s);
+    if (a.D <= 1024) return run_backward<T, true, 2, 256, true>(a, s);
+    if (a.D <= 8192) return run_backward<T, false, 2, 512, true>(a, s);
+    return run_backward<T, false, 2, 1024, false>(a, s);
 }
 
 }  // namespace
 
 int rms_norm_max_width() { return 16384; }
 
+// Workgroups of the backward: up to D = 1024 four rows at once, then one; on
+// 256 CUs so many per CU as measured best (56160 rows: D = 128 31 us with four,
+// D = 640 68 with three and 83 with four, D = 1280 133 with six, 147 with four,
+// D = 2560 261 with three, 275 with four, D = 5120 549 with one, 570 with two).
 int rms_norm_partials(int64_t M, int D) {
-    const int64_t rows = D <= 512 ? 4 : 1;
+    const int64_t rows = D <= 1024 ? 4 : 1;
+    const int waves = lanes_for(D, 2) / 64;
+    const int64_t most = 256 * (D <= 512 ? 4 : D <= 1024 ? 3 : waves == 2 ? 6 : waves == 3 ? 3 : waves == 4 ? 2 : 1);
     const int64_t sets = (M + rows - 1) / rows;
-    return static_cast<int>(sets < 1024 ? sets : 1024);
+    return static_cast<int>(sets < most ? sets : most);
 }
 
 hipError_t launch_rms_norm(const void *x, const void *r, const void *w, bool w_f32, void *y, void *q,
