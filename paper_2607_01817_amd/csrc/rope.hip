@@ -24,14 +24,20 @@ struct Unit;   // V elements of T in one access
 template <typename T>
 struct Unit<T, 1> {
     float v[1];
-    __device__ void load(const T *p, bool) { v[0] = static_cast<float>(*p); }
+    template <bool ONCE>
+    __device__ void load(const T *p) {
+        v[0] = static_cast<float>(*p);
+    }
     __device__ void store(T *p) const { *p = static_cast<T>(v[0]); }
 };
 template <typename T>
 struct Unit<T, 8> {
     float v[8];
-    __device__ void load(const T *p, bool once) {
-        const fp8::f32x8 x = widen(once ? load_raw_once(p) : load_raw(p));
+    template <bool ONCE>
+    __device__ void load(const T *p) {
+        fp8::f32x8 x;
+        if constexpr (ONCE) x = widen(load_raw_once(p));
+        else x = widen(load_raw(p));
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = x[i];
     }
@@ -106,8 +112,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeSide qs, RopeSide ks, con
             if (h >= he) break;
             const RopeSide &side = h < qs.H ? qs : ks;
             const T *x = static_cast<const T *>(side.x) + token * side.x_token + (h < qs.H ? h : h - qs.H) * side.x_head;
-            a[k].load(x + e0, ONCE);
-            if (second) b[k].load(x + e1, ONCE);
+            a[k].template load<ONCE>(x + e0);
+            if (second) b[k].template load<ONCE>(x + e1);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
