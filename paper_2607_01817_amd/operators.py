@@ -344,15 +344,27 @@ def rope_table_freqs(grid, axis_pairs, freqs, magnitude: float = 1.0, device="cu
     return table
 
 
-def _side(x, y, S, d, dtype, name):
-    """A side's heads as the library takes them: x and y [S][heads][d], any strides of
-    tokens and heads."""
+def _check_side(x, y, S, d, dtype, name):
+    """x and y must be [S][heads][d], any strides of tokens and heads."""
     if x.shape != y.shape or x.shape[0] != S or x.shape[2] != d or not x.dtype == y.dtype == dtype:
         raise ValueError(f"{name} and its output must be [S][heads][d] of one dtype")
-    xs, ys = x.stride(), y.stride()
-    if x.numel() and d > 1 and not xs[2] == ys[2] == 1:
+    if x.numel() and d > 1 and not x.stride(2) == y.stride(2) == 1:
         raise ValueError(f"the head vectors of {name} must be contiguous")
+
+
+def _side(x, y):
+    """A side's heads as the library takes them."""
+    xs, ys = x.stride(), y.stride()
     return RopeHeads(x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], x.shape[1])
+
+
+def _rope(q, k, yq, yk, table, axes, positions, layout, inverse, stream=None):
+    """The launch of :func:`rope` on tensors that have been checked."""
+    ks = None if k is None else ctypes.byref(_side(k, yk))
+    _check(load().hcms_rope(ctypes.byref(_side(q, yq)), ks, table.data_ptr(), axes[0], axes[1], axes[2],
+                            _ptr(positions), 0 if positions is None else positions.element_size(),
+                            q.shape[0], q.shape[2], _LAYOUTS[layout], 1 if inverse else 0, _dtype(q),
+                            _stream(stream, q)))
 
 
 def rope(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, grid, axis_pairs,
@@ -373,16 +385,15 @@ def rope(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, grid, axi
     if layout not in _LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}")
     S, _, d = q.shape
-    g, p, na, entries = _axes(tuple(grid), tuple(axis_pairs))
-    _expect(table, (entries, 2), torch.float32, "table")
-    pb = 0
+    axes = _axes(tuple(grid), tuple(axis_pairs))
+    na = axes[2]
+    _expect(table, (axes[3], 2), torch.float32, "table")
     if positions is not None:
         if not isinstance(positions, torch.Tensor) or positions.dtype not in (torch.int32, torch.int64):
             raise TypeError("positions must be an int32 or int64 tensor")
         if tuple(positions.shape) != (S, na) and not (na == 1 and tuple(positions.shape) == (S,)):
             raise ValueError("positions must be [S] or [S][axes]")
         _dev(positions, "positions")
-        pb = positions.element_size()
     _dev(table, "table")
     if out is None:
         with _on(stream):
@@ -395,10 +406,10 @@ def rope(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, grid, axi
         raise ValueError("q must be a GPU tensor")
     _one_device(q, ((yq, "out's q"), (k, "k"), (None if k is None else yk, "out's k"), (table, "table"),
                     (positions, "positions")))
-    qs = _side(q, yq, S, d, q.dtype, "q")
-    ks = None if k is None else ctypes.byref(_side(k, yk, S, d, q.dtype, "k"))
-    _check(load().hcms_rope(ctypes.byref(qs), ks, table.data_ptr(), g, p, na, _ptr(positions), pb, S, d,
-                            _LAYOUTS[layout], 1 if inverse else 0, _dtype(q), _stream(stream, q)))
+    _check_side(q, yq, S, d, q.dtype, "q")
+    if k is not None:
+        _check_side(k, yk, S, d, q.dtype, "k")
+    _rope(q, k, yq, yk, table, axes, positions, layout, inverse, stream)
     return yq if k is None else (yq, yk)
 
 
@@ -410,17 +421,18 @@ class Rope(torch.autograd.Function):
     def forward(fctx, q, k, table, grid, axis_pairs, positions=None, layout="interleaved"):
         fctx.set_materialize_grads(False)
         fctx.save_for_backward(table, positions)
-        fctx.hcms = (tuple(grid), tuple(axis_pairs), layout)
+        fctx.hcms = (_axes(tuple(grid), tuple(axis_pairs)), layout)
         return rope(q, k, table, grid, axis_pairs, positions, layout)
 
     @staticmethod
     def backward(fctx, dq, dk):
+        # autograd gives gradients of the outputs' shapes and type
         table, positions = fctx.saved_tensors
-        grid, pairs, layout = fctx.hcms
-        back = {"positions": positions, "layout": layout, "inverse": True}
+        axes, layout = fctx.hcms
         dq, dk = (g if g is None or g.stride(2) == 1 else g.contiguous() for g in (dq, dk))
-        if dq is not None and dk is not None:
-            dq, dk = rope(dq, dk, table, grid, pairs, **back)
-        else:
-            dq, dk = (None if g is None else rope(g, None, table, grid, pairs, **back) for g in (dq, dk))
-        return dq, dk, None, None, None, None, None
+        gq, gk = (None if g is None else g.new_empty(g.shape) for g in (dq, dk))
+        if dq is None and dk is not None:   # one side alone, as the queries' place
+            _rope(dk, None, gk, None, table, axes, positions, layout, True)
+        elif dq is not None:
+            _rope(dq, dk, gq, gk, table, axes, positions, layout, True)
+        return gq, gk, None, None, None, None, None
