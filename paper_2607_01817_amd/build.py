@@ -1,8 +1,9 @@
-"""Build libhcms.so (the HIP library behind include/hcms.h) for gfx950.
+"""Build libhcms.so (the HIP library behind include/hcms.h) for gfx950, and
+_hcms_torch.so (the tensor side of the operators, which calls it).
 
 Usage: ``python -m paper_2607_01817_amd.build`` or ``build()`` from Python.
-Every call recompiles.  Objects go to ``_build/`` beside this file; the
-library is written in-tree as ``libhcms.so``.
+Every call recompiles.  Objects go to ``_build/`` beside this file; both
+libraries are written in-tree.
 """
 from __future__ import annotations
 
@@ -10,6 +11,7 @@ import concurrent.futures
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -17,6 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhcms.so")
+TORCH_LIB = os.path.join(PKG, "_hcms_torch.so")
+TORCH_SOURCE = "torch_ops.cpp"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -97,10 +101,33 @@ def _compile(src: str, verbose: bool) -> tuple:
     return obj, parse_resource_remarks(text)
 
 
+def _compile_torch(verbose: bool) -> tuple:
+    """The object of TORCH_SOURCE (host code: g++) and PyTorch's library folder."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc = os.path.join(root, "include")
+    obj = os.path.join(BUILD, os.path.splitext(TORCH_SOURCE)[0] + ".o")
+    cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-fvisibility=hidden",
+           "-DTORCH_EXTENSION_NAME=_hcms_torch", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+           "-isystem", inc, "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"],
+           "-isystem", os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include"),
+           "-c", os.path.join(CSRC, TORCH_SOURCE), "-o", obj]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on {TORCH_SOURCE}:\n" + r.stderr)
+    return obj, os.path.join(root, "lib")
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        torch_side = ex.submit(_compile_torch, verbose)
         done = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
+        torch_obj, torch_libs = torch_side.result()
     objs = [o for o, _ in done]
     res = {k: v for _, r in done for k, v in r.items()}
     if not res:
@@ -117,6 +144,13 @@ def build(verbose: bool = False) -> str:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
+    tmp = TORCH_LIB + ".tmp"
+    cmd = ["g++", "-shared", "-fPIC", "-o", tmp, torch_obj, "-L", torch_libs, "-ltorch", "-ltorch_cpu",
+           "-ltorch_python", "-lc10", "-lc10_hip", "-L", PKG, "-l:libhcms.so", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    os.replace(tmp, TORCH_LIB)
     return LIB
 
 
