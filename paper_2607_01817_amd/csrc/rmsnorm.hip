@@ -16,7 +16,7 @@ using fp8::f32x8;
 // Lane t of a row's L lanes holds the chunks of 8 elements t, t + L, ...  The
 // chunk that the row's end cuts is read from D - 8 on: its first `dup` elements
 // are another lane's too, which stores the same values; sums take them from
-// that lane alone.
+// that lane alone.  Chunks past the end lie there too, with all 8 doubled.
 struct Chunk {
     int e0, dup;
 };
@@ -62,33 +62,35 @@ __device__ inline f32x8 weights(const void *w, bool w_f32, int e0) {
                  : widen(load_raw(static_cast<const __bf16 *>(w) + e0));
 }
 
-// F8: y as e4m3 values q [M][D] and scales [D / 512][M][4] (fp8.h).
-template <typename T, bool F8, int NC>
+// F8: y as e4m3 values q [M][D] and scales [D / 512][M][4] (fp8.h).  RES: with
+// the residual.  All loads of a row are issued at once: lanes past its end read
+// its last chunk, for a load behind a branch is waited for there.
+template <typename T, typename W, bool F8, int NC, bool RES>
 __global__ __launch_bounds__(1024) void rms_norm_kernel(
-    const T *__restrict__ x, const T *__restrict__ r, const void *__restrict__ w, bool w_f32,
-    T *__restrict__ y, unsigned char *__restrict__ q, unsigned *__restrict__ scale, T *__restrict__ h_out,
-    int64_t M, int D, int64_t ldx, int64_t ldr, float eps) {
+    const T *__restrict__ x, const T *__restrict__ r, const W *__restrict__ w, T *__restrict__ y,
+    unsigned char *__restrict__ q, unsigned *__restrict__ scale, T *__restrict__ h_out, int64_t M, int D,
+    int64_t ldx, int64_t ldr, float eps) {
     __shared__ float red[16][1];
     const int t = threadIdx.x, L = blockDim.x;
     const int64_t m = blockIdx.x;
-    const T *xr = x + m * ldx;
-    f32x8 h[NC];
+    const T *xr = x + m * ldx, *rr = RES ? r + m * ldr : nullptr;
+    using Raw = decltype(load_raw(x));
+    Raw xv[NC], rv[RES ? NC : 1];
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-        const int c = j * L + t;
-        h[j] = c * 8 < D ? widen(load_raw(xr + chunk_at(c, D).e0)) : f32x8{};
+        const int e0 = chunk_at(j * L + t, D).e0;
+        xv[j] = load_raw(xr + e0);
+        if constexpr (RES) rv[j] = load_raw(rr + e0);
     }
-    if (r) {
-        const T *rr = r + m * ldr;
+    decltype(load_raw(w)) wv[NC];
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            const int c = j * L + t;
-            if (c * 8 < D) h[j] += widen(load_raw(rr + chunk_at(c, D).e0));
-        }
-    }
+    for (int j = 0; j < NC; ++j) wv[j] = load_raw(w + chunk_at(j * L + t, D).e0);
+    f32x8 h[NC];
     float sum[1] = {0};
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
+        h[j] = widen(xv[j]);
+        if constexpr (RES) h[j] += widen(rv[j]);
         const int dup = chunk_at(j * L + t, D).dup;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[0] += i >= dup ? h[j][i] * h[j][i] : 0.0f;
@@ -102,8 +104,8 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(
         const int e0 = chunk_at(c, D).e0;
         f32x8 v{};
         if (in) {
-            if (r) store_8(h_out + m * D + e0, h[j]);
-            v = h[j] * rstd * weights(w, w_f32, e0);
+            if constexpr (RES) store_8(h_out + m * D + e0, h[j]);
+            v = h[j] * rstd * widen(wv[j]);
         }
         if constexpr (!F8) {
             if (in) store_8(y + m * D + e0, v);
@@ -133,11 +135,13 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(
 // and r costs one tensor more), n = h rstd, g = dy w,
 //   dx = rstd (g - n mean(g n)) + dh,   dw = sum over rows of dy n.
 // A workgroup takes every gridDim.x-th set of rows, its next row's loads issued
-// ahead of this row's sums (AHEAD; rows that 512 lanes do not hold, whose values
-// and next row would not fit the registers, are read twice instead), and keeps its share of dw in registers; the shares
-// go to partial [gridDim.x][D] and are summed by sum_rows_kernel, so no
-// atomics: the order is fixed.
-template <typename T, bool ROWS, int NC, int MAX, bool AHEAD>
+// ahead of this row's sums (AHEAD; 7800 rows of 5120 with dh 103 us where
+// branches around the loads waited for them, 74 without), and keeps its share of
+// dw in registers.  Rows that 512 lanes do not hold, whose values and next row
+// would not fit the registers, are read twice instead.  The shares go to partial
+// [gridDim.x][D] and are summed by sum_rows_kernel, so no atomics: the order is
+// fixed.  RES, DH: with the residual, with dh.
+template <typename T, bool ROWS, int NC, int MAX, bool AHEAD, bool RES, bool DH>
 __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
     const T *__restrict__ dy, const T *__restrict__ x, const T *__restrict__ r, const T *__restrict__ dh,
     const void *__restrict__ w, bool w_f32, T *__restrict__ dx, float *__restrict__ partial, int64_t M, int D,
@@ -181,39 +185,44 @@ __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
     using Raw = decltype(load_raw(x));
     if constexpr (AHEAD) {
         f32x8 wv[NC];
-        Raw xn[NC], rn[NC], gn[NC];
+        Raw xn[NC], rn[RES ? NC : 1], gn[NC];
+        // No branch around loads and stores, which would wait for all that is in
+        // flight: lanes past the row's end read its last chunk and store the
+        // same values there, and the load past the last row reads that row.
         const auto fetch = [&](int64_t at) {
+            at = at < M ? at : M - 1;
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                if (!in[j]) continue;
                 xn[j] = load_raw(x + at * ldx + e0[j]);
                 gn[j] = load_raw(dy + at * D + e0[j]);
-                if (r) rn[j] = load_raw(r + at * ldr + e0[j]);
+                if constexpr (RES) rn[j] = load_raw(r + at * ldr + e0[j]);
             }
         };
 #pragma unroll
-        for (int j = 0; j < NC; ++j) wv[j] = in[j] ? weights(w, w_f32, e0[j]) : f32x8{};
-        if (m < M) fetch(m);
+        for (int j = 0; j < NC; ++j) wv[j] = weights(w, w_f32, e0[j]);
+        fetch(m);
         for (; m < M; m += step) {
             f32x8 n[NC], g[NC];
-            Raw dhr[NC];
+            Raw dhr[DH ? NC : 1];
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                n[j] = in[j] ? widen(xn[j]) : f32x8{};
-                if (r && in[j]) n[j] += widen(rn[j]);
-                g[j] = in[j] ? widen(gn[j]) : f32x8{};
-                if (dh && in[j]) dhr[j] = load_raw(dh + m * D + e0[j]);
+                if constexpr (DH) dhr[j] = load_raw(dh + m * D + e0[j]);
             }
-            if (m + step < M) fetch(m + step);
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                n[j] = widen(xn[j]);
+                if constexpr (RES) n[j] += widen(rn[j]);
+                g[j] = widen(gn[j]);
+            }
+            fetch(m + step);
             float sums[2] = {0, 0};
 #pragma unroll
             for (int j = 0; j < NC; ++j) add(sums, j, n[j], g[j], wv[j]);
             finish_sums(sums);
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                if (!in[j]) continue;
                 f32x8 o = gradient(j, n[j], g[j], wv[j]);
-                if (dh) o += widen(dhr[j]);
+                if constexpr (DH) o += widen(dhr[j]);
                 store_8(dx + m * D + e0[j], o);
             }
         }
@@ -223,7 +232,7 @@ __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
             const auto fetch = [&](int j) {
                 asm volatile("" : "+v"(e0[j]));   // the second reading is one: nothing is kept
                 n = widen(load_raw(x + m * ldx + e0[j]));
-                if (r) n += widen(load_raw(r + m * ldr + e0[j]));
+                if constexpr (RES) n += widen(load_raw(r + m * ldr + e0[j]));
                 g = widen(load_raw(dy + m * D + e0[j]));
                 wv = weights(w, w_f32, e0[j]);
             };
@@ -240,7 +249,7 @@ __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
                 if (in[j]) {
                     fetch(j);
                     f32x8 o = gradient(j, n, g, wv);
-                    if (dh) o += widen(load_raw(dh + m * D + e0[j]));
+                    if constexpr (DH) o += widen(load_raw(dh + m * D + e0[j]));
                     store_8(dx + m * D + e0[j], o);
                 }
         }
@@ -298,21 +307,26 @@ struct NormArgs {
 // Lanes of a row of D elements in NC chunks each, in whole waves.
 int lanes_for(int D, int NC) { return ((D + 7) / 8 + 64 * NC - 1) / (64 * NC) * 64; }
 
-template <typename T, bool F8, int NC>
-hipError_t run_norm(const NormArgs &a, hipStream_t s) {
+template <typename T, typename W, bool F8, int NC>
+hipError_t run_norm_of(const NormArgs &a, hipStream_t s) {
     const int threads = lanes_for(a.D, NC);
     if (a.M < 1 || a.M > 0x7fffffff || threads > 1024) return hipErrorInvalidValue;
-    rms_norm_kernel<T, F8, NC><<<static_cast<unsigned>(a.M), threads, 0, s>>>(
-        static_cast<const T *>(a.x), static_cast<const T *>(a.r), a.w, a.w_f32, static_cast<T *>(a.y),
-        static_cast<unsigned char *>(a.q), static_cast<unsigned *>(a.scale), static_cast<T *>(a.h), a.M, a.D,
-        a.ldx, a.ldr, a.eps);
+    const auto kernel = a.r ? rms_norm_kernel<T, W, F8, NC, true> : rms_norm_kernel<T, W, F8, NC, false>;
+    kernel<<<static_cast<unsigned>(a.M), threads, 0, s>>>(
+        static_cast<const T *>(a.x), static_cast<const T *>(a.r), static_cast<const W *>(a.w),
+        static_cast<T *>(a.y), static_cast<unsigned char *>(a.q), static_cast<unsigned *>(a.scale),
+        static_cast<T *>(a.h), a.M, a.D, a.ldx, a.ldr, a.eps);
     return hipGetLastError();
 }
+template <typename T, bool F8, int NC>
+hipError_t run_norm(const NormArgs &a, hipStream_t s) {
+    return a.w_f32 ? run_norm_of<T, float, F8, NC>(a, s) : run_norm_of<T, __bf16, F8, NC>(a, s);
+}
 
-// One chunk per lane, two for many long rows (bf16 with a residual, 56160 rows:
-// D = 5120 428 us with one, 386 (6.0 TB/s) with two, 450 with ten on one wave;
-// D = 2560 197 and 195; D = 1280 99 and 102; one row of 5120 3.3 and 3.5) and
-// for rows that 1024 lanes do not hold.
+// One chunk per lane, two for many long rows and for rows that 1024 lanes do
+// not hold.  With one and with two, bf16 with a residual, 56160 rows: D = 5120
+// 399 and 396 us (5.8 TB/s), in 8 bits 391 and 340; D = 2560 200 and 198, in 8
+// bits 179 and 173; D = 1280 102 and 102; D = 128 15.8 and 18.0.
 template <typename T, bool F8>
 hipError_t norm_typed(const NormArgs &a, hipStream_t s) {
     if ((a.M >= 1024 && a.D > 2048) || a.D > 8192) return run_norm<T, F8, 2>(a, s);
@@ -335,7 +349,11 @@ template <typename T, bool ROWS, int NC, int MAX, bool AHEAD>
 hipError_t run_backward(const BackwardArgs &a, hipStream_t s) {
     const int threads = ROWS ? 256 : lanes_for(a.D, NC);
     if (threads > MAX) return hipErrorInvalidValue;
-    rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD><<<a.P, threads, 0, s>>>(
+    const auto kernel = a.r ? (a.dh ? rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, true, true>
+                                    : rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, true, false>)
+                            : (a.dh ? rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, false, true>
+                                    : rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, false, false>);
+    kernel<<<a.P, threads, 0, s>>>(
         static_cast<const T *>(a.dy), static_cast<const T *>(a.x), static_cast<const T *>(a.r),
         static_cast<const T *>(a.dh), a.w, a.w_f32, static_cast<T *>(a.dx), a.partial, a.M, a.D, a.ldx, a.ldr,
         a.eps);
@@ -355,13 +373,13 @@ hipError_t backward_typed(const BackwardArgs &a, hipStream_t s) {
 int rms_norm_max_width() { return 16384; }
 
 // Workgroups of the backward: up to D = 1024 four rows at once, then one; on
-// 256 CUs so many per CU as measured best (56160 rows: D = 128 31 us with four,
-// D = 640 68 with three and 83 with four, D = 1280 133 with six, 147 with four,
-// D = 2560 261 with three, 275 with four, D = 5120 549 with one, 570 with two).
+// 256 CUs so many per CU as measured best (56160 rows with residual and dh, bf16:
+// D = 128 36 us with one, 28 with two, 24 with four, 22 with eight; D = 640 110,
+// 77, 71, 72; D = 1280 135 with three, 242 with one, 138 with four; D = 2560 274
+// with one or two, 287 with three; D = 5120 528 (5.4 TB/s) with one, 566 with two).
 int rms_norm_partials(int64_t M, int D) {
     const int64_t rows = D <= 1024 ? 4 : 1;
-    const int waves = lanes_for(D, 2) / 64;
-    const int64_t most = 256 * (D <= 512 ? 4 : D <= 1024 ? 3 : waves == 2 ? 6 : waves == 3 ? 3 : waves == 4 ? 2 : 1);
+    const int64_t most = 256 * (D <= 1024 ? 4 : D <= 2048 ? 3 : 1);
     const int64_t sets = (M + rows - 1) / rows;
     return static_cast<int>(sets < most ? sets : most);
 }
