@@ -95,6 +95,23 @@ __device__ inline raw_f32x8 load_raw_once(const float *p) {
     return {__builtin_nontemporal_load(reinterpret_cast<const f32x4_any *>(p)),
             __builtin_nontemporal_load(reinterpret_cast<const f32x4_any *>(p + 4))};
 }
+// A launch's threads along one axis of its grid stay below 2^32, so `blocks`
+// workgroups of up to 1024 threads may take a second axis, which `block_index`
+// joins again; the last ones may have nothing to do.
+inline dim3 grid_of(int64_t blocks) {
+    const int64_t row = int64_t{1} << 21;
+    if (blocks <= row) return dim3(static_cast<unsigned>(blocks));
+    return dim3(static_cast<unsigned>(row), 1, static_cast<unsigned>((blocks + row - 1) / row));
+}
+__device__ inline int64_t block_index() {
+    return static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x;
+}
+
+template <bool ONCE, typename T>
+__device__ inline auto load_raw_if(const T *p) {
+    if constexpr (ONCE) return load_raw_once(p);
+    else return load_raw(p);
+}
 __device__ inline fp8::f32x8 widen(bf16x8_any v) { return __builtin_convertvector(v, fp8::f32x8); }
 __device__ inline fp8::f32x8 widen(raw_f32x8 v) {
     return fp8::f32x8{v.a[0], v.a[1], v.a[2], v.a[3], v.b[0], v.b[1], v.b[2], v.b[3]};
@@ -105,6 +122,20 @@ __device__ inline void store_8(__bf16 *p, fp8::f32x8 v) {
 __device__ inline void store_8(float *p, fp8::f32x8 v) {
     *reinterpret_cast<f32x4_any *>(p) = f32x4_any{v[0], v[1], v[2], v[3]};
     *reinterpret_cast<f32x4_any *>(p + 4) = f32x4_any{v[4], v[5], v[6], v[7]};
+}
+// The same with the hint.
+__device__ inline void store_8_once(__bf16 *p, fp8::f32x8 v) {
+    __builtin_nontemporal_store(static_cast<bf16x8_any>(__builtin_convertvector(v, fp8::bf16x8)),
+                                reinterpret_cast<bf16x8_any *>(p));
+}
+__device__ inline void store_8_once(float *p, fp8::f32x8 v) {
+    __builtin_nontemporal_store(f32x4_any{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_any *>(p));
+    __builtin_nontemporal_store(f32x4_any{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4_any *>(p + 4));
+}
+template <bool ONCE, typename T>
+__device__ inline void store_8_if(T *p, fp8::f32x8 v) {
+    if constexpr (ONCE) store_8_once(p, v);
+    else store_8(p, v);
 }
 
 }  // namespace hcms

@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeSide qs, RopeSide ks, con
     const int turn = R / 2 / NP, units = turn + (d - R + CP - 1) / CP;
     const int per = 256 / units;                          // tokens per workgroup
     const int lt = threadIdx.x / units, u = threadIdx.x - lt * units;
-    const int64_t token = static_cast<int64_t>(blockIdx.x) * per + lt;
+    const int64_t token = block_index() * per + lt;
     if (lt >= per || token >= S) return;
 
     const bool rotates = u < turn;
@@ -164,7 +164,8 @@ hipError_t run_rope(const RopeSide &q, const RopeSide &k, const float *table, co
     int split = 1;
     while (split * blocks < 1024 && (heads + split - 1) / split > kAhead) split *= 2;
     const int each = (heads + split - 1) / split;
-    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>((heads + each - 1) / each));
+    dim3 grid = grid_of(blocks);
+    grid.y = static_cast<unsigned>((heads + each - 1) / each);
     // Inputs and outputs that the 256 MiB of last-level cache do not hold: the
     // inputs are read past it (56160 tokens of 10 heads of 128 in bf16 take 51 us
     // against 58; 7800 of them would take 11.0 against 9.8).

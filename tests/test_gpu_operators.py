@@ -551,3 +551,55 @@ def test_operators_on_another_stream_and_in_a_graph(hcms):
         torch.cuda.synchronize()
         for a, b in zip(out, want):
             assert torch.equal(bits(a), bits(b))
+
+
+def test_rows_past_the_caches_and_past_32_bits(hcms):
+    """Norm, quantisation and rotation of tensors of more than 2^31 elements (the
+    norm then reads past the caches too): bit for bit the last rows taken alone."""
+    M, D, n = 139000, 16384, 1500
+    x = torch.randn(M, D, generator=torch.Generator("cuda").manual_seed(1), dtype=BF16, device="cuda")
+    w = torch.ones(D, dtype=BF16, device="cuda")
+    assert x.numel() > 1 << 31
+    last = x[-n:]
+    log("[2^31] norm")
+    assert torch.equal(bits(hcms.rms_norm(x, w)[-n:]), bits(hcms.rms_norm(last, w)))
+    y, h = hcms.rms_norm(x, w, residual=x)
+    for a, b in zip((y, h), hcms.rms_norm(last, w, residual=last)):
+        assert torch.equal(bits(a[-n:]), bits(b))
+    log("[2^31] norm backward")
+    dx, _ = hcms.rms_norm_backward(x, x, w, residual=x, dh=y)
+    assert torch.equal(bits(dx[-n:]), bits(hcms.rms_norm_backward(last, last, w, residual=last, dh=y[-n:].clone())[0]))
+    del h, dx
+    log("[2^31] norm in 8 bits")
+    q, s = hcms.rms_norm_fp8(x, w)
+    a, b = hcms.rms_norm_fp8(last, w)
+    assert torch.equal(bits(q[-n:]), bits(a)) and torch.equal(bits(s[:, -n:].contiguous()), bits(b))
+    log("[2^31] quantisation")
+    m = M // 512 * 512                       # whole groups of t's scales
+    q, s, t, ts = hcms.quantize_fp8(x[:m], 1, 1)
+    a, b, ta, tb = hcms.quantize_fp8(x[m - 1024:m], 1, 1)
+    assert torch.equal(bits(q[-1024:]), bits(a)) and torch.equal(bits(s[:, -1024:].contiguous()), bits(b))
+    assert torch.equal(bits(t[:, m - 1024:m].contiguous()), bits(ta)) and torch.equal(bits(ts[-2:]), bits(tb))
+    q, s = hcms.quantize_fp8(x, 1)
+    a, b = hcms.quantize_fp8(last, 1)
+    assert torch.equal(bits(q[-n:]), bits(a)) and torch.equal(bits(s[:, -n:].contiguous()), bits(b))
+    del q, s, t, ts
+    log("[2^31] rotation")
+    table = hcms.rope_table([M], [64])
+    r = hcms.rope(x.view(M, 128, 128), None, table, [M], [64])
+    at = torch.arange(M - n, M, dtype=torch.int32, device="cuda")
+    assert torch.equal(bits(r[-n:]), bits(hcms.rope(last.view(n, 128, 128), None, table, [M], [64], positions=at)))
+
+
+def test_rms_norm_in_8_bits_past_the_caches(hcms):
+    """fp32 rows, and bf16 rows whose last chunk the end cuts, past the caches."""
+    for M, D, dtype in ((7000, 5120, FP32), (27000, 2600, BF16)):
+        x = torch.randn(M, D, generator=torch.Generator("cuda").manual_seed(M), dtype=dtype, device="cuda")
+        w = torch.randn(D, generator=torch.Generator("cuda").manual_seed(D), dtype=dtype, device="cuda")
+        for a, b in zip(hcms.rms_norm(x, w, residual=x), hcms.rms_norm(x[-1100:], w, residual=x[-1100:])):
+            assert torch.equal(bits(a[-1100:]), bits(b))
+        if D % 16 == 0:
+            q, s, h = hcms.rms_norm_fp8(x, w, residual=x)
+            a, b, c = hcms.rms_norm_fp8(x[-1100:], w, residual=x[-1100:])
+            assert torch.equal(bits(q[-1100:]), bits(a)) and torch.equal(bits(s[:, -1100:].contiguous()), bits(b))
+            assert torch.equal(bits(h[-1100:]), bits(c))
