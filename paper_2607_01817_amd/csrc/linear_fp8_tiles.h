@@ -9,20 +9,25 @@ namespace hcms {
 // The tiles, and what a round of workgroups and a stage of 128 k take on
 // them, in us, measured: a stage with every CU busy, at the clock the power
 // limit leaves, and with few of them busy; and the start and the epilogue of a
-// round.  On 56160 x 1920 x 5120 the first four take 508, 584, 633 and 595 us;
-// on 1560 x 5120 x 5120 55, 49, 76 and 58 (the fifth 64); on 1560 x 1920 x
-// 5120 52, 47, 43 and 23 (34); on 512 x 512 x 4096 37, 29, 23, 17, 14 and 13.
+// round.  `groups`: of waves, which share the stages of a tile between them and
+// add up their sums (halves the time of a long k where few tiles are at work).
+// On 56160 x 1920 x 5120 the first four take 508, 584, 546 and 595 us; on 1560
+// x 5120 x 5120 55, 49, 61 and 58 (the fifth 64); on 1560 x 1920 x 5120 52, 47,
+// 32 and 23 (34); on 512 x 512 x 4096 37, 29, 22, 17, 14, 13 and 10.4; on 256 x
+// 1920 x 5120 the last two 15.9 and 12.1, on 100 x 640 x 640 4.5 and 5.1.
 struct Fp8TileCost {
-    int bm, bn, per_cu;
+    int bm, bn, per_cu, groups;
     double full, alone, fixed;
 };
 inline constexpr Fp8TileCost kFp8Tiles[] = {
-    {256, 256, 1, 1.70, 0.99, 5.0}, {192, 256, 1, 1.30, 0.79, 4.0}, {128, 256, 1, 0.99, 0.60, 2.7},
-    {128, 128, 1, 0.54, 0.37, 2.0}, {64, 128, 1, 0.40, 0.26, 1.0},  {64, 64, 2, 0.46, 0.26, 1.0}};
+    {256, 256, 1, 1, 1.70, 0.99, 5.0}, {192, 256, 1, 1, 1.30, 0.79, 4.0}, {128, 256, 1, 1, 0.89, 0.70, 2.7},
+    {128, 128, 1, 1, 0.54, 0.37, 2.0}, {64, 128, 1, 1, 0.40, 0.26, 1.0},  {64, 64, 2, 1, 0.46, 0.26, 1.0},
+    {64, 64, 1, 2, 0.25, 0.18, 2.1}};
 // For fp32 output, whose widened operands run at the bf16 rate and do not fit
 // beside the accumulators of a larger tile.
 inline constexpr Fp8TileCost kFp8WideTiles[] = {
-    {256, 128, 1, 1.53, 1.23, 4.5}, {128, 128, 1, 0.98, 0.83, 2.2}, {64, 64, 2, 0.70, 0.57, 1.2}};
+    {256, 128, 1, 1, 1.53, 1.23, 4.5}, {128, 128, 1, 1, 0.98, 0.83, 2.2}, {64, 64, 2, 1, 0.70, 0.57, 1.2},
+    {64, 64, 1, 2, 0.40, 0.37, 2.2}};   // 256 x 1920 x 5120: the last two 26.7 and 19.3 us
 
 // Up to so many rows the kernel for few rows runs (64 rows by N = K = 5120 take
 // 17.6 us on it and 15.3 on tiles; by N = 640, 16.1 and 15.3).

@@ -3,8 +3,9 @@
 ragged rows, columns and last blocks of k.  A host test checks the tiles; the GPU
 tests run the shapes."""
 
-TILES = {"bf16": [(256, 256), (192, 256), (128, 256), (128, 128), (64, 128), (64, 64)],
-         "fp32": [(256, 128), (128, 128), (64, 64)]}
+# (rows, columns, groups of waves)
+TILES = {"bf16": [(256, 256, 1), (192, 256, 1), (128, 256, 1), (128, 128, 1), (64, 128, 1), (64, 64, 1), (64, 64, 2)],
+         "fp32": [(256, 128, 1), (128, 128, 1), (64, 64, 1), (64, 64, 2)]}
 
 # (output type, tile, more than one round, M, N, K)
 SHAPES = [
@@ -20,10 +21,14 @@ SHAPES = [
     ("bf16", 4, True, 265, 10952, 272),
     ("bf16", 5, False, 35, 16, 272),
     ("bf16", 5, True, 521, 7184, 80),
+    ("bf16", 6, False, 35, 72, 2064),
+    ("bf16", 6, False, 1561, 520, 4240),
     ("fp32", 0, False, 321, 10888, 272),
     ("fp32", 0, True, 13111, 904, 80),
     ("fp32", 1, False, 145, 10888, 656),
     ("fp32", 1, True, 529, 10904, 272),
-    ("fp32", 2, False, 35, 16, 656),
+    ("fp32", 2, False, 35, 16, 80),
     ("fp32", 2, True, 10889, 264, 272),
+    ("fp32", 3, False, 35, 16, 656),
+    ("fp32", 3, False, 261, 1928, 2064),
 ]
