@@ -7,10 +7,12 @@
 // magnitude kept, which is the transpose and so the backward.  Elements past R
 // are copied.
 //
-// What bounds it: bytes, once in and once out.  A thread takes one unit (8
-// elements, in the layout of halves 8 and their partners) of one token and
-// goes through the heads with it, so the table entries and the coordinates
-// are read once for all of them.
+// What bounds it: bytes, once in and once out (56160 tokens of 10 heads of 128
+// in bf16, row-major positions: 50 us, 5.8 TB/s; 7801 tokens of 18 heads of 64
+// in fp32 15.8 us, 4.5 TB/s; a few tokens 3.5 us, which is latency).  A thread
+// takes one unit (8 elements, in the layout of halves 8 and their partners) of
+// one token and goes through the heads with it, so the table entries and the
+// coordinates are read once for all of them.
 #include "fp8.h"
 #include "hcms_internal.h"
 
@@ -20,28 +22,32 @@ namespace {
 constexpr int kAhead = 4;   // heads whose loads are in flight together
 
 template <typename T, int V>
-struct Unit;   // V elements of T in one access
+struct Unit;   // V elements of T in one access, as stored until they are used
 template <typename T>
 struct Unit<T, 1> {
-    float v[1];
+    T raw;
     template <bool ONCE>
     __device__ void load(const T *p) {
-        v[0] = static_cast<float>(*p);
+        raw = *p;
     }
-    __device__ void store(T *p) const { *p = static_cast<T>(v[0]); }
+    __device__ void get(float (&v)[1]) const { v[0] = static_cast<float>(raw); }
+    __device__ void copy(T *p) const { *p = raw; }
+    static __device__ void store(T *p, const float (&v)[1]) { *p = static_cast<T>(v[0]); }
 };
 template <typename T>
 struct Unit<T, 8> {
-    float v[8];
+    decltype(load_raw(static_cast<const T *>(nullptr))) raw;
     template <bool ONCE>
     __device__ void load(const T *p) {
-        fp8::f32x8 x;
-        if constexpr (ONCE) x = widen(load_raw_once(p));
-        else x = widen(load_raw(p));
+        raw = load_raw_if<ONCE>(p);
+    }
+    __device__ void get(float (&v)[8]) const {
+        const fp8::f32x8 x = widen(raw);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = x[i];
     }
-    __device__ void store(T *p) const {
+    __device__ void copy(T *p) const { store_8(p, widen(raw)); }
+    static __device__ void store(T *p, const float (&v)[8]) {
         store_8(p, fp8::f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
     }
 };
@@ -68,6 +74,23 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeSide qs, RopeSide ks, con
     const int e0 = rotates ? (HALF ? p0 : 2 * p0) : R + (u - turn) * CP;
     const int e1 = rotates ? (HALF ? p0 + R / 2 : 2 * p0 + 1) : e0 + 1;
     const bool second = TWO && (rotates || (V == 1 && e1 < d));
+    const int heads = qs.H + ks.H;
+    const int hb = blockIdx.y * heads_per_block, he = min(hb + heads_per_block, heads);
+    // The loads of kAhead heads from h0 on, none behind a branch, which would wait
+    // for those in flight: heads past the last and second accesses that there are
+    // not read what is read anyway.
+    Unit<T, V> a[kAhead], b[kAhead];
+    const auto fetch = [&](int h0) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int h = min(h0 + k, he - 1);
+            const RopeSide &side = h < qs.H ? qs : ks;
+            const T *x = static_cast<const T *>(side.x) + token * side.x_token + (h < qs.H ? h : h - qs.H) * side.x_head;
+            a[k].template load<ONCE>(x + e0);
+            if constexpr (TWO) b[k].template load<ONCE>(x + (second ? e1 : e0));
+        }
+    };
+    fetch(hb);   // ahead of the coordinates and the table: 8 tokens of 48 heads 3.5 us, behind them 3.8
     float c[NP], s[NP];
     if (rotates) {
         int row[kRopeMaxAxes] = {};
@@ -102,37 +125,32 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeSide qs, RopeSide ks, con
             s[i] = inside ? (inverse ? -cs.y : cs.y) : __builtin_nanf("");
         }
     }
-    const int heads = qs.H + ks.H;
-    const int hb = blockIdx.y * heads_per_block, he = min(hb + heads_per_block, heads);
     for (int h0 = hb; h0 < he; h0 += kAhead) {
-        Unit<T, V> a[kAhead], b[kAhead];
+        if (h0 > hb) fetch(h0);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int h = h0 + k;
             if (h >= he) break;
-            const RopeSide &side = h < qs.H ? qs : ks;
-            const T *x = static_cast<const T *>(side.x) + token * side.x_token + (h < qs.H ? h : h - qs.H) * side.x_head;
-            a[k].template load<ONCE>(x + e0);
-            if (second) b[k].template load<ONCE>(x + e1);
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int h = h0 + k;
-            if (h >= he) break;
-            if (rotates) {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    float &x0 = a[k].v[TWO ? i : 2 * i];
-                    float &x1 = TWO ? b[k].v[i] : a[k].v[2 * i + 1];
-                    const float u0 = x0, u1 = x1;
-                    x0 = __builtin_fmaf(u0, c[i], -(u1 * s[i]));
-                    x1 = __builtin_fmaf(u0, s[i], u1 * c[i]);
-                }
-            }
             const RopeSide &side = h < qs.H ? qs : ks;
             T *y = static_cast<T *>(side.y) + token * side.y_token + (h < qs.H ? h : h - qs.H) * side.y_head;
-            a[k].store(y + e0);
-            if (second) b[k].store(y + e1);
+            if (!rotates) {
+                a[k].copy(y + e0);
+                if (second) b[k].copy(y + e1);
+                continue;
+            }
+            float u[V], v[V];
+            a[k].get(u);
+            if constexpr (TWO) b[k].get(v);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                float &x0 = u[TWO ? i : 2 * i];
+                float &x1 = TWO ? v[i] : u[2 * i + 1];
+                const float u0 = x0, u1 = x1;
+                x0 = __builtin_fmaf(u0, c[i], -(u1 * s[i]));
+                x1 = __builtin_fmaf(u0, s[i], u1 * c[i]);
+            }
+            Unit<T, V>::store(y + e0, u);
+            if constexpr (TWO) Unit<T, V>::store(y + e1, v);
         }
     }
 }
@@ -168,7 +186,8 @@ hipError_t run_rope(const RopeSide &q, const RopeSide &k, const float *table, co
     grid.y = static_cast<unsigned>((heads + each - 1) / each);
     // Inputs and outputs that the 256 MiB of last-level cache do not hold: the
     // inputs are read past it (56160 tokens of 10 heads of 128 in bf16 take 51 us
-    // against 58; 7800 of them would take 11.0 against 9.8).
+    // against 58; 7800 of them would take 11.0 against 9.8; the outputs written
+    // past it too, 56).
     const bool once = V > 1 && 2 * static_cast<int64_t>(sizeof(T)) * S * heads * d > (256LL << 20);
     if (V > 1 && once)
         rope_kernel<T, V, HALF, (V > 1)><<<grid, 256, 0, stream>>>(q, k, table, ax, positions, pos64, S, d, R,
