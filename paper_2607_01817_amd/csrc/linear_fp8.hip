@@ -424,9 +424,9 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
 }
 
 // Few rows: what counts is that all of W is in flight at once (1 x 5120 x 5120
-// takes 7.6 us, 16 rows 9.2 and 32 12.1; on 64 x 64 tiles, whose stages wait
-// for each other, 15.3).  A workgroup
-// takes 16 NT columns of Y and all rows (16 MT hold them), its waves the blocks
+// takes 7.6 us, 9.2 with W from memory, 2.8 TB/s; 16 rows 9.2 and 32 12.1; on
+// 64 x 64 tiles, whose stages wait for each other, 15.3).  A workgroup takes
+// 16 NT columns of Y and all rows (16 MT hold them), its waves the blocks
 // of k in turn; every wave loads its operands straight into registers, and the
 // waves' sums are added through LDS in the order of the waves.  MFMA 16 x 16 x
 // 128 (for fp32 output 16 x 16 x 32 in bf16): lane (li, g) holds 32 k of one
@@ -437,8 +437,9 @@ __global__ __launch_bounds__(512) void linear_fp8_rows_kernel(
     const unsigned char *__restrict__ x, const unsigned *__restrict__ xs, const unsigned char *__restrict__ w,
     const unsigned *__restrict__ ws, T *__restrict__ y, int M, int N, int K, int np) {
     constexpr bool kWide = sizeof(T) == 4;
-    // Blocks whose loads are in flight together: 5 for K = 5120 on 8 waves.
-    constexpr int kDeep = NT * MT == 1 ? 8 : NT * MT == 2 ? 5 : 4;
+    // Blocks whose loads are in flight together: K = 5120 on 8 waves has 5 each
+    // (with 5 in place of 6, one row by 5120 x 640 took 7.2 us and not 3.4).
+    constexpr int kDeep = NT * MT == 1 ? 8 : NT * MT == 2 ? 6 : 4;
     __shared__ f32x4 part[8][NT][MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int li = lane & 15, g = lane >> 4;
