@@ -11,11 +11,13 @@ namespace hcms {
 // limit leaves, and with few of them busy; and the start and the epilogue of a
 // round.  `groups`: of waves, which share the stages of a tile between them and
 // add up their sums (halves the time of a long k where few tiles are at work).
-// On 56160 x 1920 x 5120 the first four take 508, 584, 546 and 595 us; on 1560
-// x 5120 x 5120 55, 49, 61 and 58 (the fifth 64); on 1560 x 1920 x 5120 52, 47,
-// 32 and 23 (34); on 512 x 512 x 4096 37, 29, 22, 17, 14, 13 and 10.4; on 256 x
-// 1920 x 5120 the 64 x 64 ones 15.9 and 12.1, on 100 x 640 x 640 4.5 and 5.1; the
-// last 497, 45, 33 on the first three.
+// In us, in the order of the table:
+//   56160 x 1920 x 5120   491  583  531  606  850 1043 1135  476  799
+//   1560 x 5120 x 5120     54   48   62   60   67   79   88   40   62
+//   1560 x 1920 x 5120     52   47   31   23   34   41   34   33   30
+//   1000 x 1920 x 5120     53   44   31   22   19   22   23   33   16.2
+//   512 x 512 x 4096       37   30   25   18   15   14   10.4 26   12.6
+//   1000 x 1536 x 640      10.0  8.6  8.4  6.6  5.6  6.2  8.8  8.7  6.0
 struct Fp8TileCost {
     int bm, bn, per_cu, groups;
     double full, alone, fixed;
@@ -23,13 +25,17 @@ struct Fp8TileCost {
 inline constexpr Fp8TileCost kFp8Tiles[] = {
     {256, 256, 1, 1, 1.70, 0.99, 5.0}, {192, 256, 1, 1, 1.30, 0.79, 4.0}, {128, 256, 1, 1, 0.89, 0.70, 2.7},
     {128, 128, 1, 1, 0.54, 0.37, 2.0}, {64, 128, 1, 1, 0.40, 0.26, 1.0},  {64, 64, 2, 1, 0.46, 0.26, 1.0},
-    {64, 64, 1, 2, 0.25, 0.18, 2.1},   {192, 192, 1, 1, 1.00, 0.65, 3.4}};
+    {64, 64, 1, 2, 0.25, 0.18, 2.1},   {192, 192, 1, 1, 0.96, 0.65, 3.4},
+    {64, 128, 1, 2, 0.335, 0.27, 2.1}};
 // For fp32 output, whose widened operands run at the bf16 rate and do not fit
-// beside the accumulators of a larger tile.  56160 x 1920 x 5120: the first 911
-// us, the last 981; 1560 x 5120 x 5120: 117, 114, 127, 140, 83; 256 x 1920 x 5120:
-// the 64 x 64 ones 26.7 and 19.3.
+// beside the accumulators of a larger tile:
+//   56160 x 1920 x 5120   900  989 1572 1799  955
+//   1560 x 5120 x 5120    114  103  118  140   80
+//   3001 x 1000 x 1936     26.6 18.4 29.6 28.1 35.6
+//   256 x 1920 x 5120      53   32   27.5 18.7 76
+// (128 x 128 without groups, on eight waves: 1126, 117, 21.9 and 40).
 inline constexpr Fp8TileCost kFp8WideTiles[] = {
-    {256, 128, 1, 1, 1.53, 1.23, 4.5}, {128, 128, 1, 1, 0.98, 0.83, 2.2}, {64, 64, 2, 1, 0.70, 0.57, 1.2},
+    {256, 128, 1, 1, 1.53, 1.23, 4.5}, {128, 128, 1, 2, 0.87, 0.66, 2.2}, {64, 64, 2, 1, 0.70, 0.57, 1.2},
     {64, 64, 1, 2, 0.40, 0.37, 2.2},   {192, 192, 1, 1, 1.95, 1.79, 3.5}};
 
 // Up to so many rows the kernel for few rows runs (64 rows by N = K = 5120 take
