@@ -11,9 +11,9 @@
 //
 // What bounds it: bytes, each element read once, whatever is made of it.  bf16,
 // read and written bytes: 56160 x 5120 by rows 146 us (5.9 TB/s), with the
-// transpose 227 (5.1); 7800 x 5120 20.7 and 32; 1560 x 5120 6.5 and 11.  The rows
-// alone have a kernel of their own, without the tile's detour: 20.7 us against the
-// 22.5 that the 128 x 128 tile takes for the same bytes.
+// transpose 228 (5.0); 7800 x 5120 19.4 (6.2 TB/s) and 28 (5.7); 1560 x 5120 5.5
+// and 9.4.  The rows alone have a kernel of their own, without the tile's detour:
+// 7800 x 5120 20.7 us against the tile's 22.5 for the same bytes.
 #include "fp8.h"
 #include "hcms_internal.h"
 
@@ -102,9 +102,14 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(const T *__restrict_
     const int e = kb * kTile + c * 8;
     // Kept as stored and widened where they are used: 32 registers, not 64.
     using Raw = decltype(load_raw(x));
+    // Loads past the ends read the last row or columns (a load behind a branch
+    // would be waited for there) and count as zeros.
     Raw v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = m0 + i < M && e < K ? load_raw(x + (m0 + i) * ldx + e) : Raw{};
+    for (int i = 0; i < 8; ++i) v[i] = load_raw(x + min(m0 + i, M - 1) * ldx + min(e, K - 8));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (m0 + i >= M || e >= K) v[i] = Raw{};
     unsigned row_max[8], all = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
