@@ -142,8 +142,8 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(
 // dw in registers.  Rows that 512 lanes do not hold, whose values and next row
 // would not fit the registers, are read twice instead.  The shares go to partial
 // [gridDim.x][D] and are summed by sum_rows_kernel, so no atomics: the order is
-// fixed.  RES, DH: with the residual, with dh.
-template <typename T, bool ROWS, int NC, int MAX, bool AHEAD, bool RES, bool DH>
+// fixed.  RES, DH: with the residual, with dh.  ONCE: past the caches.
+template <typename T, bool ROWS, int NC, int MAX, bool AHEAD, bool RES, bool DH, bool ONCE>
 __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
     const T *__restrict__ dy, const T *__restrict__ x, const T *__restrict__ r, const T *__restrict__ dh,
     const void *__restrict__ w, bool w_f32, T *__restrict__ dx, float *__restrict__ partial, int64_t M, int D,
@@ -195,9 +195,9 @@ __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
             at = at < M ? at : M - 1;
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                xn[j] = load_raw(x + at * ldx + e0[j]);
-                gn[j] = load_raw(dy + at * D + e0[j]);
-                if constexpr (RES) rn[j] = load_raw(r + at * ldr + e0[j]);
+                xn[j] = load_raw_if<ONCE>(x + at * ldx + e0[j]);
+                gn[j] = load_raw_if<ONCE>(dy + at * D + e0[j]);
+                if constexpr (RES) rn[j] = load_raw_if<ONCE>(r + at * ldr + e0[j]);
             }
         };
 #pragma unroll
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
             Raw dhr[DH ? NC : 1];
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                if constexpr (DH) dhr[j] = load_raw(dh + m * D + e0[j]);
+                if constexpr (DH) dhr[j] = load_raw_if<ONCE>(dh + m * D + e0[j]);
             }
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
             for (int j = 0; j < NC; ++j) {
                 f32x8 o = gradient(j, n[j], g[j], wv[j]);
                 if constexpr (DH) o += widen(dhr[j]);
-                store_8(dx + m * D + e0[j], o);
+                store_8_if<ONCE>(dx + m * D + e0[j], o);
             }
         }
     } else {
@@ -277,21 +277,29 @@ __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
         if (in[j]) store_8(partial + static_cast<int64_t>(blockIdx.x) * D + e0[j], acc[j]);
 }
 
-// out[d] = sum over P rows of partial[P][D]: 16 columns per workgroup, 16 lanes
-// each, whose sums are added in order.
+// out[d] = sum over P rows of partial[P][D]: 16 columns per workgroup, 64 lanes
+// each, whose sums are added in a fixed order (16 lanes each: 256 rows of 5120
+// 4.3 us in the trace).
 template <typename T>
-__global__ __launch_bounds__(256) void sum_rows_kernel(const float *__restrict__ partial, T *__restrict__ out,
-                                                       int P, int D) {
-    __shared__ float part[16][17];
+__global__ __launch_bounds__(1024) void sum_rows_kernel(const float *__restrict__ partial, T *__restrict__ out,
+                                                        int P, int D) {
+    __shared__ float part[64][17];
     const int col = threadIdx.x & 15, k = threadIdx.x >> 4, d = blockIdx.x * 16 + col;
     float s = 0;
     if (d < D)
-#pragma unroll 8
-        for (int p = k; p < P; p += 16) s += partial[static_cast<int64_t>(p) * D + d];
+#pragma unroll 4
+        for (int p = k; p < P; p += 64) s += partial[static_cast<int64_t>(p) * D + d];
     part[k][col] = s;
     __syncthreads();
+    if (k < 8) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) s += part[k + 8 * i][col];
+        part[k][col] = s;
+    }
+    __syncthreads();
     if (k == 0 && d < D) {
-        for (int i = 1; i < 16; ++i) s += part[i][col];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) s += part[i][col];
         out[d] = static_cast<T>(s);
     }
 }
@@ -355,19 +363,29 @@ struct BackwardArgs {
     int P;
 };
 
-template <typename T, bool ROWS, int NC, int MAX, bool AHEAD>
-hipError_t run_backward(const BackwardArgs &a, hipStream_t s) {
+template <typename T, bool ROWS, int NC, int MAX, bool AHEAD, bool ONCE>
+hipError_t run_backward_of(const BackwardArgs &a, hipStream_t s) {
     const int threads = ROWS ? 256 : lanes_for(a.D, NC);
     if (threads > MAX) return hipErrorInvalidValue;
-    const auto kernel = a.r ? (a.dh ? rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, true, true>
-                                    : rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, true, false>)
-                            : (a.dh ? rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, false, true>
-                                    : rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, false, false>);
+    const auto kernel = a.r ? (a.dh ? rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, true, true, ONCE>
+                                    : rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, true, false, ONCE>)
+                            : (a.dh ? rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, false, true, ONCE>
+                                    : rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, false, false, ONCE>);
     kernel<<<a.P, threads, 0, s>>>(
         static_cast<const T *>(a.dy), static_cast<const T *>(a.x), static_cast<const T *>(a.r),
         static_cast<const T *>(a.dh), a.w, a.w_f32, static_cast<T *>(a.dx), a.partial, a.M, a.D, a.ldx, a.ldr,
         a.eps);
     return hipGetLastError();
+}
+// Tensors that the last-level cache does not hold together are read and written
+// past the caches (bf16 with residual and dh: 7800 x 5120, 400 MB, 73 us without and
+// 65 with; 56160 x 5120 520 and 476; 30000 x 1280 72 and 63; 3000 x 5120, 154 MB, 27.0
+// and 27.5).  Rows that are read twice have to be kept.
+template <typename T, bool ROWS, int NC, int MAX, bool AHEAD>
+hipError_t run_backward(const BackwardArgs &a, hipStream_t s) {
+    const int64_t bytes = a.M * a.D * static_cast<int64_t>(sizeof(T)) * (3 + (a.r != nullptr) + (a.dh != nullptr));
+    if (AHEAD && bytes > int64_t{256} << 20) return run_backward_of<T, ROWS, NC, MAX, AHEAD, AHEAD>(a, s);
+    return run_backward_of<T, ROWS, NC, MAX, AHEAD, false>(a, s);
 }
 
 template <typename T>
@@ -383,13 +401,14 @@ hipError_t backward_typed(const BackwardArgs &a, hipStream_t s) {
 int rms_norm_max_width() { return 16384; }
 
 // Workgroups of the backward: up to D = 1024 four rows at once, then one; on
-// 256 CUs so many per CU as measured best (56160 rows with residual and dh, bf16:
-// D = 128 36 us with one, 28 with two, 24 with four, 22 with eight; D = 640 110,
-// 77, 71, 72; D = 1280 135 with three, 242 with one, 138 with four; D = 2560 274
-// with one or two, 287 with three; D = 5120 528 (5.4 TB/s) with one, 566 with two).
+// 256 CUs so many per CU as measured best (bf16 with residual and dh; 56160 rows: D =
+// 128 36 us with one, 28 with two, 24 with four, 22 with eight; D = 640 110, 77, 71,
+// 72; 30000 rows: D = 1280 130, 94, 70 with three, 63 with four; D = 2560 142, 124,
+// 134, 137; D = 3840 178, 202; 56160 x 5120 476 (6.0 TB/s), 524).
 int rms_norm_partials(int64_t M, int D) {
     const int64_t rows = D <= 1024 ? 4 : 1;
-    const int64_t most = 256 * (D <= 1024 ? 4 : D <= 2048 ? 3 : 1);
+    const int waves = lanes_for(D, 2) / 64;   // of a row past D = 1024
+    const int64_t most = 256 * (D <= 1024 || waves <= 2 ? 4 : waves == 3 ? 2 : 1);
     const int64_t sets = (M + rows - 1) / rows;
     return static_cast<int>(sets < most ? sets : most);
 }
@@ -413,8 +432,8 @@ hipError_t launch_rms_norm_backward(const void *dy, const void *x, const void *r
         if (e != hipSuccess) return e;
     }
     const int blocks = (D + 15) / 16;
-    if (w_f32) sum_rows_kernel<<<blocks, 256, 0, stream>>>(partial, static_cast<float *>(dw), P, D);
-    else sum_rows_kernel<<<blocks, 256, 0, stream>>>(partial, static_cast<__bf16 *>(dw), P, D);
+    if (w_f32) sum_rows_kernel<<<blocks, 1024, 0, stream>>>(partial, static_cast<float *>(dw), P, D);
+    else sum_rows_kernel<<<blocks, 1024, 0, stream>>>(partial, static_cast<__bf16 *>(dw), P, D);
     return hipGetLastError();
 }
 

@@ -603,3 +603,28 @@ def test_rms_norm_in_8_bits_past_the_caches(hcms):
             a, b, c = hcms.rms_norm_fp8(x[-1100:], w, residual=x[-1100:])
             assert torch.equal(bits(q[-1100:]), bits(a)) and torch.equal(bits(s[:, -1100:].contiguous()), bits(b))
             assert torch.equal(bits(h[-1100:]), bits(c))
+
+
+@pytest.mark.parametrize("M,D,dtype", [(70001, 512, BF16), (30003, 1000, BF16), (14003, 1608, FP32), (13001, 2560, BF16),
+                                       (5001, 5117, FP32)])
+def test_rms_norm_gradient_past_the_caches(hcms, M, D, dtype):
+    """Each form of the backward on tensors that the caches do not hold: dx of the
+    first and last rows bit for bit as taken alone, dw against float64."""
+    log(f"[norm gradient past the caches] M={M} D={D} {dtype}")
+    g = torch.Generator("cuda").manual_seed(M + D)
+    dy, x, r, dh = (torch.randn(M, D, generator=g, dtype=dtype, device="cuda") for _ in range(4))
+    assert 5 * x.numel() * x.element_size() > 256 << 20
+    w = 1 + 0.1 * torch.randn(D, generator=g, device="cuda")
+    dx, dw = hcms.rms_norm_backward(dy, x, w, 1e-5, r, dh)
+    n = 700
+    for a in (slice(0, n), slice(M - n, M)):
+        alone, _ = hcms.rms_norm_backward(dy[a].clone(), x[a].clone(), w, 1e-5, r[a].clone(), dh[a].clone())
+        assert torch.equal(bits(dx[a].contiguous()), bits(alone))
+    want, size = torch.zeros(D, device="cuda", dtype=torch.float64), torch.zeros(D, device="cuda", dtype=torch.float64)
+    for i in range(0, M, 8192):
+        s = slice(i, i + 8192)
+        h = x[s].double() + r[s].double()
+        t = dy[s].double() * h / (h.square().mean(1, keepdim=True) + 1e-5).sqrt()
+        want += t.sum(0)
+        size += t.abs().sum(0)
+    _within(dw, _f64(want), 2.0 ** -24 * np.abs(_f64(want)) + 2.0 ** -17 * _f64(size), "dw")
