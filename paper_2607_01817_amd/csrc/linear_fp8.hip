@@ -423,79 +423,127 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
     wait_vm<0>();   // no load into LDS is pending when the workgroup ends
 }
 
-// Few rows: what counts is that all of W is in flight at once (1 x 5120 x 5120
-// takes 7.6 us, 9.2 with W from memory, 2.8 TB/s; 16 rows 9.2 and 32 12.1; on
-// 64 x 64 tiles, whose stages wait for each other, 15.3).  A workgroup takes
-// 16 NT columns of Y and all rows (16 MT hold them), its waves the blocks
-// of k in turn; every wave loads its operands straight into registers, and the
-// waves' sums are added through LDS in the order of the waves.  MFMA 16 x 16 x
-// 128 (for fp32 output 16 x 16 x 32 in bf16): lane (li, g) holds 32 k of one
-// row of W and of X (chunks g and 4 + g of the block's eight, so that a load
-// covers 64 bytes of a row), and of Y^T row m = li, columns 4 g .. 4 g + 3.
+// Few rows: what counts is that all of W is in flight at once and that a load
+// covers whole lines: 16 consecutive lanes of a load that read 16 rows cost 16
+// look-ups, and straight from memory into the MFMA's operands (lane li holds row
+// li) every load is of that kind: 1 x 5120 x 5120 7.5 us, 16 rows 9.2, 32 rows 12.0.
+// So 8 lanes load a row's block of 128, and the operands pass through LDS, a place
+// of each wave's own: 5.2 us (5.0 TB/s; 7.6 with W from memory), 5.3 and 7.4; 64
+// rows 9.8, on 64 x 64 tiles, whose stages wait for each other, 12.2.  A workgroup
+// takes 16 NT columns of Y and all rows (16 MT hold them), its waves the blocks of
+// k in turn, and the waves' sums are added through LDS in the order of the waves.
+// MFMA 16 x 16 x 128 (for fp32 output 16 x 16 x 32 in bf16): lane (li, g) holds 32
+// k of one row of W and of X (chunks g and 4 + g of the block's eight), and of Y^T
+// row m = li, columns 4 g .. 4 g + 3.
 template <typename T, int NT, int MT>
 __global__ __launch_bounds__(512) void linear_fp8_rows_kernel(
     const unsigned char *__restrict__ x, const unsigned *__restrict__ xs, const unsigned char *__restrict__ w,
     const unsigned *__restrict__ ws, T *__restrict__ y, int M, int N, int K, int np) {
     constexpr bool kWide = sizeof(T) == 4;
-    // Blocks whose loads are in flight together: K = 5120 on 8 waves has 5 each
-    // (with 5 in place of 6, one row by 5120 x 640 took 7.2 us and not 3.4).
-    constexpr int kDeep = NT * MT == 1 ? 8 : NT * MT == 2 ? 6 : 4;
+    // Blocks whose loads are in flight together, as many as the registers hold (32
+    // rows by 5120 x 5120 from memory: 4 of them 10.9 us, 3 11.1, 5 spill).
+    constexpr int kDeep = NT + MT == 2 ? 8 : NT + MT == 3 ? 6 : MT == 2 ? 4 : 2;
+    __shared__ __attribute__((aligned(16))) char stage[8][(NT + MT) * 2048];
     __shared__ f32x4 part[8][NT][MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int li = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * (16 * NT), nkb = (K + 127) / 128, n_blocks = (N + 127) / 128;
-    const unsigned char *wr[NT], *xr[MT];
-    int m[MT];
+    // Lane l loads chunk l % 8 of rows l / 8 and 8 + l / 8 of each 16.
+    const int row = lane >> 3, chunk = (lane & 7) * 16;
+    const unsigned char *wr[NT][2], *xr[MT][2];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) wr[i] = w + static_cast<int64_t>(min(n0 + 16 * i + li, N - 1)) * K + g * 16;
+    for (int c = 0; c < 2; ++c) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        m[i] = min(16 * i + li, M - 1);
-        xr[i] = x + static_cast<int64_t>(m[i]) * K + g * 16;
+        for (int i = 0; i < NT; ++i)
+            wr[i][c] = w + static_cast<int64_t>(min(n0 + 16 * i + 8 * c + row, N - 1)) * K;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xr[i][c] = x + static_cast<int64_t>(min(16 * i + 8 * c + row, M - 1)) * K;
     }
+    // Chunk q of staged row r sits at place q ^ (r / 2 % 8): the 16 rows of a read
+    // lie in 16 different groups of 4 banks.
+    char *const mine = stage[wave];
+    char *const put = mine + row * 128 + (chunk ^ ((row >> 1) << 4));          // of row 8 + row: place ^ 4
+    const char *const get = mine + li * 128 + ((g ^ (li >> 1)) << 4);          // of chunk 4 + g: place ^ 4
     f32x4 acc[NT][MT]{};
-    const auto load32 = [&](const unsigned char *p, int kb, bool row) {
-        i32x4 lo{}, hi{};
-        const int k = row ? kb * 128 + g * 16 : K;
-        if (k < K) lo = *reinterpret_cast<const i32x4 *>(p + kb * 128);
-        if (k + 64 < K) hi = *reinterpret_cast<const i32x4 *>(p + kb * 128 + 64);
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    for (int kb0 = wave; kb0 < nkb; kb0 += waves * kDeep) {
-        i32x8 a[kDeep][NT], b[kDeep][MT];
-        unsigned sa[kDeep], sb[kDeep][MT];
+    // D blocks from kb0 on, without a branch around the loads, which would wait for
+    // them there: rows past the ends read the last row (their sums are not stored),
+    // chunks past K the row's last one, and are made zeros before they are used.
+    const auto blocks = [&](int kb0, auto depth) {
+        constexpr int D = depth();
+        i32x4 a[D][NT][2], b[D][MT][2];
+        unsigned sa[D], sb[D][MT];
 #pragma unroll
-        for (int d = 0; d < kDeep; ++d) {
-            const int kb = kb0 + d * waves;
-            if (kb >= nkb) break;
+        for (int d = 0; d < D; ++d) {
+            const int kb = kb0 + d * waves, at = min(kb * 128 + chunk, K - 16);
 #pragma unroll
-            for (int i = 0; i < NT; ++i) a[d][i] = load32(wr[i], kb, true);
+            for (int c = 0; c < 2; ++c) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) b[d][i] = load32(xr[i], kb, 16 * i + li < M);
+                for (int i = 0; i < NT; ++i) a[d][i][c] = *reinterpret_cast<const i32x4 *>(wr[i][c] + at);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) b[d][i][c] = *reinterpret_cast<const i32x4 *>(xr[i][c] + at);
+            }
             const int64_t grp = kb >> 2;
-            sa[d] = ws[grp * n_blocks + n0 / 128] >> (kb & 3) * 8 & 255;
+            sa[d] = ws[grp * n_blocks + n0 / 128];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) sb[d][i] = xs[grp * M + m[i]] >> (kb & 3) * 8 & 255;
+            for (int i = 0; i < MT; ++i) sb[d][i] = xs[grp * M + min(16 * i + li, M - 1)];
         }
 #pragma unroll
-        for (int d = 0; d < kDeep; ++d) {
-            if (kb0 + d * waves >= nkb) break;
+        for (int d = 0; d < D; ++d) {
+            const int kb = kb0 + d * waves, sh = (kb & 3) * 8;
+            if (d == D - 1 && kb * 128 + chunk >= K) {
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
+                for (int c = 0; c < 2; ++c) {
 #pragma unroll
-                for (int j = 0; j < MT; ++j) {
+                    for (int i = 0; i < NT; ++i) a[d][i][c] = i32x4{};
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) b[d][i][c] = i32x4{};
+                }
+            }
+            // The wave's own place, whose accesses stay in order: no barrier.
+#pragma unroll
+            for (int i = 0; i < NT + MT; ++i)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    *reinterpret_cast<i32x4 *>(c == 0 ? put + i * 2048 : mine + i * 2048 + 1024 + ((put - mine) ^ 64)) =
+                        i < NT ? a[d][i][c] : b[d][i - NT][c];
+            const auto operand = [&](int i) {
+                const i32x4 lo = *reinterpret_cast<const i32x4 *>(get + i * 2048);
+                const i32x4 hi = *reinterpret_cast<const i32x4 *>(mine + i * 2048 + ((get - mine) ^ 64));
+                return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            };
+            const unsigned wa = sa[d] >> sh & 255;
+            i32x8 av[NT];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) av[i] = operand(i);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                const i32x8 bv = operand(NT + j);
+                const unsigned wb = sb[d][j] >> sh & 255;
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
                     if constexpr (kWide) {
 #pragma unroll
-                        for (int t = 0; t < 4; ++t)
+                        for (int q = 0; q < 4; ++q)
                             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                widened(a[d][i], t, sa[d] << 23), widened(b[d][j], t, sb[d][j] << 23), acc[i][j], 0, 0, 0);
+                                widened(av[i], q, wa << 23), widened(bv, q, wb << 23), acc[i][j], 0, 0, 0);
                     } else {
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[d][i], b[d][j], acc[i][j], 0, 0,
-                                                                                    0, sa[d], 0, sb[d][j]);
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av[i], bv, acc[i][j], 0, 0, 0, wa,
+                                                                                    0, wb);
                     }
                 }
+            }
         }
-    }
+    };
+    int kb0 = wave;
+    for (; kb0 + (kDeep - 1) * waves < nkb; kb0 += kDeep * waves) blocks(kb0, std::integral_constant<int, kDeep>{});
+    const int left = kb0 < nkb ? (nkb - 1 - kb0) / waves + 1 : 0;
+    const auto rest = [&](auto self, auto n) {
+        if constexpr (n() < kDeep) {
+            if (left == n()) blocks(kb0, n);
+            else self(self, std::integral_constant<int, n() + 1>{});
+        }
+    };
+    rest(rest, std::integral_constant<int, 1>{});
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -576,8 +624,10 @@ hipError_t launch_few(const ProductArgs &p, bool wide) {
     };
     using One = std::integral_constant<int, 1>;
     using Two = std::integral_constant<int, 2>;
+    using Four = std::integral_constant<int, 4>;
     if (p.M <= 16) return wide ? run(Two{}, One{}) : run(One{}, One{});
-    return wide ? run(Two{}, Two{}) : run(One{}, Two{});
+    if (p.M <= 32) return wide ? run(Two{}, Two{}) : run(One{}, Two{});
+    return wide ? run(Two{}, Four{}) : run(One{}, Four{});
 }
 
 }  // namespace

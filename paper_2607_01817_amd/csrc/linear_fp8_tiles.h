@@ -39,11 +39,12 @@ inline constexpr Fp8TileCost kFp8WideTiles[] = {
     {64, 64, 1, 2, 0.40, 0.37, 2.2},   {192, 192, 1, 1, 1.95, 1.79, 3.5}};
 
 // Up to so many rows the kernel for few rows runs (64 rows by N = K = 5120 take
-// 17.6 us on it and 15.3 on tiles; by N = 640, 16.1 and 15.3).
-inline constexpr int64_t kFp8Rows = 32;
+// 9.8 us on it and 12.2 on tiles; by 1920 x 5120 7.5 and 12.0; by 640 x 640 3.3
+// and 5.3).
+inline constexpr int64_t kFp8Rows = 64;
 // Its workgroups take 32 columns instead of 16 where those of 16 do not fit
-// the CUs at once (1 x 5120 x 5120: 7.6 us against 8.9; 1 x 640 x 5120: 7.4
-// against 5.2).
+// the CUs at once (1 x 5120 x 5120: 5.2 us against 7.0; 64 rows: 9.8 against 14.9;
+// 1 x 1920 x 5120: 5.1 against 4.2).
 inline bool fp8_rows_wide(int64_t N, int64_t n_cu) { return N > 16 * n_cu; }
 
 // The tile with the shortest estimated time: whole rounds of workgroups, then

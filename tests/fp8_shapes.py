@@ -18,11 +18,11 @@ SHAPES = [
     ("bf16", 2, True, 10809, 1288, 272),
     ("bf16", 3, False, 145, 10888, 656),
     ("bf16", 3, True, 12439, 600, 80),
-    ("bf16", 4, False, 35, 72, 656),
+    ("bf16", 4, False, 67, 72, 656),
     ("bf16", 4, True, 265, 10952, 272),
-    ("bf16", 5, False, 35, 16, 272),
+    ("bf16", 5, False, 67, 16, 272),
     ("bf16", 5, True, 521, 7184, 80),
-    ("bf16", 6, False, 35, 72, 2064),
+    ("bf16", 6, False, 67, 72, 2064),
     ("bf16", 6, False, 1561, 520, 4240),
     ("bf16", 7, False, 11748, 520, 80),
     ("bf16", 7, False, 1561, 5000, 1040),
@@ -35,9 +35,9 @@ SHAPES = [
     ("fp32", 1, False, 145, 10888, 656),
     ("fp32", 1, True, 10231, 848, 80),
     ("fp32", 1, False, 3001, 1000, 1936),
-    ("fp32", 2, False, 35, 16, 80),
+    ("fp32", 2, False, 67, 16, 80),
     ("fp32", 2, True, 10889, 264, 272),
-    ("fp32", 3, False, 35, 16, 656),
+    ("fp32", 3, False, 67, 16, 656),
     ("fp32", 3, False, 261, 1928, 2064),
     ("fp32", 4, False, 1561, 5000, 1040),
     ("fp32", 4, True, 1037, 10952, 80),

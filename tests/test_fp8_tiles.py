@@ -51,7 +51,7 @@ def test_shapes_take_every_tile(tiles):
 
 
 def test_few_rows_take_their_kernel(tiles):
-    rows = [(1, 8), (16, 4096), (17, 4096), (32, 4104), (33, 8)]
+    rows = [(1, 8), (16, 4096), (17, 4096), (64, 4104), (65, 8)]
     got = [t[4] for t in tiles([(M, N, 640, 0, 256) for M, N in rows])]
     assert got == [1, 1, 1, 2, 0]
 

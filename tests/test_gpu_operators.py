@@ -274,7 +274,7 @@ def test_linear_fp8_on_every_tile(hcms, out, tile, more, M, N, K):
     _product(hcms, M, N, K, BF16 if out == "bf16" else FP32)
 
 
-@pytest.mark.parametrize("M", [1, 15, 16, 17, 32, 33])
+@pytest.mark.parametrize("M", [1, 15, 16, 17, 32, 33, 64, 65])
 @pytest.mark.parametrize("N,K", [(24, 16), (520, 656), (4104, 1040), (4152, 5120), (72, 9104)])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_linear_fp8_of_few_rows(hcms, M, N, K, dtype):
