@@ -97,12 +97,23 @@ __device__ inline bf16x8 widened(const i32x8 &v, int t, int s) {
 // staged row r sits at position c ^ (r / 4 % 4).  Column n of Y lies in part
 // n / np (np is a multiple of 8, so no chunk crosses parts).  Of KG groups
 // of waves group `grp` stores every KG-th tile.
-template <typename T, typename C>
+// FULL: the wave's rows and columns all lie inside of Y, and no store is skipped.
+template <typename T, typename C, bool FULL>
 __device__ inline void store_tile(f32x16 (&acc)[C::NT][C::MT], char *stage, T *y, int np, int mb, int nb, int M,
                                   int N, int lane, int grp) {
     constexpr int SEG = sizeof(T) == 2 ? 1 : 2;          // segments per 32 columns
     constexpr int E = 16 / static_cast<int>(sizeof(T));  // elements per chunk
     const int li = lane & 31, g = lane >> 5;
+    // A segment's stores wait for its reads from LDS, so they stand behind the
+    // next segment's writes and reads.
+    u32x4 o[2];
+    T *to = nullptr;
+    int row = 0, n = 0;
+    const auto store = [&]() {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            if (FULL || (row + q * 16 < M && n < N)) *reinterpret_cast<u32x4 *>(to + static_cast<int64_t>(q * 16) * np) = o[q];
+    };
 #pragma unroll
     for (int mt = 0; mt < C::MT; ++mt) {
 #pragma unroll
@@ -120,22 +131,22 @@ __device__ inline void store_tile(f32x16 (&acc)[C::NT][C::MT], char *stage, T *y
                     *reinterpret_cast<f32x4 *>(stage + li * 64 + (((i * 2 + g) ^ ((li >> 2) & 3)) << 4)) = v;
             }
             const int ch = lane & 3;
-            const int n = nb + sg * (32 / SEG) + ch * E;
+            u32x4 next[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int r = q * 16 + (lane >> 2);
+                next[q] = *reinterpret_cast<const u32x4 *>(stage + r * 64 + ((ch ^ ((r >> 2) & 3)) << 4));
+            }
+            if (to) store();
+            n = nb + sg * (32 / SEG) + ch * E;
+            row = mb + mt * 32 + (lane >> 2);
             const int part = n / np;
-            T *col = y + static_cast<int64_t>(part) * M * np + (n - part * np);
-            u32x4 o[2];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int row = q * 16 + (lane >> 2);
-                o[q] = *reinterpret_cast<const u32x4 *>(stage + row * 64 + ((ch ^ ((row >> 2) & 3)) << 4));
-            }
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int mm = mb + mt * 32 + q * 16 + (lane >> 2);
-                if (mm < M && n < N) *reinterpret_cast<u32x4 *>(col + static_cast<int64_t>(mm) * np) = o[q];
-            }
+            to = y + static_cast<int64_t>(part) * M * np + (n - part * np) + static_cast<int64_t>(row) * np;
+            o[0] = next[0];
+            o[1] = next[1];
         }
     }
+    store();
 }
 
 template <typename T, typename C>
@@ -360,6 +371,9 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
             }
         __builtin_amdgcn_sched_barrier(0);
     };
+    constexpr int kStores = NT * MT * (sizeof(T) == 2 ? 2 : 4);   // of a wave's whole tile
+    static_assert((ST - 2) * LPW + kStores < 64, "counted by vmcnt");
+    bool behind = false;   // kStores stores were issued behind the tile before
     int buf = 0, prev = ST - 1;
     for (int r = 0; r < n_mine; ++r) {
 #pragma unroll
@@ -378,7 +392,11 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
             advance();
             // The second k-step's operands are in registers: past this barrier
             // the stage's buffer is free and the next stage is in LDS.
-            wait_vm<(ST - 2) * LPW>();
+            // With three buffers and more that stage's loads are older than the
+            // stores of the tile before, which may then go on (vector memory ends in
+            // the order of issue); with two, half of them were issued just now.
+            if (ST > 2 && s == 0 && behind) wait_vm<(ST - 2) * LPW + (ST > 2 ? kStores : 0)>();
+            else wait_vm<(ST - 2) * LPW>();
             __syncthreads();
             const int next = buf + 1 == ST ? 0 : buf + 1;
             phase(1, 0, next, 0, kHalf, buf);
@@ -419,8 +437,11 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
         if constexpr (KG == 1) asm volatile("" : "+s"(M), "+s"(N), "+s"(np));
         int m0, n0;
         origin(r, m0, n0);
-        store_tile<T, C>(acc, lds + (KG == 1 ? ST * C::STAGE_B : 0) + wave_all * C::OUT_B, y, np,
-                         m0 + wm * MT * 32, n0 + wn * NT * 32, M, N, lane, grp);
+        const int mb = m0 + wm * MT * 32, nb = n0 + wn * NT * 32;
+        char *const out = lds + (KG == 1 ? ST * C::STAGE_B : 0) + wave_all * C::OUT_B;
+        behind = KG == 1 && mb + MT * 32 <= M && nb + NT * 32 <= N;
+        if (behind) store_tile<T, C, true>(acc, out, y, np, mb, nb, M, N, lane, grp);
+        else store_tile<T, C, false>(acc, out, y, np, mb, nb, M, N, lane, grp);
     }
     wait_vm<0>();   // no load into LDS is pending when the workgroup ends
 }
