@@ -25,8 +25,8 @@
 //
 // What bounds it.  Large products: the power limit (the matrix cores alone take
 // 8-bit operands at 3200-3500 TFLOP/s for a short while) and what is not MFMAs:
-// 56160 x 1920 x 5120 runs at 2280 TFLOP/s (484 us) with the MFMAs busy 57 % of the
-// SIMDs' cycles at 1.86 GHz, 3.4 us of each tile's 44 its start and epilogue; 8192^3
+// 56160 x 1920 x 5120 runs at 2290 TFLOP/s (482 us) with the MFMAs busy 57 % of the
+// SIMDs' cycles at 1.86 GHz, 2.5 us of each tile's 41 its start and epilogue; 8192^3
 // at 2700.  Each stage also moves its operands through LDS, WN times for X and WM
 // times for W, at 128 bytes per clock: 0.95 us per stage of a 256 x 256 tile against
 // 0.85 of MFMAs, which is why the waves' rectangles are large.  Few tiles: the
