@@ -334,8 +334,13 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
     // waves' reads fill the LDS queue and the matrix cores wait behind them),
     // and the loads l0 .. l1 - 1 into `into`.
     auto phase = [&](int set, int ks, int from, int l0, int l1, int into) {
-        constexpr int kOps = NT + MT, kOver = (NT * MT * (kWide ? 4 : 1) * 3 + 3) / 4;
-        constexpr int kMf = NT * MT * (kWide ? 4 : 1);
+        // In the order in which the next MFMAs take them: W's first, X's, W's others.
+        // Over 3/4 of the MFMAs ahead of the barrier, over all of them behind it (W's
+        // first with W's others: 1920 x 5120 x 7808 75.8 us, so 72.7), and over half of
+        // those of widened operands, which take longer (3/4: 3001 x 1000 x 1936 19.1
+        // us, half 18.6).
+        constexpr int kOps = NT + MT, kMf = NT * MT * (kWide ? 4 : 1);
+        const int kOver = kWide ? (kMf + 1) / 2 : ks == 0 ? kMf : (kMf * 3 + 3) / 4;
         bf16x8 aw[NT], bw[MT];
 #pragma unroll
         for (int i = 0; i < kMf; ++i) {
@@ -353,7 +358,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
             }
 #pragma unroll
             for (int o = 0; o < kOps; ++o)
-                if (o * kOver / kOps == i) read_op(o, set ^ 1, ks, from);
+                if (o * kOver / kOps == i) read_op(o == 0 ? 0 : o <= MT ? NT + o - 1 : o - MT, set ^ 1, ks, from);
             if (i == kMf - 1 && ks == 0) read_scales(from);
 #pragma unroll
             for (int l = 0; l < LPW; ++l)
