@@ -146,7 +146,7 @@ def build(verbose: bool = False) -> str:
     os.replace(tmp, LIB)
     tmp = TORCH_LIB + ".tmp"
     cmd = ["g++", "-shared", "-fPIC", "-o", tmp, torch_obj, "-L", torch_libs, "-ltorch", "-ltorch_cpu",
-           "-ltorch_python", "-lc10", "-lc10_hip", "-L", PKG, "-l:libhcms.so", "-Wl,-rpath,$ORIGIN"]
+           "-ltorch_hip", "-ltorch_python", "-lc10", "-lc10_hip", "-L", PKG, "-l:libhcms.so", "-Wl,-rpath,$ORIGIN"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)

@@ -46,41 +46,41 @@ def _ops():
     return _hcms_torch
 
 
-def _on_stream(fn):
-    """With ``stream``, the call under it as the current stream."""
-    @functools.wraps(fn)
-    def call(*args, stream=None, **kwargs):
-        if stream is None:
-            return fn(*args, **kwargs)
-        with torch.cuda.stream(stream):
-            return fn(*args, **kwargs)
-    return call
+def _under(stream, fn, *args):
+    """fn(*args) with ``stream`` as the current stream."""
+    with torch.cuda.stream(stream):
+        return fn(*args)
 
 
-@_on_stream
 def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6,
              residual: torch.Tensor | None = None, out: torch.Tensor | None = None,
-             h_out: torch.Tensor | None = None):
+             h_out: torch.Tensor | None = None, *, stream=None):
     """Root-mean-square norm of rows: ``y = h / sqrt(mean(h^2) + eps) * weight``
     with ``h = x + residual``.  Returns y, or (y, h) with a residual, where h is
     the residual stream's next value.  x and residual [M][D] may have any row
     stride (a slice of a projection's output, for a norm of queries)."""
+    if stream is not None:
+        return _under(stream, rms_norm, x, weight, eps, residual, out, h_out)
     return _ops().rms_norm(x, weight, eps, residual, out, h_out)
 
 
-@_on_stream
 def rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6,
-                 residual: torch.Tensor | None = None, h_out: torch.Tensor | None = None):
+                 residual: torch.Tensor | None = None, h_out: torch.Tensor | None = None, *,
+                 stream=None):
     """:func:`rms_norm` with y in 8 bits, as :func:`linear_fp8` reads it: returns
     (q, scale), or (q, scale, h) with a residual.  D must be a multiple of 16."""
+    if stream is not None:
+        return _under(stream, rms_norm_fp8, x, weight, eps, residual, h_out)
     return _ops().rms_norm_fp8(x, weight, eps, residual, h_out)
 
 
-@_on_stream
 def rms_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6,
-                      residual: torch.Tensor | None = None, dh: torch.Tensor | None = None):
+                      residual: torch.Tensor | None = None, dh: torch.Tensor | None = None, *,
+                      stream=None):
     """Gradients (dx, dw) of :func:`rms_norm` from its inputs: dx is the gradient
     of x and of the residual alike, dh the gradient that reaches h from elsewhere."""
+    if stream is not None:
+        return _under(stream, rms_norm_backward, dy, x, weight, eps, residual, dh)
     return _ops().rms_norm_backward(dy, x, weight, eps, residual, dh)
 
 
@@ -94,24 +94,26 @@ class RmsNorm:
         return _ops().rms_norm_train(x, weight, eps, residual)
 
 
-@_on_stream
-def quantize_fp8(x: torch.Tensor, block: int | None = 1, t_block: int | None = None):
+def quantize_fp8(x: torch.Tensor, block: int | None = 1, t_block: int | None = None, *, stream=None):
     """x [M][K] in 8 bits, as operands of :func:`linear_fp8`: (q, scale) with one
     scale per row and 128 columns (``block`` 1, an activation) or per 128 x 128
     (``block`` 128, a weight).  ``t_block`` asks for the transpose too (or, with
     ``block`` None, alone): (q, scale, t, t_scale) with t [K][M rounded up to 16],
     padded with zeros, and its scales along M."""
+    if stream is not None:
+        return _under(stream, quantize_fp8, x, block, t_block)
     return _ops().quantize_fp8(x, block, t_block)
 
 
-@_on_stream
 def linear_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
                dtype: torch.dtype = torch.bfloat16, parts: int = 1,
-               out: torch.Tensor | None = None) -> torch.Tensor:
+               out: torch.Tensor | None = None, *, stream=None) -> torch.Tensor:
     """8-bit projection: x [M][K] (scales per row and 128 k) times w [N][K] (scales
     per 128 x 128), accumulated in fp32, as ``dtype`` [M][N].  With ``parts`` the
     columns come as so many tensors, [parts][M][N / parts]: the queries, keys and
     values of a QKV projection.  K must be a multiple of 16 and N / parts of 8."""
+    if stream is not None:
+        return _under(stream, linear_fp8, x, x_scale, w, w_scale, dtype, parts, out)
     return _ops().linear_fp8(x, x_scale, w, w_scale, dtype, parts, out)
 
 
@@ -142,10 +144,12 @@ def rope_frequencies(pairs: int, base: float = 10000.0, scaling: str = "none", f
     return list(buf), mag.value
 
 
-@_on_stream
-def rope_table_freqs(grid, axis_pairs, freqs, magnitude: float = 1.0, device="cuda") -> torch.Tensor:
+def rope_table_freqs(grid, axis_pairs, freqs, magnitude: float = 1.0, device="cuda", *,
+                     stream=None) -> torch.Tensor:
     """The rotation table (see :func:`rope_table`) of given frequencies, one per
     pair, with every entry times ``magnitude``: float32 [entries][2]."""
+    if stream is not None:
+        return _under(stream, rope_table_freqs, grid, axis_pairs, freqs, magnitude, device)
     n = _table_rows(grid, axis_pairs)
     g, na = _ints(grid)
     p, _ = _ints(axis_pairs)
@@ -164,10 +168,9 @@ def _half(layout: str) -> bool:
     return _HALF[layout]
 
 
-@_on_stream
 def rope(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, grid, axis_pairs,
          positions: torch.Tensor | None = None, layout: str = "interleaved", inverse: bool = False,
-         out=None):
+         out=None, *, stream=None):
     """Rotary positions of queries q [S][H][d] and keys k [S][Hk][d] (or None), any
     strides of tokens and heads: the first 2 sum(axis_pairs) elements of each head
     turn by ``table`` (:func:`rope_table` or :func:`rope_table_freqs` of the same
@@ -176,6 +179,8 @@ def rope(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, grid, axi
     token t sits at place t of the row-major grid.  A position outside the grid
     gives NaN.  ``inverse`` turns back (the gradient's rotation).  ``out``: (q, k)
     to write to, which may be the inputs themselves.  Returns (q, k), or q."""
+    if stream is not None:
+        return _under(stream, rope, q, k, table, grid, axis_pairs, positions, layout, inverse, out)
     return _ops().rope(q, k, table, grid, axis_pairs, positions, _half(layout), bool(inverse), out)
 
 
