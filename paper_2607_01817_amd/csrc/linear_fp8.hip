@@ -456,7 +456,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
 // look-ups, and straight from memory into the MFMA's operands (lane li holds row
 // li) every load is of that kind: 1 x 5120 x 5120 7.5 us, 16 rows 9.2, 32 rows 12.0.
 // So 8 lanes load a row's block of 128, and the operands pass through LDS, a place
-// of each wave's own: 5.2 us (5.0 TB/s; 7.6 with W from memory), 5.3 and 7.4; 64
+// of each wave's own: 4.8 us (5.4 TB/s; 7.4 with W from memory), 5.2 and 7.1; 64
 // rows 9.8, on 64 x 64 tiles, whose stages wait for each other, 12.2.  A workgroup
 // takes 16 NT columns of Y and all rows (16 MT hold them), its waves the blocks of
 // k in turn, and the waves' sums are added through LDS in the order of the waves.
@@ -493,6 +493,9 @@ __global__ __launch_bounds__(512) void linear_fp8_rows_kernel(
     char *const put = mine + row * 128 + (chunk ^ ((row >> 1) << 4));          // of row 8 + row: place ^ 4
     const char *const get = mine + li * 128 + ((g ^ (li >> 1)) << 4);          // of chunk 4 + g: place ^ 4
     f32x4 acc[NT][MT]{};
+    // Else X's last 8 staged rows are nobody's, and are neither loaded nor staged (1 x
+    // 5120 x 5120 5.2 us with them).
+    const bool upper = M > 16 * MT - 8;
     // D blocks from kb0 on, without a branch around the loads, which would wait for
     // them there: rows past the ends read the last row (their sums are not stored),
     // chunks past K the row's last one, and are made zeros before they are used.
@@ -508,7 +511,8 @@ __global__ __launch_bounds__(512) void linear_fp8_rows_kernel(
 #pragma unroll
                 for (int i = 0; i < NT; ++i) a[d][i][c] = *reinterpret_cast<const i32x4 *>(wr[i][c] + at);
 #pragma unroll
-                for (int i = 0; i < MT; ++i) b[d][i][c] = *reinterpret_cast<const i32x4 *>(xr[i][c] + at);
+                for (int i = 0; i < MT; ++i)
+                    if (c == 0 || i < MT - 1 || upper) b[d][i][c] = *reinterpret_cast<const i32x4 *>(xr[i][c] + at);
             }
             const int64_t grp = kb >> 2;
             sa[d] = ws[grp * n_blocks + n0 / 128];
@@ -532,8 +536,10 @@ __global__ __launch_bounds__(512) void linear_fp8_rows_kernel(
             for (int i = 0; i < NT + MT; ++i)
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
-                    *reinterpret_cast<i32x4 *>(c == 0 ? put + i * 2048 : mine + i * 2048 + 1024 + ((put - mine) ^ 64)) =
-                        i < NT ? a[d][i][c] : b[d][i - NT][c];
+                    if (c == 0 || i < NT + MT - 1 || upper) {
+                        char *const to = c == 0 ? put + i * 2048 : mine + i * 2048 + 1024 + ((put - mine) ^ 64);
+                        *reinterpret_cast<i32x4 *>(to) = i < NT ? a[d][i][c] : b[d][i - NT][c];
+                    }
             const auto operand = [&](int i) {
                 const i32x4 lo = *reinterpret_cast<const i32x4 *>(get + i * 2048);
                 const i32x4 hi = *reinterpret_cast<const i32x4 *>(mine + i * 2048 + ((get - mine) ^ 64));

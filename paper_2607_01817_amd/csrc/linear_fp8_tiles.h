@@ -43,8 +43,8 @@ inline constexpr Fp8TileCost kFp8WideTiles[] = {
 // and 5.3).
 inline constexpr int64_t kFp8Rows = 64;
 // Its workgroups take 32 columns instead of 16 where those of 16 do not fit
-// the CUs at once (1 x 5120 x 5120: 5.2 us against 7.0; 64 rows: 9.8 against 14.9;
-// 1 x 1920 x 5120: 5.1 against 4.2).
+// the CUs at once (1 x 5120 x 5120: 4.8 us against 6.5; 64 rows: 9.8 against 14.8;
+// 1 x 1920 x 5120: 4.7 against 3.9).
 inline bool fp8_rows_wide(int64_t N, int64_t n_cu) { return N > 16 * n_cu; }
 
 // The tile with the shortest estimated time: whole rounds of workgroups, then

@@ -1,9 +1,10 @@
 // Tensor side of the operators beside the chunk loop: checks of tensors,
 // outputs and workspaces on the current stream, and autograd, in C++ so that a
 // small call costs its launch and little else.  Host time of a call, with the
-// same checks in Python and here: a norm 8.9 and 4.8 us (4.0 of them
-// its launch), a rotation 12.2 and 5.0; a forward and backward through autograd (39 of a Python function that
-// does nothing): norm 106 and 43, rotation 111 and 33, projection 142 and 70.
+// same checks in Python and here: a norm 8.9 and 4.8 us (4.0 of them its launch), a
+// rotation 12.2 and 5.0; a forward and backward through autograd (39 of a Python
+// function that does nothing): norm 106 and 43, rotation 111 and 33, projection 142
+// and 70.
 // Every call runs through the C ABI (hcms.h), whose refusals become HcmsError.
 #include <ATen/hip/EmptyTensor.h>
 #include <torch/extension.h>
