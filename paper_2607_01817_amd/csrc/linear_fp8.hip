@@ -25,7 +25,7 @@
 //
 // What bounds it.  Large products: the power limit (the matrix cores alone take
 // 8-bit operands at 3200-3500 TFLOP/s for a short while) and what is not MFMAs:
-// 56160 x 1920 x 5120 runs at 2290 TFLOP/s (482 us) with the MFMAs busy 57 % of the
+// 56160 x 1920 x 5120 runs at 2210-2290 TFLOP/s (482-500 us) with the MFMAs busy 57 % of the
 // SIMDs' cycles at 1.86 GHz, 2.5 us of each tile's 41 its start and epilogue; 8192^3
 // at 2700.  Each stage also moves its operands through LDS, WN times for X and WM
 // times for W, at 128 bytes per clock: 0.95 us per stage of a 256 x 256 tile against
@@ -334,13 +334,16 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
     // waves' reads fill the LDS queue and the matrix cores wait behind them),
     // and the loads l0 .. l1 - 1 into `into`.
     auto phase = [&](int set, int ks, int from, int l0, int l1, int into) {
-        // In the order in which the next MFMAs take them: W's first, X's, W's others.
-        // Over 3/4 of the MFMAs ahead of the barrier, over all of them behind it (W's
-        // first with W's others: 1920 x 5120 x 7808 75.8 us, so 72.7), and over half of
-        // those of widened operands, which take longer (3/4: 3001 x 1000 x 1936 19.1
-        // us, half 18.6).
+        // In the order in which the next MFMAs take them: W's first, X's, W's others,
+        // over 3/4 of the MFMAs ahead of the barrier and over all of them behind it,
+        // against W's first and 3/4: 1920 x 5120 x 7808 on 192 x 256 72 us against 75,
+        // on 64 x 128 116 against 120, but with three of W's and more in a wave that
+        // has its SIMD alone 488 against 483 (56160 x 1920 x 5120 on 192 x 192) and 76
+        // against 73 (7800 x 5120 x 1920 on 128 x 256).  Over half of the MFMAs of
+        // widened operands, which take longer (3/4: 3001 x 1000 x 1936 19.1 us, half 18.6).
         constexpr int kOps = NT + MT, kMf = NT * MT * (kWide ? 4 : 1);
-        const int kOver = kWide ? (kMf + 1) / 2 : ks == 0 ? kMf : (kMf * 3 + 3) / 4;
+        constexpr bool kByUse = kWide || C::WAVES > 1 || NT < 3;
+        const int kOver = kWide ? (kMf + 1) / 2 : kByUse && ks == 0 ? kMf : (kMf * 3 + 3) / 4;
         bf16x8 aw[NT], bw[MT];
 #pragma unroll
         for (int i = 0; i < kMf; ++i) {
@@ -358,7 +361,8 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
             }
 #pragma unroll
             for (int o = 0; o < kOps; ++o)
-                if (o * kOver / kOps == i) read_op(o == 0 ? 0 : o <= MT ? NT + o - 1 : o - MT, set ^ 1, ks, from);
+                if (o * kOver / kOps == i)
+                    read_op(!kByUse || o == 0 ? o : o <= MT ? NT + o - 1 : o - MT, set ^ 1, ks, from);
             if (i == kMf - 1 && ks == 0) read_scales(from);
 #pragma unroll
             for (int l = 0; l < LPW; ++l)
