@@ -75,6 +75,20 @@ __device__ inline float wave_sum(float v) {
             __builtin_bit_cast(float, __builtin_amdgcn_readlane(i, 48)));
 }
 
+// Sum over groups of L lanes (16 or 32), in the order of wave_sum.
+template <int L>
+__device__ inline float lanes_sum(float v) {
+#define HCMS_ROR(n) \
+    v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + n, 0xF, 0xF, true))
+    HCMS_ROR(8);
+    HCMS_ROR(4);
+    HCMS_ROR(2);
+    HCMS_ROR(1);
+#undef HCMS_ROR
+    if constexpr (L == 32) v += __shfl_xor(v, 16);
+    return v;
+}
+
 // 8 consecutive elements from any element's address (the hardware takes
 // 16-byte accesses at every alignment of global memory) as fp32, and back,
 // rounded to nearest even.

@@ -132,6 +132,34 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(
     }
 }
 
+// Narrow rows (a norm of head vectors), one chunk per lane: L lanes (16 or 32) take a
+// row, a workgroup 256 / L of them; with a wave per row 280800 x 128 in bf16 takes 61.6
+// us, so 22.3 (6.4 TB/s), 56160 x 256 15.1 and 10.6 (x 512 17.6 and, on 64 lanes,
+// 18.1).  The sums are those of the kernel above, in its order, whose lanes past the
+// row add zeros.
+template <typename T, typename W, int L, bool RES>
+__global__ __launch_bounds__(256) void rms_norm_narrow_kernel(
+    const T *__restrict__ x, const T *__restrict__ r, const W *__restrict__ w, T *__restrict__ y,
+    T *__restrict__ h_out, int64_t M, int D, int64_t ldx, int64_t ldr, float eps) {
+    const int t = threadIdx.x & (L - 1);
+    const int64_t row = block_index() * (256 / L) + threadIdx.x / L, m = min(row, M - 1);
+    const Chunk c = chunk_at(t, D);
+    const auto xv = load_raw(x + m * ldx + c.e0);
+    decltype(load_raw(x)) rv;
+    if constexpr (RES) rv = load_raw(r + m * ldr + c.e0);
+    const f32x8 wv = widen(load_raw(w + c.e0));
+    f32x8 h = widen(xv);
+    if constexpr (RES) h += widen(rv);
+    float sum = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += i >= c.dup ? h[i] * h[i] : 0.0f;
+    sum = lanes_sum<L>(sum);
+    const float rstd = 1.0f / __builtin_sqrtf(sum / static_cast<float>(D) + eps);
+    if (row >= M || t * 8 >= D) return;
+    if constexpr (RES) store_8(h_out + m * D + c.e0, h);
+    store_8(y + m * D + c.e0, h * rstd * wv);
+}
+
 // Backward: h = x + r again, unrounded as in the forward (from the stored h,
 // rounded, dw would be 1.4 times as far from the exact sum in bf16; reading x
 // and r costs one tensor more), n = h rstd, g = dy w,
@@ -328,6 +356,21 @@ hipError_t run_norm_of(const NormArgs &a, hipStream_t s) {
         static_cast<T *>(a.h), a.M, a.D, a.ldx, a.ldr, a.eps);
     return hipGetLastError();
 }
+template <typename T, typename W, int L>
+hipError_t run_narrow(const NormArgs &a, hipStream_t s) {
+    if (a.M < 1 || a.D > 8 * L) return hipErrorInvalidValue;
+    const auto kernel = a.r ? rms_norm_narrow_kernel<T, W, L, true> : rms_norm_narrow_kernel<T, W, L, false>;
+    kernel<<<grid_of((a.M + 256 / L - 1) / (256 / L)), 256, 0, s>>>(
+        static_cast<const T *>(a.x), static_cast<const T *>(a.r), static_cast<const W *>(a.w), static_cast<T *>(a.y),
+        static_cast<T *>(a.h), a.M, a.D, a.ldx, a.ldr, a.eps);
+    return hipGetLastError();
+}
+template <typename T, typename W>
+hipError_t narrow_typed(const NormArgs &a, hipStream_t s) {
+    if (a.D <= 128) return run_narrow<T, W, 16>(a, s);
+    return run_narrow<T, W, 32>(a, s);
+}
+
 // Tensors that together are twice what the caches hold (256 MiB) are read and
 // written past them (bf16 with a residual: 56160 x 5120 396 us without, 385 with,
 // in 8 bits 340 and 329; 15000 x 16384 349 and 318; below, a reader finds them there).
@@ -344,9 +387,10 @@ hipError_t run_norm(const NormArgs &a, hipStream_t s) {
 // One chunk per lane, two for many long rows and for rows that 1024 lanes do
 // not hold.  With one and with two, bf16 with a residual, 56160 rows: D = 5120
 // 399 and 396 us (5.8 TB/s), in 8 bits 391 and 340; D = 2560 200 and 198, in 8
-// bits 179 and 173; D = 1280 102 and 102; D = 128 15.8 and 18.0.
+// bits 179 and 173; D = 1280 102 and 102.
 template <typename T, bool F8>
 hipError_t norm_typed(const NormArgs &a, hipStream_t s) {
+    if (!F8 && a.D <= 256) return a.w_f32 ? narrow_typed<T, float>(a, s) : narrow_typed<T, __bf16>(a, s);
     if ((a.M >= 1024 && a.D > 2048) || a.D > 8192) return run_norm<T, F8, 2>(a, s);
     return run_norm<T, F8, 1>(a, s);
 }

@@ -50,7 +50,7 @@ def _within(got, want, bound, what):
 # ---------------------------------------------------------------------------
 # Norm
 # ---------------------------------------------------------------------------
-NORM_SHAPES = [(1, 8), (1, 5120), (3, 13), (5, 129), (9, 512), (7, 640), (2, 2048), (2, 2049), (3, 6151),
+NORM_SHAPES = [(1, 8), (1, 5120), (3, 13), (33, 64), (17, 128), (1037, 121), (5, 129), (9, 256), (1029, 250), (5, 257), (9, 512), (7, 640), (2, 2048), (2, 2049), (3, 6151),
                (2, 8193), (2, 16384), (1100, 513), (1030, 2560), (1025, 2561), (1030, 5120), (1025, 5117)]
 
 
