@@ -25,23 +25,26 @@ __device__ inline Chunk chunk_at(int c, int D) {
     return {e0, e - e0};
 }
 
-// The lane's place in a workgroup that takes one row, or with ROWS one for each
-// of its four waves.
-template <bool ROWS>
+// The lane's place in a workgroup that takes one row (L = 0), or of 256 threads
+// that take one for each L of them.
+template <int L>
 struct Lane {
-    static __device__ int t() { return ROWS ? threadIdx.x & 63 : threadIdx.x; }
-    static __device__ int lanes() { return ROWS ? 64 : blockDim.x; }
-    static __device__ int row() { return ROWS ? threadIdx.x >> 6 : 0; }
-    static __device__ int rows() { return ROWS ? 4 : 1; }
+    static __device__ int t() { return L ? threadIdx.x & (L - 1) : threadIdx.x; }
+    static __device__ int lanes() { return L ? L : blockDim.x; }
+    static __device__ int row() { return L ? threadIdx.x / (L ? L : 1) : 0; }
+    static constexpr int rows() { return L ? 256 / (L ? L : 1) : 1; }
 };
 
 // Sums of N values over the lanes of a row, in a fixed order; `red` holds N
 // floats per wave.
-template <bool ROWS, int N>
+template <int L, int N>
 __device__ inline void row_sums(float (&v)[N], float (*red)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
-    if constexpr (!ROWS) {
+    for (int i = 0; i < N; ++i) {
+        if constexpr (L == 16 || L == 32) v[i] = lanes_sum<L>(v[i]);
+        else v[i] = wave_sum(v[i]);
+    }
+    if constexpr (L == 0) {
         const int waves = blockDim.x >> 6;
         if (waves == 1) return;
         __syncthreads();   // the sums before have been read
@@ -97,7 +100,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[0] += i >= dup ? h[j][i] * h[j][i] : 0.0f;
     }
-    row_sums<false>(sum, red);
+    row_sums<0>(sum, red);
     const float rstd = 1.0f / __builtin_sqrtf(sum[0] / static_cast<float>(D) + eps);
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
@@ -171,14 +174,14 @@ __global__ __launch_bounds__(256) void rms_norm_narrow_kernel(
 // would not fit the registers, are read twice instead.  The shares go to partial
 // [gridDim.x][D] and are summed by sum_rows_kernel, so no atomics: the order is
 // fixed.  RES, DH: with the residual, with dh.  ONCE: past the caches.
-template <typename T, bool ROWS, int NC, int MAX, bool AHEAD, bool RES, bool DH, bool ONCE>
+template <typename T, int LANES, int NC, int MAX, bool AHEAD, bool RES, bool DH, bool ONCE>
 __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
     const T *__restrict__ dy, const T *__restrict__ x, const T *__restrict__ r, const T *__restrict__ dh,
     const void *__restrict__ w, bool w_f32, T *__restrict__ dx, float *__restrict__ partial, int64_t M, int D,
     int64_t ldx, int64_t ldr, float eps) {
     __shared__ float red[16][2];
-    __shared__ float share[ROWS ? 64 * NC * 8 : 1];
-    using P = Lane<ROWS>;
+    __shared__ float share[LANES ? LANES * NC * 8 : 1];
+    using P = Lane<LANES>;
     const int t = P::t(), L = P::lanes();
     f32x8 acc[NC];
     int e0[NC], dup[NC];
@@ -202,7 +205,7 @@ __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
     };
     float rstd, mean;
     const auto finish_sums = [&](float (&sums)[2]) {
-        row_sums<ROWS>(sums, red);
+        row_sums<LANES>(sums, red);
         rstd = 1.0f / __builtin_sqrtf(sums[0] / static_cast<float>(D) + eps);
         mean = sums[1] * rstd / static_cast<float>(D);
     };
@@ -284,21 +287,22 @@ __global__ __launch_bounds__(MAX) void rms_norm_backward_kernel(
                 }
         }
     }
-    if constexpr (ROWS) {
-        // The waves' shares, added in the order of the waves.
-        for (int k = 0; k < 4; ++k) {
+    if constexpr (LANES > 0) {
+        // The rows' shares, added in their order.
+        constexpr int last = P::rows() - 1;
+        for (int k = 0; k <= last; ++k) {
             if (P::row() == k)
 #pragma unroll
                 for (int j = 0; j < NC; ++j)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        float &s = share[(j * 8 + i) * 64 + t];
+                        float &s = share[(j * 8 + i) * LANES + t];
                         s = k == 0 ? acc[j][i] : s + acc[j][i];
-                        if (k == 3) acc[j][i] = s;
+                        if (k == last) acc[j][i] = s;
                     }
             __syncthreads();
         }
-        if (P::row() != 3) return;
+        if (P::row() != last) return;
     }
 #pragma unroll
     for (int j = 0; j < NC; ++j)
@@ -407,14 +411,14 @@ struct BackwardArgs {
     int P;
 };
 
-template <typename T, bool ROWS, int NC, int MAX, bool AHEAD, bool ONCE>
+template <typename T, int LANES, int NC, int MAX, bool AHEAD, bool ONCE>
 hipError_t run_backward_of(const BackwardArgs &a, hipStream_t s) {
-    const int threads = ROWS ? 256 : lanes_for(a.D, NC);
-    if (threads > MAX) return hipErrorInvalidValue;
-    const auto kernel = a.r ? (a.dh ? rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, true, true, ONCE>
-                                    : rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, true, false, ONCE>)
-                            : (a.dh ? rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, false, true, ONCE>
-                                    : rms_norm_backward_kernel<T, ROWS, NC, MAX, AHEAD, false, false, ONCE>);
+    const int threads = LANES ? 256 : lanes_for(a.D, NC);
+    if (threads > MAX || (LANES && a.D > LANES * NC * 8)) return hipErrorInvalidValue;
+    const auto kernel = a.r ? (a.dh ? rms_norm_backward_kernel<T, LANES, NC, MAX, AHEAD, true, true, ONCE>
+                                    : rms_norm_backward_kernel<T, LANES, NC, MAX, AHEAD, true, false, ONCE>)
+                            : (a.dh ? rms_norm_backward_kernel<T, LANES, NC, MAX, AHEAD, false, true, ONCE>
+                                    : rms_norm_backward_kernel<T, LANES, NC, MAX, AHEAD, false, false, ONCE>);
     kernel<<<a.P, threads, 0, s>>>(
         static_cast<const T *>(a.dy), static_cast<const T *>(a.x), static_cast<const T *>(a.r),
         static_cast<const T *>(a.dh), a.w, a.w_f32, static_cast<T *>(a.dx), a.partial, a.M, a.D, a.ldx, a.ldr,
@@ -425,32 +429,36 @@ hipError_t run_backward_of(const BackwardArgs &a, hipStream_t s) {
 // past the caches (bf16 with residual and dh: 7800 x 5120, 400 MB, 73 us without and
 // 65 with; 56160 x 5120 520 and 476; 30000 x 1280 72 and 63; 3000 x 5120, 154 MB, 27.0
 // and 27.5).  Rows that are read twice have to be kept.
-template <typename T, bool ROWS, int NC, int MAX, bool AHEAD>
+template <typename T, int LANES, int NC, int MAX, bool AHEAD>
 hipError_t run_backward(const BackwardArgs &a, hipStream_t s) {
     const int64_t bytes = a.M * a.D * static_cast<int64_t>(sizeof(T)) * (3 + (a.r != nullptr) + (a.dh != nullptr));
-    if (AHEAD && bytes > int64_t{256} << 20) return run_backward_of<T, ROWS, NC, MAX, AHEAD, AHEAD>(a, s);
-    return run_backward_of<T, ROWS, NC, MAX, AHEAD, false>(a, s);
+    if (AHEAD && bytes > int64_t{256} << 20) return run_backward_of<T, LANES, NC, MAX, AHEAD, AHEAD>(a, s);
+    return run_backward_of<T, LANES, NC, MAX, AHEAD, false>(a, s);
 }
 
 template <typename T>
 hipError_t backward_typed(const BackwardArgs &a, hipStream_t s) {
-    if (a.D <= 512) return run_backward<T, true, 1, 256, true>(a, s);
-    if (a.D <= 1024) return run_backward<T, true, 2, 256, true>(a, s);
-    if (a.D <= 8192) return run_backward<T, false, 2, 512, true>(a, s);
-    return run_backward<T, false, 2, 1024, false>(a, s);
+    if (a.D <= 128) return run_backward<T, 16, 1, 256, true>(a, s);
+    if (a.D <= 256) return run_backward<T, 32, 1, 256, true>(a, s);
+    if (a.D <= 512) return run_backward<T, 64, 1, 256, true>(a, s);
+    if (a.D <= 1024) return run_backward<T, 64, 2, 256, true>(a, s);
+    if (a.D <= 8192) return run_backward<T, 0, 2, 512, true>(a, s);
+    return run_backward<T, 0, 2, 1024, false>(a, s);
 }
 
 }  // namespace
 
 int rms_norm_max_width() { return 16384; }
 
-// Workgroups of the backward: up to D = 1024 four rows at once, then one; on
-// 256 CUs so many per CU as measured best (bf16 with residual and dh; 56160 rows: D =
-// 128 36 us with one, 28 with two, 24 with four, 22 with eight; D = 640 110, 77, 71,
-// 72; 30000 rows: D = 1280 130, 94, 70 with three, 63 with four; D = 2560 142, 124,
-// 134, 137; D = 3840 178, 202; 56160 x 5120 476 (6.0 TB/s), 524).
+// Workgroups of the backward: up to D = 128 sixteen rows at once, to 256 eight, to
+// 1024 four, then one (56160 x 128 with a wave per row 24.6 us, on 16 lanes 13.5;
+// 280800 x 128 98 and 38; 56160 x 256 26.0 and, on 32, 19.7); on 256 CUs so many per
+// CU as measured best (bf16 with residual and dh; 56160 rows: D = 640 110 with one, 77
+// with two, 71 with four, 72 with eight; 30000 rows: D = 1280 130, 94, 70 with three,
+// 63 with four; D = 2560 142, 124, 134, 137; D = 3840 178, 202; 56160 x 5120 476 (6.0
+// TB/s), 524).
 int rms_norm_partials(int64_t M, int D) {
-    const int64_t rows = D <= 1024 ? 4 : 1;
+    const int64_t rows = D <= 128 ? 16 : D <= 256 ? 8 : D <= 1024 ? 4 : 1;
     const int waves = lanes_for(D, 2) / 64;   // of a row past D = 1024
     const int64_t most = 256 * (D <= 1024 || waves <= 2 ? 4 : waves == 3 ? 2 : 1);
     const int64_t sets = (M + rows - 1) / rows;
