@@ -768,8 +768,10 @@ HCMS_API int hcms_linear_fp8(const void *x, const void *x_scale, const void *w, 
  *   base factor^(pairs / (pairs - 1)), so that the slowest pair is slowed by
  *   factor and the fastest not at all; HCMS_ROPE_YARN keeps pairs that turn at
  *   least beta_fast times over original_length, slows those that turn at most
- *   beta_slow times by factor and mixes linearly between, and gives the table
- *   the magnitude 0.1 ln(factor) + 1.  Host only.  Errors: NULL, SHAPE (pairs
+ *   beta_slow times by factor and mixes the two in between, linearly from the
+ *   last pair of the first kind (or pair 0) to the first one of the second (which
+ *   may lie past the last pair, up to 2 pairs - 1), and gives the table the
+ *   magnitude 0.1 ln(factor) + 1.  Host only.  Errors: NULL, SHAPE (pairs
  *   outside 1..256), ARG.
  * hcms_rope_table_freqs: hcms_rope_table with given frequencies (freqs: host,
  *   sum(axis_pairs) <= 256 doubles) and magnitude: entries magnitude (cos, sin).

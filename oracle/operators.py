@@ -108,11 +108,13 @@ def frequencies(pairs, base=10000.0, scaling="none", factor=1.0, original_length
         return (f if pairs == 1 else (base * factor ** (pairs / (pairs - 1))) ** (-i / pairs)), 1.0
     if scaling == "none":
         return f, 1.0
-    # index (not rounded) of a pair that turns `beta` times
-    at = [pairs * math.log(original_length / (beta * 2 * math.pi)) / math.log(base)
-          for beta in (beta_fast, beta_slow)]
-    lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), pairs - 1)
-    slow = np.array([min(max((k - lo) / max(hi - lo, 1e-3), 0.0), 1.0) for k in range(pairs)])
+    # Turns over the original length, of twice as many pairs as there are: the mixture
+    # starts at the last pair that turns beta_fast times and ends at the first one that
+    # turns no more than beta_slow times, past the pairs or not.
+    turns = original_length / (2 * math.pi) * base ** (-np.arange(2 * pairs) / pairs)
+    lo, hi = max(int((turns >= beta_fast).sum()) - 1, 0), min(int((turns > beta_slow).sum()), 2 * pairs - 1)
+    slow = np.interp(i, [lo, hi], [0.0, 1.0]) if hi > lo else np.ones(pairs)
+    slow = np.where(turns[:pairs] >= beta_fast, 0.0, np.where(turns[:pairs] <= beta_slow, 1.0, slow))
     return f * (1 - slow) + f / factor * slow, 0.1 * math.log(factor) + 1.0
 
 

@@ -223,17 +223,21 @@ int hcms_rope_frequencies(int pairs, double base, int scaling, double factor, do
     if (scaling != HCMS_ROPE_UNSCALED && (!std::isfinite(factor) || !(factor >= 1.0)))
         return fail(HCMS_ERR_ARG, "factor must be finite and >= 1 (got %g)", factor);
     const double two_pi = 6.283185307179586476925;
-    double lo = 0, hi = 0;
+    double fast = 0, slow = 0, lo = 0, hi = 0;
     if (scaling == HCMS_ROPE_YARN) {
         if (!std::isfinite(original_length) || !(original_length > 0) || !std::isfinite(beta_fast) ||
             !std::isfinite(beta_slow) || !(beta_slow > 0) || !(beta_fast >= beta_slow))
             return fail(HCMS_ERR_ARG, "need original_length > 0 and beta_fast >= beta_slow > 0");
-        // The pair that turns `beta` times over the original length.
+        // The pair, not rounded, that turns `beta` times over the original length.
         const auto at = [&](double beta) {
             return pairs * std::log(original_length / (two_pi * beta)) / std::log(base);
         };
-        lo = std::max(std::floor(at(beta_fast)), 0.0);
-        hi = std::min(std::ceil(at(beta_slow)), pairs - 1.0);
+        fast = at(beta_fast);
+        slow = at(beta_slow);
+        // The mixture's ends.  The upper one may lie past the last pair, which then is
+        // not slowed in full: it turns more than beta_slow times.
+        lo = std::max(std::floor(fast), 0.0);
+        hi = std::min(std::ceil(slow), 2.0 * pairs - 1.0);
     }
     const double b = scaling == HCMS_ROPE_NTK && pairs > 1 ? base * std::pow(factor, pairs / (pairs - 1.0)) : base;
     *magnitude = scaling == HCMS_ROPE_YARN ? 0.1 * std::log(factor) + 1.0 : 1.0;
@@ -241,7 +245,7 @@ int hcms_rope_frequencies(int pairs, double base, int scaling, double factor, do
         double f = std::pow(b, -static_cast<double>(i) / pairs);
         if (scaling == HCMS_ROPE_LINEAR) f /= factor;
         if (scaling == HCMS_ROPE_YARN) {
-            const double keep = 1.0 - std::min(std::max((i - lo) / std::max(hi - lo, 1e-3), 0.0), 1.0);
+            const double keep = i <= fast ? 1.0 : i >= slow ? 0.0 : 1.0 - std::min((i - lo) / (hi - lo), 1.0);
             f = f * keep + f / factor * (1.0 - keep);
         }
         freqs[i] = f;

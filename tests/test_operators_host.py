@@ -105,6 +105,28 @@ def test_scaled_frequencies_slow_the_slowest_pair_by_the_factor(lib):
     assert abs(m - (0.1 * math.log(4) + 1)) < 1e-15
 
 
+@pytest.mark.parametrize("pairs", [1, 2, 8, 21, 64, 256])
+@pytest.mark.parametrize("length", [3.0, 100.0, 4096.0, 65536.0, 262144.0, 1e6, 1e9])
+@pytest.mark.parametrize("fast,slow", [(32.0, 1.0), (8.0, 2.0), (4.0, 4.0)])
+def test_yarn_slows_pairs_by_their_turns(lib, pairs, length, fast, slow):
+    """From each pair's turns over the original length alone: kept from beta_fast on,
+    slowed by the factor up to beta_slow, strictly between in between (but for the pair
+    of the last whole index up to beta_fast, where the mixture starts)."""
+    base, factor = 10000.0, 8.0
+    got, m = hcms.rope_frequencies(pairs, base, "yarn", factor, length, fast, slow)
+    want, wm = op.frequencies(pairs, base, "yarn", factor, length, fast, slow)
+    assert np.allclose(got, want, rtol=1e-12, atol=0) and abs(m - wm) < 1e-14
+    plain = base ** (-np.arange(pairs) / pairs)
+    turns = length * plain / (2 * math.pi)
+    share = np.asarray(got) / plain
+    near = 1 + 1e-9
+    assert np.allclose(share[turns >= fast * near], 1, rtol=1e-12, atol=0)
+    assert np.allclose(share[turns * near <= slow], 1 / factor, rtol=1e-12, atol=0)
+    between = (turns * near < fast) & (turns > slow * near)
+    assert (share[between] > 1 / factor * near).all() and (share[between] <= 1).all()
+    assert (np.diff(share) <= 1e-12).all()
+
+
 def test_rotation_preserves_scores_of_equal_distance():
     rng = np.random.default_rng(2)
     q, k = rng.standard_normal((2, 1, 1, 16))
