@@ -754,7 +754,8 @@ HCMS_API int hcms_linear_fp8(const void *x, const void *x_scale, const void *w, 
  * transpose: the gradient's rotation, with a scaled table's magnitude kept.
  *   q, k      : heads of a side (k may be NULL): input x and output y at
  *               x + t x_token + h x_head (strides in elements); the output may be
- *               the input itself (same address and strides)
+ *               the input itself (same address and strides), and shares no memory
+ *               with the other side's input or output
  *   positions : NULL (token t at place t of the row-major grid; S at most its
  *               size) or device [S][n_axes] of position_bytes 4 (int32) or 8
  *               (int64).  A token with a position outside the grid gets NaN.

@@ -12,6 +12,7 @@
 #include "checks.h"
 #include "fp8.h"
 #include "hcms_internal.h"
+#include "rope_heads.h"
 
 namespace {
 
@@ -293,15 +294,15 @@ int hcms_rope(const hcms_rope_heads *q, const hcms_rope_heads *k, const float *t
         return fail(HCMS_ERR_SHAPE, "S=%d tokens on a grid of %lld", S, static_cast<long long>(tokens));
     const int es = elem_bytes(dtype);
     const hcms_rope_heads *sides[2] = {q, k};
+    static const char *const in_name[2] = {"q", "k"}, *const out_name[2] = {"the rotated q", "the rotated k"};
     hcms::RopeSide side[2] = {};
-    Buffer in[4], out[2];
+    hcms::HeadBlock in[2], out[2];   // of the sides that have heads
     bool in_place[2] = {};
-    int n_in = 0, n_out = 0;
     if (S > 0 && !table) return fail(HCMS_ERR_NULL, "table is NULL");
     if (!aligned(table, 8) || !aligned(positions, position_bytes ? position_bytes : 1))
         return fail(HCMS_ERR_ALIGN, "table must be 8-byte aligned, positions to their elements");
-    in[n_in++] = {"table", table, entries * 8};
-    in[n_in++] = {"positions", positions, static_cast<int64_t>(S) * n_axes * position_bytes};
+    const Buffer shared[2] = {{"table", table, entries * 8},
+                              {"positions", positions, static_cast<int64_t>(S) * n_axes * position_bytes}};
     for (int i = 0; i < 2; ++i) {
         const hcms_rope_heads *h = sides[i];
         if (!h) continue;
@@ -319,26 +320,29 @@ int hcms_rope(const hcms_rope_heads *q, const hcms_rope_heads *k, const float *t
             return fail(HCMS_ERR_SHAPE, "output tokens overlap");
         if (!aligned(h->x, es) || !aligned(h->y, es))
             return fail(HCMS_ERR_ALIGN, "buffers must be aligned to their elements");
-        const int64_t xb = ((S - 1) * h->x_token + (h->heads - 1) * h->x_head + d) * es;
-        const int64_t yb = ((S - 1) * h->y_token + (h->heads - 1) * h->y_head + d) * es;
         side[i] = {h->x, h->y, h->x_token, h->x_head, h->y_token, h->y_head, h->heads};
+        in[i] = {reinterpret_cast<uintptr_t>(h->x), h->x_token * es, h->x_head * es, S, d * es, h->heads};
+        out[i] = {reinterpret_cast<uintptr_t>(h->y), h->y_token * es, h->y_head * es, S, d * es, h->heads};
         in_place[i] = h->x == h->y && h->x_token == h->y_token && h->x_head == h->y_head;
-        if (!in_place[i]) {
-            in[n_in++] = {i ? "k" : "q", h->x, xb};
-            out[n_out++] = {i ? "the rotated k" : "the rotated q", h->y, yb};
-        } else {
-            // Its heads may lie between the other side's, so only the table and
-            // the positions are compared.
-            const Buffer self[] = {{i ? "k" : "q", h->x, xb}};
-            if ((st = check_disjoint(self, 1, in, 2)) != HCMS_OK) return st;
-        }
+        const Buffer y[] = {{out_name[i], h->y, hcms::heads_span(out[i])}};
+        if ((st = check_disjoint(y, 1, shared, 2)) != HCMS_OK) return st;
     }
-    if ((st = check_disjoint(out, n_out, in, n_in)) != HCMS_OK) return st;
-    for (int i = 0; i < 2; ++i)   // one side in place: the other's output is elsewhere
-        if (in_place[i] && n_out == 1) {
-            const Buffer self[] = {{i ? "k" : "q", side[i].x,
-                                    ((S - 1) * side[i].x_token + (side[i].H - 1) * side[i].x_head + d) * es}};
-            if ((st = check_disjoint(out, n_out, self, 1)) != HCMS_OK) return st;
+    // A head is written by one workgroup and read by it alone.  A side in place lies
+    // between the other one's heads where both are of one packed buffer, so its heads
+    // are compared, not its first and last byte.
+    const auto meet = [&](const hcms::HeadBlock &a, const hcms::HeadBlock &b, bool exact) {
+        return exact ? hcms::heads_meet(a, b)
+                     : overlaps(reinterpret_cast<const void *>(a.p), hcms::heads_span(a),
+                                reinterpret_cast<const void *>(b.p), hcms::heads_span(b));
+    };
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2; ++j) {
+            if (side[i].H == 0 || side[j].H == 0) continue;
+            const bool exact = in_place[i] || in_place[j];
+            if ((i != j || !in_place[i]) && meet(out[i], in[j], exact))
+                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out_name[i], in_name[j]);
+            if (i < j && meet(out[i], out[j], exact))
+                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out_name[i], out_name[j]);
         }
     if (S == 0 || side[0].H + side[1].H == 0) return ok();
     const hipError_t e = hcms::launch_rope(side[0], side[1], table, ax, positions, position_bytes == 8, S, d,

@@ -240,6 +240,27 @@ def test_rope_refusals(lib):
     assert call(q=heads(A, A, yt=512)) == EALIAS                   # same address, other strides
 
 
+def test_rope_in_place_refuses_heads_that_overlap(lib):
+    """Sides in place (output = input, 4 heads of 64 bf16 in tokens of xt elements)
+    whose heads another workgroup reads or writes.  Refused calls only: the addresses
+    are no memory."""
+    def call(q, k, S=10):
+        def heads(x, y, t=512, n=4):
+            return ctypes.byref(RopeHeads(x, y, t, 64, t, 64, n))
+        one = ctypes.c_int * 1
+        return lib.hcms_rope(heads(*q), heads(*k), C, one(100), one(32), 1, None, 0, S, 64, 0, 0, 0, None)
+
+    for S in (1, 10):
+        assert call((A, A), (A, A), S) == EALIAS                   # one buffer, turned twice
+        assert call((A, A), (A + 3 * 128, A + 3 * 128), S) == EALIAS   # k begins at q's last head
+        assert call((A, A), (A + 3 * 128 + 126, A + 3 * 128 + 126), S) == EALIAS   # by one element
+        assert call((A, A), (A, D), S) == EALIAS                   # k reads what q turns in place
+        assert call((A, D), (A, A), S) == EALIAS and call((A, D), (D, D), S) == EALIAS
+    assert call((A, A), (A + 7 * 128, A + 7 * 128)) == EALIAS      # k's second head is the next token's first
+    assert call((A, A), (A + 4 * 128, A + 4 * 128, 256)) == EALIAS   # other token strides
+    assert b"overlaps" in lib.hcms_last_error()
+
+
 def test_rope_table_and_frequency_refusals(lib):
     g, p = (ctypes.c_int * 1)(16), (ctypes.c_int * 1)(4)
     f = (ctypes.c_double * 4)(1, 0.5, 0.25, 0.1)
