@@ -323,25 +323,19 @@ int hcms_rope(const hcms_rope_heads *q, const hcms_rope_heads *k, const float *t
         side[i] = {h->x, h->y, h->x_token, h->x_head, h->y_token, h->y_head, h->heads};
         in[i] = {reinterpret_cast<uintptr_t>(h->x), h->x_token * es, h->x_head * es, S, d * es, h->heads};
         out[i] = {reinterpret_cast<uintptr_t>(h->y), h->y_token * es, h->y_head * es, S, d * es, h->heads};
-        in_place[i] = h->x == h->y && h->x_token == h->y_token && h->x_head == h->y_head;
+        // The strides of a single token and of a single head say nothing.
+        in_place[i] = h->x == h->y && (S == 1 || h->x_token == h->y_token) && (h->heads == 1 || h->x_head == h->y_head);
         const Buffer y[] = {{out_name[i], h->y, hcms::heads_span(out[i])}};
         if ((st = check_disjoint(y, 1, shared, 2)) != HCMS_OK) return st;
     }
-    // A head is written by one workgroup and read by it alone.  A side in place lies
-    // between the other one's heads where both are of one packed buffer, so its heads
-    // are compared, not its first and last byte.
-    const auto meet = [&](const hcms::HeadBlock &a, const hcms::HeadBlock &b, bool exact) {
-        return exact ? hcms::heads_meet(a, b)
-                     : overlaps(reinterpret_cast<const void *>(a.p), hcms::heads_span(a),
-                                reinterpret_cast<const void *>(b.p), hcms::heads_span(b));
-    };
+    // A head is written by one workgroup and read by it alone.  Heads are compared, not
+    // a side's first and last byte: both sides may lie in one packed buffer.
     for (int i = 0; i < 2; ++i)
         for (int j = 0; j < 2; ++j) {
             if (side[i].H == 0 || side[j].H == 0) continue;
-            const bool exact = in_place[i] || in_place[j];
-            if ((i != j || !in_place[i]) && meet(out[i], in[j], exact))
+            if ((i != j || !in_place[i]) && hcms::heads_meet(out[i], in[j]))
                 return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out_name[i], in_name[j]);
-            if (i < j && meet(out[i], out[j], exact))
+            if (i < j && hcms::heads_meet(out[i], out[j]))
                 return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out_name[i], out_name[j]);
         }
     if (S == 0 || side[0].H + side[1].H == 0) return ok();

@@ -478,6 +478,38 @@ def test_rope_strides_and_in_place(hcms, layout):
     assert torch.equal(bits(qkv[:, 8 + (H + Hk) * d:]), bits(before[:, 8 + (H + Hk) * d:]))
 
 
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+def test_rope_into_one_packed_buffer(hcms, layout):
+    """Outputs that lie between each other in one buffer, side by side or head by head,
+    beside their inputs too: the bits of the contiguous call, and nothing else touched."""
+    S, H, d = 37, 3, 32
+    table = hcms.rope_table([S], [8])
+    args = (table, [S], [8])
+    q, k = _randn(1, S, H, d, dtype=BF16).cuda(), _randn(2, S, H, d, dtype=BF16).cuda()
+    want = hcms.rope(q, k, *args, layout=layout)
+    for shape, pick in (((S, 5 * H, d), lambda t, i: t[:, i * H:(i + 1) * H]), ((S, H, 5, d), lambda t, i: t[:, :, i])):
+        buf = _randn(3, *shape, dtype=BF16).cuda()
+        before = buf.clone()
+        pick(buf, 0).copy_(q)
+        pick(buf, 1).copy_(k)
+        got = hcms.rope(pick(buf, 0), pick(buf, 1), *args, layout=layout, out=(pick(buf, 3), pick(buf, 2)))
+        for i, w in ((0, q), (1, k), (2, want[1]), (3, want[0]), (4, pick(before, 4))):
+            assert torch.equal(bits(pick(buf, i).contiguous()), bits(w.contiguous())), i
+        assert got[0].data_ptr() == pick(buf, 3).data_ptr()
+        hcms.rope(pick(buf, 0), pick(buf, 1), *args, layout=layout, out=(pick(buf, 0), pick(buf, 4)))   # one in place
+        assert torch.equal(bits(pick(buf, 0).contiguous()), bits(want[0])) and \
+            torch.equal(bits(pick(buf, 4).contiguous()), bits(want[1]))
+        with pytest.raises(hcms.HcmsError, match="overlaps"):
+            hcms.rope(q, k, *args, layout=layout, out=(pick(buf, 0), pick(buf, 0)))
+    # a single token, whose token strides differ
+    wide = _randn(4, 2, H, d, dtype=BF16).cuda()
+    x, y = wide[:1], torch.as_strided(wide, (1, H, d), (7 * H * d, d, 1))
+    table1 = hcms.rope_table([1], [8])
+    first = wide[:1].clone()
+    hcms.rope(x, None, table1, [1], [8], layout=layout, out=(y, None))
+    assert torch.equal(bits(x), bits(hcms.rope(first, None, table1, [1], [8], layout=layout)))
+
+
 def test_rope_positions_outside_the_grid_give_nan(hcms):
     table = hcms.rope_table([10], [8])
     q = _randn(1, 5, 2, 32).cuda()
