@@ -169,6 +169,16 @@ def _table_rows(grid, axis_pairs) -> int:
     return _check(load().hcms_rope_table_entries(g, p, na))
 
 
+def _gpu_device(device) -> torch.device:
+    """``device`` for memory that a kernel on the current device writes."""
+    device = torch.get_default_device() if device is None else torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"device must be a GPU (got {device})")
+    if device.index is not None and device.index != torch.cuda.current_device():
+        raise ValueError(f"device is {device}, the current device is {torch.cuda.current_device()}")
+    return device
+
+
 def _stream(s) -> ctypes.c_void_p:
     if s is None:
         s = torch.cuda.current_stream()
@@ -428,11 +438,12 @@ def rope_table(grid, axis_pairs, base: float = 10000.0, device="cuda",
                stream=None) -> torch.Tensor:
     """The rotation table of the latent grid ``grid`` whose head vectors'
     pairs split into consecutive groups of ``axis_pairs`` (one per axis):
-    float32 [E][2] (cos, sin), filled on the GPU."""
+    float32 [E][2] (cos, sin), filled on the GPU.  ``device`` is the current one."""
     g, na = _ints(grid)
     p, npairs = _ints(axis_pairs)
     if na != npairs:
         raise ValueError("one pair count per grid axis")
+    device = _gpu_device(device)
     lib = load()
     n = _check(lib.hcms_rope_table_entries(g, p, na))
     table = torch.empty((max(1, n), 2), dtype=torch.float32, device=device)

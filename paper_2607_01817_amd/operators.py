@@ -20,7 +20,7 @@ import os
 
 import torch
 
-from . import _PKG, _check, _ints, _table_rows, load
+from . import _PKG, _check, _gpu_device, _ints, _table_rows, load
 
 E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 SCALE_BLOCK = 128
@@ -147,9 +147,11 @@ def rope_frequencies(pairs: int, base: float = 10000.0, scaling: str = "none", f
 def rope_table_freqs(grid, axis_pairs, freqs, magnitude: float = 1.0, device="cuda", *,
                      stream=None) -> torch.Tensor:
     """The rotation table (see :func:`rope_table`) of given frequencies, one per
-    pair, with every entry times ``magnitude``: float32 [entries][2]."""
+    pair, with every entry times ``magnitude``: float32 [entries][2].  ``device`` is
+    the current one (that of ``stream``)."""
     if stream is not None:
         return _under(stream, rope_table_freqs, grid, axis_pairs, freqs, magnitude, device)
+    device = _gpu_device(device)
     n = _table_rows(grid, axis_pairs)
     g, na = _ints(grid)
     p, _ = _ints(axis_pairs)

@@ -308,3 +308,12 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         hcms.linear_fp8(q, s, q, s, parts=5)
     with pytest.raises(TypeError, match="dtype"):
         hcms.linear_fp8(q, s, q, s, dtype=torch.float16)
+
+
+def test_rope_tables_refuse_devices_whose_memory_a_kernel_here_does_not_write(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for make in (lambda dev: hcms.rope_table([4], [2], device=dev),
+                 lambda dev: hcms.rope_table_freqs([4], [2], [1.0, 0.1], device=dev)):
+        for dev in ("cpu", torch.device("cpu"), None, "meta", "cuda:1", torch.device("cuda", 3)):
+            with pytest.raises(ValueError, match="device"):
+                make(dev)
