@@ -115,11 +115,22 @@ int64_t row_stride(const Tensor &t, const char *name) {
 // The same of rows that have been checked.
 int64_t stride_of(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
 
+// A caller's tensor that a call writes: no gradient reaches what it writes, and
+// autograd learns of the write (of a tensor that an operator has saved), once the call
+// has taken place.
+void writable(const Tensor &t, const char *name) {
+    VALUE(!(t.requires_grad() && at::GradMode::is_enabled()), name, " requires grad: no gradient reaches its values");
+}
+void wrote(const MaybeTensor &t) {
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 Tensor output(const MaybeTensor &t, at::IntArrayRef shape, at::ScalarType type, const Tensor &x, const char *name) {
     if (!t) return empty(shape, type, x);
     expect(*t, shape, type, name);
     dense(*t, name);
     with(x, *t, name);
+    writable(*t, name);
     return *t;
 }
 
@@ -165,6 +176,8 @@ py::object rms_norm(const Tensor &x, const Tensor &weight, double eps, const May
     MaybeTensor h;
     if (residual) h = output(h_out, x.sizes(), x.scalar_type(), x, "h_out");
     launch_norm(x, weight, eps, residual, y, h);
+    wrote(out);
+    wrote(h_out);
     return h ? py::object(py::make_tuple(y, *h)) : py::cast(y);
 }
 
@@ -181,6 +194,7 @@ py::tuple rms_norm_fp8(const Tensor &x, const Tensor &weight, double eps, const 
                                  stride_of(x), residual ? stride_of(*residual) : x.size(1), static_cast<float>(eps),
                                  dtype_of(x), dtype_of(weight), stream);
     });
+    wrote(h_out);
     return h ? py::make_tuple(q, s, *h) : py::make_tuple(q, s);
 }
 
@@ -326,6 +340,7 @@ Tensor linear_fp8(const Tensor &x, const Tensor &x_scale, const Tensor &w, const
     int_of(K, "K");
     const Tensor y = parts == 1 ? output(out, {M, N}, type, x, "out") : output(out, {parts, M, N / parts}, type, x, "out");
     launch_linear(x, x_scale, w, w_scale, y, parts);
+    wrote(out);
     return y;
 }
 
@@ -449,16 +464,22 @@ py::object rope(const Tensor &q, const MaybeTensor &k, const Tensor &table, cons
         yq = *out->first;
         check_side(yq, q, "out's q");
         VALUE(yq.sizes() == q.sizes(), "out's q must match q");
+        writable(yq, "out's q");
         if (k) {
             yk = out->second;
             check_side(*yk, q, "out's k");
             VALUE(yk->sizes() == k->sizes(), "out's k must match k");
+            writable(*yk, "out's k");
         }
     } else {
         yq = empty(q.sizes(), q.scalar_type(), q);
         if (k) yk = empty(k->sizes(), k->scalar_type(), *k);
     }
     launch_rope(q, k, yq, yk, table, ax, positions, half, inverse);
+    if (out) {
+        wrote(yq);
+        wrote(yk);
+    }
     return k ? py::object(py::make_tuple(yq, *yk)) : py::cast(yq);
 }
 

@@ -10,7 +10,10 @@ The tensors are checked, allocated and passed on in ``_hcms_torch.so``
 (csrc/torch_ops.cpp), which calls the C ABI and refuses what it refuses with
 :class:`HcmsError`; wrong shapes, types and devices are ValueError and TypeError.
 Calls run on the current stream, or on ``stream``, to which their outputs and
-workspaces then belong.
+workspaces then belong.  Tensors given to write to (``out``, ``h_out``) carry no
+gradient: one that requires grad is refused where autograd records, and a write to
+one that an operator has saved for its backward makes that backward raise, as
+PyTorch's own writes in place do.
 """
 from __future__ import annotations
 

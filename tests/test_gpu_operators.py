@@ -550,6 +550,59 @@ def test_rope_gradient(hcms, layout):
 
 
 # ---------------------------------------------------------------------------
+# Outputs of the caller, and autograd
+# ---------------------------------------------------------------------------
+def _writes(hcms, t, stream=None):
+    """Calls that write t [32][64] bf16 through each argument that takes an output."""
+    other = [_randn(i, 32, 64, dtype=BF16).cuda() for i in (1, 2)]
+    w = torch.ones(64, dtype=BF16, device="cuda")
+    q8, w8 = hcms.quantize_fp8(other[0], 1), hcms.quantize_fp8(_randn(3, 64, 64).cuda(), 128)
+    rope = (hcms.rope_table([32], [16]), [32], [16])
+    heads = [x.view(32, 1, 64) for x in (*other, t)]
+    return {
+        "norm": lambda: hcms.rms_norm(other[0], w, out=t, stream=stream),
+        "norm h": lambda: hcms.rms_norm(other[0], w, residual=other[1], h_out=t, stream=stream),
+        "norm fp8 h": lambda: hcms.rms_norm_fp8(other[0], w, residual=other[1], h_out=t, stream=stream),
+        "linear": lambda: hcms.linear_fp8(*q8, *w8, out=t, stream=stream),
+        "rope q": lambda: hcms.rope(heads[0], None, *rope, out=(heads[2], None), stream=stream),
+        "rope k": lambda: hcms.rope(heads[0], heads[1], *rope, out=(torch.empty_like(heads[0]), heads[2]), stream=stream),
+        "rope in place": lambda: hcms.rope(heads[2], None, *rope, out=(heads[2], None), stream=stream),
+    }
+
+
+WRITES = ["norm", "norm h", "norm fp8 h", "linear", "rope q", "rope k", "rope in place"]
+
+
+@pytest.mark.parametrize("how", WRITES)
+def test_backward_raises_after_a_saved_tensor_was_written(hcms, how):
+    """RmsNorm keeps x and the residual, of which its backward works out h again."""
+    w = torch.ones(64, dtype=BF16, device="cuda", requires_grad=True)
+    for which in (0, 1):
+        kept = [_randn(10 + i, 32, 64, dtype=BF16).cuda() for i in range(2)]
+        y, _ = hcms.RmsNorm.apply(kept[0], w, 1e-6, kept[1])
+        version = kept[which]._version
+        _writes(hcms, kept[which])[how]()
+        assert kept[which]._version == version + 1
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.float().sum().backward()
+    with torch.inference_mode():
+        _writes(hcms, torch.zeros(32, 64, dtype=BF16, device="cuda"))[how]()   # has no version
+
+
+@pytest.mark.parametrize("how", WRITES)
+def test_outputs_that_require_grad_are_refused(hcms, how):
+    leaf = torch.zeros(32, 64, dtype=BF16, device="cuda", requires_grad=True)
+    call = _writes(hcms, leaf)[how]
+    with pytest.raises(ValueError, match="requires grad"):
+        call()
+    assert leaf._version == 0 and not leaf.any()
+    with torch.no_grad():                    # as an optimizer writes its parameters
+        call = _writes(hcms, leaf)[how]
+        call()
+    assert leaf._version == 1
+
+
+# ---------------------------------------------------------------------------
 # Streams and graphs
 # ---------------------------------------------------------------------------
 def _chain(hcms, x, r, w, wq, ws, table, stream=None):
