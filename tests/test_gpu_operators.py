@@ -602,6 +602,20 @@ def test_outputs_that_require_grad_are_refused(hcms, how):
     assert leaf._version == 1
 
 
+def test_operators_are_differentiable_once(hcms):
+    """A gradient of a gradient would be wrong without a word: it is refused."""
+    def leaf(seed, *shape):
+        return _randn(seed, *shape, dtype=BF16).cuda().requires_grad_(True)
+
+    x, w, q = leaf(1, 32, 64), leaf(2, 32, 64), leaf(3, 5, 2, 32)
+    table = hcms.rope_table([5], [16])
+    for out, leaves in ((hcms.RmsNorm.apply(x, torch.ones(64, dtype=BF16, device="cuda")), (x,)),
+                        (hcms.Fp8Linear.apply(x, w), (x, w)), (hcms.Rope.apply(q, None, table, [5], [16]), (q,))):
+        with pytest.raises(RuntimeError, match="differentiable once"):
+            torch.autograd.grad(out.float().sum(), leaves, create_graph=True, retain_graph=True)
+        assert all(torch.isfinite(g).all() for g in torch.autograd.grad(out.float().sum(), leaves))
+
+
 # ---------------------------------------------------------------------------
 # Streams and graphs
 # ---------------------------------------------------------------------------
