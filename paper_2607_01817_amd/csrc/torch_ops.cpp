@@ -24,6 +24,7 @@ using MaybeTensor = std::optional<Tensor>;
 constexpr auto kE4M3 = at::kFloat8_e4m3fn;
 constexpr auto kE8M0 = at::kFloat8_e8m0fnu;
 constexpr int64_t kBlock = 128;
+constexpr int64_t kMostK = 1 << 20;   // of the 8-bit product
 
 template <typename... A>
 std::string text(const A &...a) {
@@ -378,6 +379,8 @@ Tensor fp8_linear_train(const Tensor &x, const Tensor &w) {
     const bool grad = at::GradMode::is_enabled(), need_x = grad && x.requires_grad(), need_w = grad && w.requires_grad();
     VALUE(w.size(0) % (need_x || need_w ? 16 : 8) == 0, "N = ", w.size(0),
           " must be a multiple of 16, or of 8 without gradients");
+    // The tokens are the contraction of w's gradient: refused here, not after the forward.
+    VALUE(!need_w || x.size(0) <= kMostK, "M = ", x.size(0), " exceeds 2^20, the most tokens of a gradient of w");
     check_quantize(x);
     check_quantize(w);
     with(x, w, "w");

@@ -125,7 +125,8 @@ class Fp8Linear:
     is x [M][K] times w [N][K] in their dtype, with activations and gradients
     quantised per row and 128 of the contraction, and weights (and the activations
     of the weight's gradient) per 128 x 128.  K and N must be multiples of 16 (N of
-    8 without gradients).  What the backward needs is kept in 8 bits."""
+    8 without gradients), each at most 2^20, and M too where w needs a gradient, whose
+    contraction runs over the tokens.  What the backward needs is kept in 8 bits."""
 
     @staticmethod
     def apply(x, w):

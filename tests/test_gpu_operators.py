@@ -388,6 +388,21 @@ def test_fp8_linear_of_no_tokens_and_refusals(hcms):
     assert hcms.Fp8Linear.apply(_randn(2, 4, 64).cuda(), _randn(3, 24, 64).cuda()).shape == (4, 24)
 
 
+def test_fp8_linear_refuses_tokens_that_its_backward_cannot_contract(hcms):
+    """More than 2^20 tokens: refused ahead of the forward where w needs a gradient."""
+    most = 1 << 20
+    x = torch.ones(most + 1, 16, dtype=BF16, device="cuda", requires_grad=True)
+    w = torch.ones(16, 16, dtype=BF16, device="cuda", requires_grad=True)
+    with pytest.raises(ValueError, match="2\\^20"):
+        hcms.Fp8Linear.apply(x, w)
+    (dx,) = torch.autograd.grad(hcms.Fp8Linear.apply(x, w.detach()).float().sum(), (x,))
+    assert (dx == 16).all()
+    with torch.no_grad():
+        assert (hcms.Fp8Linear.apply(x, w) == 16).all()
+    (dw,) = torch.autograd.grad(hcms.Fp8Linear.apply(x[:most], w).float().sum(), (w,))
+    assert (dw == most).all()                # a power of two
+
+
 # ---------------------------------------------------------------------------
 # Rotary positions
 # ---------------------------------------------------------------------------
