@@ -362,7 +362,8 @@ struct Fp8Linear : torch::autograd::Function<Fp8Linear> {
         Tensor dx, dw;
         if (need_x) dx = empty({M, K}, g[0].scalar_type(), g[0]);
         if (need_w) dw = empty({N, K}, g[0].scalar_type(), g[0]);
-        if (M == 0) {
+        if (M == 0 || N == 0) {   // sums of nothing
+            if (need_x) dx.zero_();
             if (need_w) dw.zero_();
         } else {
             const Quantized d = launch_quantize(g[0].contiguous(), need_x ? 1 : 0, need_w ? 1 : 0);

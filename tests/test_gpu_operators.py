@@ -403,6 +403,16 @@ def test_fp8_linear_refuses_tokens_that_its_backward_cannot_contract(hcms):
     assert (dw == most).all()                # a power of two
 
 
+def test_fp8_linear_of_no_outputs(hcms):
+    """N = 0: the gradient of x is a sum of nothing."""
+    x = _randn(1, 5, 64, dtype=BF16).cuda().requires_grad_(True)
+    w = torch.empty(0, 64, dtype=BF16, device="cuda", requires_grad=True)
+    y = hcms.Fp8Linear.apply(x, w)
+    assert y.shape == (5, 0)
+    dx, dw = torch.autograd.grad(y, (x, w), torch.empty(5, 0, dtype=BF16, device="cuda"))
+    assert dx.shape == (5, 64) and (dx == 0).all() and dw.shape == (0, 64)
+
+
 # ---------------------------------------------------------------------------
 # Rotary positions
 # ---------------------------------------------------------------------------
