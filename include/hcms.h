@@ -668,7 +668,8 @@ HCMS_API int hcms_layer_forward(hcms_ctx *ctx, const void *x, const void *w_qkv,
  * h is rounded to the storage type when it is stored; y is computed from the
  * unrounded sum, in fp32, and rounded once.  Without a residual (NULL, with h
  * NULL) h is x.
- *   x, residual : device, rows of D elements ldx and ldr elements apart
+ *   x, residual : device, rows of D elements ldx and ldr elements apart (at most
+ *                 2^40, and all M rows within 2^60)
  *   weight      : device, [D] of weight_dtype
  *   y, h        : device, [M][D], disjoint from the inputs and each other
  * Buffers need the alignment of their elements only.  8 <= D <= 16384, eps >= 0.
@@ -714,7 +715,8 @@ HCMS_API int hcms_rms_norm_backward(const void *dy, const void *x, const void *r
  * groups of four blocks, [ceil(K / 512)][R][4] bytes: byte [g][r][i] belongs to
  * block 4 g + i.  Bytes of blocks past K are those of a block of zeros (1).
  *
- * hcms_quantize_fp8 makes operands of x [M][K] (rows ldx elements apart):
+ * hcms_quantize_fp8 makes operands of x [M][K] (rows ldx elements apart, with the
+ * norm's limits):
  *   q : [M][K], NULL for none; q_scale: per row (q_block 1, R = M) or per 128 x
  *       128 (q_block 128, R = ceil(M / 128))
  *   t : x transposed, [K][M'] with M' = M rounded up to 16, padded with zeros,
@@ -753,7 +755,8 @@ HCMS_API int hcms_linear_fp8(const void *x, const void *x_scale, const void *w, 
  * for the token's coordinates; elements past R are copied.  The inverse is the
  * transpose: the gradient's rotation, with a scaled table's magnitude kept.
  *   q, k      : heads of a side (k may be NULL): input x and output y at
- *               x + t x_token + h x_head (strides in elements); the output may be
+ *               x + t x_token + h x_head (strides in elements, at most 2^40, and
+ *               all S tokens within 2^60); the output may be
  *               the input itself (same address and strides), and shares no memory
  *               with the other side's input or output
  *   positions : NULL (token t at place t of the row-major grid; S at most its

@@ -47,6 +47,8 @@ int check_disjoint(const Buffer *out, int n_out, const Buffer *in, int n_in) {
     return HCMS_OK;
 }
 
+constexpr int64_t kMostSpan = 1LL << 60;   // elements from a buffer's first to its last one, or nearly
+
 // Bytes from the first to the last element of M rows of n, ld elements apart.
 int64_t span_bytes(int64_t M, int64_t n, int64_t ld, int es) { return M < 1 ? 0 : ((M - 1) * ld + n) * es; }
 
@@ -64,10 +66,14 @@ int check_norm_shape(int M, int D, int dtype, int weight_dtype, float eps) {
     return HCMS_OK;
 }
 
-int check_stride(int64_t ld, int n, const char *name) {
+// M rows of n elements, ld apart: the span of any type's bytes fits 63 bits.
+int check_stride(int64_t ld, int n, int M, const char *name) {
     if (ld < n || ld > (1LL << 40))
         return fail(HCMS_ERR_SHAPE, "%s=%lld is below the row's %d elements or above 2^40", name,
                     static_cast<long long>(ld), n);
+    if (M > 1 && ld > kMostSpan / (M - 1))
+        return fail(HCMS_ERR_SHAPE, "%d rows %lld elements apart span more than 2^60 elements", M,
+                    static_cast<long long>(ld));
     return HCMS_OK;
 }
 
@@ -75,8 +81,8 @@ int norm_forward(const void *x, const void *residual, const void *weight, void *
                  int M, int D, int64_t ldx, int64_t ldr, float eps, int dtype, int weight_dtype, void *stream) {
     int st;
     if ((st = check_norm_shape(M, D, dtype, weight_dtype, eps)) != HCMS_OK) return st;
-    if ((st = check_stride(ldx, D, "ldx")) != HCMS_OK) return st;
-    if (residual && (st = check_stride(ldr, D, "ldr")) != HCMS_OK) return st;
+    if ((st = check_stride(ldx, D, M, "ldx")) != HCMS_OK) return st;
+    if (residual && (st = check_stride(ldr, D, M, "ldr")) != HCMS_OK) return st;
     const bool f8 = q || scale;
     if (f8 && D % 16 != 0) return fail(HCMS_ERR_SHAPE, "D=%d must be a multiple of 16 for 8-bit output", D);
     if (M == 0) return ok();
@@ -128,8 +134,8 @@ int hcms_rms_norm_backward(const void *dy, const void *x, const void *residual, 
                            int dtype, int weight_dtype, void *stream) {
     int st;
     if ((st = check_norm_shape(M, D, dtype, weight_dtype, eps)) != HCMS_OK) return st;
-    if ((st = check_stride(ldx, D, "ldx")) != HCMS_OK) return st;
-    if (residual && (st = check_stride(ldr, D, "ldr")) != HCMS_OK) return st;
+    if ((st = check_stride(ldx, D, M, "ldx")) != HCMS_OK) return st;
+    if (residual && (st = check_stride(ldr, D, M, "ldr")) != HCMS_OK) return st;
     if (!dw) return fail(HCMS_ERR_NULL, "dw is NULL");
     if (M > 0 && (!dy || !x || !weight || !dx || !partial))
         return fail(HCMS_ERR_NULL, "dy, x, weight, dx or partial is NULL");
@@ -160,7 +166,7 @@ int hcms_quantize_fp8(const void *x, void *q, void *q_scale, int q_block, void *
     if ((st = check_dtype(dtype)) != HCMS_OK) return st;
     if (M < 0 || K < 16 || K % 16 != 0 || K > (1 << 20))
         return fail(HCMS_ERR_SHAPE, "need M >= 0 and K a positive multiple of 16, at most 2^20 (M=%d K=%d)", M, K);
-    if ((st = check_stride(ldx, K, "ldx")) != HCMS_OK) return st;
+    if ((st = check_stride(ldx, K, M, "ldx")) != HCMS_OK) return st;
     if ((q_block != 1 && q_block != hcms::fp8::kBlock) || (t_block != 1 && t_block != hcms::fp8::kBlock))
         return fail(HCMS_ERR_ARG, "scale blocks have 1 or 128 rows (q_block=%d t_block=%d)", q_block, t_block);
     if ((q == nullptr) != (q_scale == nullptr) || (t == nullptr) != (t_scale == nullptr))
@@ -312,6 +318,10 @@ int hcms_rope(const hcms_rope_heads *q, const hcms_rope_heads *k, const float *t
         const int64_t strides[4] = {h->x_token, h->x_head, h->y_token, h->y_head};
         for (const int64_t s : strides)
             if (s < 0 || s > (1LL << 40)) return fail(HCMS_ERR_SHAPE, "strides must be in [0, 2^40]");
+        for (const int64_t s : {h->x_token, h->y_token})
+            if (S > 1 && s > kMostSpan / (S - 1))
+                return fail(HCMS_ERR_SHAPE, "%d tokens %lld elements apart span more than 2^60 elements", S,
+                            static_cast<long long>(s));
         // Distinct heads and tokens of the output do not overlap.
         const bool by_token = h->y_token >= h->y_head;
         if (h->y_head < d && h->heads > 1) return fail(HCMS_ERR_SHAPE, "output heads overlap");

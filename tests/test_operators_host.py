@@ -317,3 +317,20 @@ def test_rope_tables_refuse_devices_whose_memory_a_kernel_here_does_not_write(mo
         for dev in ("cpu", torch.device("cpu"), None, "meta", "cuda:1", torch.device("cuda", 3)):
             with pytest.raises(ValueError, match="device"):
                 make(dev)
+
+
+def test_rows_and_tokens_that_span_more_than_63_bits_are_refused(lib):
+    """Strides whose span wraps would pass for buffers that overlap nothing."""
+    M, far = 2 ** 31 - 1, 1 << 40
+    def norm(ldx, ldr, M=M):
+        return lib.hcms_rms_norm(A, B, C, D, E, M, 8, ldx, ldr, 1e-6, 0, 0, None)
+
+    assert norm(far, 8) == ESHAPE and norm(8, far) == ESHAPE and norm((1 << 29) + 1, 8, (1 << 31) - 1) == ESHAPE
+    assert b"span" in lib.hcms_last_error()
+    assert lib.hcms_rms_norm_backward(A, B, None, None, C, D, E, F, M, 8, far, 8, 1e-6, 0, 0, None) == ESHAPE
+    assert lib.hcms_quantize_fp8(A, B, C, 1, None, None, 1, M, 16, far, 0, None) == ESHAPE
+    one = ctypes.c_int * 1
+    for xt, yt in ((far, 64), (64, far)):
+        q = RopeHeads(A, B, xt, 64, yt, 64, 1)
+        assert lib.hcms_rope(ctypes.byref(q), None, C, one(100), one(1), 1, D, 4, M, 64, 0, 0, 0, None) == ESHAPE
+        assert b"span" in lib.hcms_last_error()
