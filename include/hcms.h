@@ -739,7 +739,7 @@ HCMS_API int hcms_quantize_fp8(const void *x, void *q, void *q_scale, int q_bloc
  *   w : device, [N][K] e4m3;  w_scale : per 128 x 128, [ceil(K / 512)][ceil(N / 128)][4]
  *   y : device, [parts][M][N / parts]: column n in part n / (N / parts) (3 parts
  *       of a QKV projection are its q, k and v as hcms_forward takes them)
- * K a positive multiple of 16 and N of 8 parts, each at most 2^20; M >= 0.
+ * K a positive multiple of 16 and N of 8 parts, each at most 2^20; 0 <= M <= 2^31 - 256.
  * Deterministic.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, HIP.
  */
 HCMS_API int hcms_linear_fp8(const void *x, const void *x_scale, const void *w, const void *w_scale,

@@ -199,7 +199,9 @@ int hcms_linear_fp8(const void *x, const void *x_scale, const void *w, const voi
                     int K, int parts, int dtype, void *stream) {
     int st;
     if ((st = check_dtype(dtype)) != HCMS_OK) return st;
-    if (M < 0 || N < 0 || N > (1 << 20)) return fail(HCMS_ERR_SHAPE, "need M >= 0 and 0 <= N <= 2^20 (M=%d N=%d)", M, N);
+    // The last tile's rows are counted in 32 bits too.
+    if (M < 0 || M > INT32_MAX - 255 || N < 0 || N > (1 << 20))
+        return fail(HCMS_ERR_SHAPE, "need 0 <= M <= 2^31 - 256 and 0 <= N <= 2^20 (M=%d N=%d)", M, N);
     if (K < 16 || K % 16 != 0 || K > (1 << 20))
         return fail(HCMS_ERR_SHAPE, "K=%d must be a positive multiple of 16, at most 2^20", K);
     if (parts < 1 || N % (8LL * parts) != 0)

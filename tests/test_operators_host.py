@@ -334,3 +334,8 @@ def test_rows_and_tokens_that_span_more_than_63_bits_are_refused(lib):
         q = RopeHeads(A, B, xt, 64, yt, 64, 1)
         assert lib.hcms_rope(ctypes.byref(q), None, C, one(100), one(1), 1, D, 4, M, 64, 0, 0, 0, None) == ESHAPE
         assert b"span" in lib.hcms_last_error()
+
+
+def test_linear_fp8_refuses_rows_whose_last_tile_passes_32_bits(lib):
+    for M in (2 ** 31 - 1, 2 ** 31 - 255):
+        assert lib.hcms_linear_fp8(A, B, C, D, E, M, 8, 16, 1, 0, None) == ESHAPE
