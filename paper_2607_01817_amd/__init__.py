@@ -129,6 +129,9 @@ def _check(status: int) -> int:
 
 def _ints(xs):
     xs = [int(x) for x in xs]
+    for x in xs:
+        if not -2 ** 31 <= x < 2 ** 31:     # ctypes would wrap it
+            raise ValueError(f"{x} does not fit 32 bits")
     return (ctypes.c_int * max(1, len(xs)))(*xs), len(xs)
 
 

@@ -140,7 +140,8 @@ def rope_frequencies(pairs: int, base: float = 10000.0, scaling: str = "none", f
     "ntk" or "yarn" (see hcms.h, hcms_rope_frequencies).  Host only."""
     if scaling not in _SCALINGS:
         raise ValueError(f"scaling must be one of {sorted(_SCALINGS)}")
-    buf = (ctypes.c_double * max(1, pairs))()
+    (pairs,), _ = _ints([pairs])
+    buf = (ctypes.c_double * min(max(pairs, 1), 256))()     # more are refused below
     mag = ctypes.c_double()
     _check(load().hcms_rope_frequencies(pairs, float(base), _SCALINGS[scaling], float(factor),
                                         float(original_length), float(beta_fast), float(beta_slow), buf,

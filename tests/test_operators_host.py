@@ -339,3 +339,16 @@ def test_rows_and_tokens_that_span_more_than_63_bits_are_refused(lib):
 def test_linear_fp8_refuses_rows_whose_last_tile_passes_32_bits(lib):
     for M in (2 ** 31 - 1, 2 ** 31 - 255):
         assert lib.hcms_linear_fp8(A, B, C, D, E, M, 8, 16, 1, 0, None) == ESHAPE
+
+
+def test_sizes_past_32_bits_are_refused_and_not_wrapped(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="32 bits"):
+        hcms.rope_table([2 ** 32 + 4], [2])
+    with pytest.raises(ValueError, match="32 bits"):
+        hcms.rope_table_freqs([4], [2 ** 32 + 2], [1.0, 0.1])
+    with pytest.raises(ValueError, match="32 bits"):
+        hcms.rope_frequencies(2 ** 32 + 8)
+    with pytest.raises(hcms.HcmsError) as e:
+        hcms.rope_frequencies(2 ** 31 - 1)     # 16 GiB of frequencies
+    assert e.value.status == ESHAPE
