@@ -752,3 +752,41 @@ def test_rms_norm_gradient_past_the_caches(hcms, M, D, dtype):
         want += t.sum(0)
         size += t.abs().sum(0)
     _within(dw, _f64(want), 2.0 ** -24 * np.abs(_f64(want)) + 2.0 ** -17 * _f64(size), "dw")
+
+
+@pytest.mark.parametrize("M,D,dtype", [(16385, 128, BF16), (40037, 121, BF16), (33000, 64, FP32), (9001, 256, BF16),
+                                       (20003, 250, FP32), (230003, 121, BF16), (110003, 250, BF16)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_rms_norm_gradient_of_narrow_rows_in_several_passes(hcms, M, D, dtype, residual):
+    """More narrow rows than all workgroups hold at once (16384 up to D = 128, 8192 up to
+    256), so that each goes on to further rows, the last pass not full, also past the
+    caches: dx of all rows and dw against float64, dx of the first, the last and a
+    pass's edge's rows bit for bit as taken alone."""
+    log(f"[norm gradient, narrow rows] M={M} D={D} {dtype} residual={residual}")
+    at_once = 16384 if D <= 128 else 8192
+    assert M > at_once and M % at_once
+    g = torch.Generator("cuda").manual_seed(M + D)
+    dy, x, r, dh = (torch.randn(M, D, generator=g, dtype=dtype, device="cuda") for _ in range(4))
+    w = (1 + 0.1 * torch.randn(D, generator=g, device="cuda")).to(dtype)
+    if not residual:
+        r = dh = None
+
+    def rows(t, a):
+        return None if t is None else t[a].clone()
+
+    dx, dw = hcms.rms_norm_backward(dy, x, w, 1e-5, r, dh)
+    for a in (slice(0, 100), slice(at_once - 50, at_once + 50), slice(M - 100, M)):
+        alone, _ = hcms.rms_norm_backward(rows(dy, a), rows(x, a), w, 1e-5, rows(r, a), rows(dh, a))
+        assert torch.equal(bits(dx[a].contiguous()), bits(alone)), a
+    h = x.double() if r is None else x.double() + r.double()
+    rs = 1 / (h.square().mean(1, keepdim=True) + 1e-5).sqrt()
+    n, gw = h * rs, dy.double() * w.double()
+    want = rs * (gw - n * (gw * n).mean(1, keepdim=True))
+    size = rs * (gw.abs() + n.abs() * (gw * n).abs().mean(1, keepdim=True))
+    if dh is not None:
+        want, size = want + dh.double(), size + dh.double().abs()
+    worst = ((dx.double() - want).abs() / (ROUND[dtype] * want.abs() + 2.0 ** -17 * size)).max().item()
+    log(f"    dx: worst error {worst:.3f} of its bound")
+    assert worst <= 1.0
+    t = dy.double() * n
+    _within(dw, _f64(t.sum(0)), ROUND[dtype] * np.abs(_f64(t.sum(0))) + 2.0 ** -17 * _f64(t.abs().sum(0)), "dw")
