@@ -790,3 +790,35 @@ def test_rms_norm_gradient_of_narrow_rows_in_several_passes(hcms, M, D, dtype, r
     assert worst <= 1.0
     t = dy.double() * n
     _within(dw, _f64(t.sum(0)), ROUND[dtype] * np.abs(_f64(t.sum(0))) + 2.0 ** -17 * _f64(t.abs().sum(0)), "dw")
+
+
+@pytest.mark.parametrize("M,D", [(57000, 2603), (17003, 8000), (9001, 16384), (9003, 16379)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_rms_norm_past_the_caches_with_ragged_rows_and_in_8_bits(hcms, M, D, residual):
+    """bf16 rows whose last chunk of 8 the end cuts (2603, 16379), and whole ones in 8
+    bits too, on tensors past twice the caches: the first and last rows bit for bit as
+    taken alone, and the last ones against the oracle."""
+    log(f"[norm past the caches] M={M} D={D} residual={residual}")
+    g = torch.Generator("cuda").manual_seed(M + D)
+    x, r = (torch.randn(M, D, generator=g, dtype=BF16, device="cuda") for _ in range(2))
+    w = 1 + 0.1 * torch.randn(D, generator=g, device="cuda")
+    assert x.numel() * 2 * (4 if residual else 2) > 512 << 20 and D > 2048
+    n = 1100                                 # still many rows, but within the caches
+
+    def both(fn, a):
+        out = fn(x[a], w, 1e-6, residual=r[a] if residual else None)
+        return out if isinstance(out, tuple) else (out,)
+
+    whole = both(hcms.rms_norm, slice(0, M))
+    for a in (slice(0, n), slice(M - n, M)):
+        for t, alone in zip(whole, both(hcms.rms_norm, a)):
+            assert torch.equal(bits(t[a]), bits(alone)), a
+    y, h = op.rms_norm(_f64(x[-8:]), _f64(w), 1e-6, _f64(r[-8:]) if residual else None)
+    _within(whole[0][-8:], y, (ROUND[BF16] + 2.0 ** -17) * np.abs(y) + 1e-30, "y")
+    if D % 16 == 0:
+        q, s, *h = both(hcms.rms_norm_fp8, slice(0, M))
+        for a in (slice(0, n), slice(M - n, M)):
+            q1, s1, *h1 = both(hcms.rms_norm_fp8, a)
+            assert torch.equal(q[a].view(torch.uint8), q1.view(torch.uint8))
+            assert torch.equal(s[:, a].view(torch.uint8), s1.view(torch.uint8))
+            assert not residual or torch.equal(bits(h[0][a]), bits(h1[0]))
