@@ -25,8 +25,8 @@
 //
 // What bounds it.  Large products: the power limit (the matrix cores alone take
 // 8-bit operands at 3200-3500 TFLOP/s for a short while) and what is not MFMAs:
-// 56160 x 1920 x 5120 runs at 2210-2290 TFLOP/s (482-500 us) with the MFMAs busy 57 % of the
-// SIMDs' cycles at 1.86 GHz, 2.5 us of each tile's 41 its start and epilogue; 8192^3
+// 56160 x 1920 x 5120 runs at 2210-2320 TFLOP/s (476-500 us, by the card) with the MFMAs busy
+// 58 % of the SIMDs' cycles at 1.86 GHz, 2.5 us of each tile's 41 its start and epilogue; 8192^3
 // at 2700.  Each stage also moves its operands through LDS, WN times for X and WM
 // times for W, at 128 bytes per clock: 0.95 us per stage of a 256 x 256 tile against
 // 0.85 of MFMAs, which is why the waves' rectangles are large.  Few tiles: the
@@ -461,7 +461,9 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void linear_fp8_kernel(
 // li) every load is of that kind: 1 x 5120 x 5120 7.5 us, 16 rows 9.2, 32 rows 12.0.
 // So 8 lanes load a row's block of 128, and the operands pass through LDS, a place
 // of each wave's own: 4.8 us (5.4 TB/s; 7.4 with W from memory), 5.2 and 7.1; 64
-// rows 9.8, on 64 x 64 tiles, whose stages wait for each other, 12.2.  A workgroup
+// rows 9.8, on 64 x 64 tiles, whose stages wait for each other, 12.2.  From 17 rows on
+// the registers that hold X's blocks leave fewer of W's in flight (kDeep), so the
+// time grows while W's bytes do not.  A workgroup
 // takes 16 NT columns of Y and all rows (16 MT hold them), its waves the blocks of
 // k in turn, and the waves' sums are added through LDS in the order of the waves.
 // MFMA 16 x 16 x 128 (for fp32 output 16 x 16 x 32 in bf16): lane (li, g) holds 32

@@ -11,13 +11,14 @@ namespace hcms {
 // limit leaves, and with few of them busy; and the start and the epilogue of a
 // round.  `groups`: of waves, which share the stages of a tile between them and
 // add up their sums (halves the time of a long k where few tiles are at work).
-// In us, in the order of the table:
-//   56160 x 1920 x 5120   491  583  531  606  850 1043 1135  476  799
-//   1560 x 5120 x 5120     54   48   62   60   67   79   88   40   62
-//   1560 x 1920 x 5120     52   47   31   23   34   41   34   33   30
-//   1000 x 1920 x 5120     53   44   31   22   19   22   23   33   16.2
-//   512 x 512 x 4096       37   30   25   18   15   14   10.4 26   12.6
-//   1000 x 1536 x 640      10.0  8.6  8.4  6.6  5.6  6.2  8.8  8.7  6.0
+// In us, in the order of the table, on one card (from card to card the first line
+// moves by 5 %: 476 to 500 on 192 x 192):
+//   56160 x 1920 x 5120   515  592  556  624  850 1046 1128  494  832
+//   1560 x 5120 x 5120     54   48   62   61   67   79   88   41   65
+//   1560 x 1920 x 5120     52   45   30   23   33   41   34   32   31
+//   1000 x 1920 x 5120     53   43   30   22   19   23   23   32   16.7
+//   512 x 512 x 4096       37   29   23   18   15   13.4 10.4 26   12.9
+//   1000 x 1536 x 640      10.3  8.4  8.2  6.6  5.9  6.7  9.2  8.4  6.3
 struct Fp8TileCost {
     int bm, bn, per_cu, groups;
     double full, alone, fixed;
@@ -29,10 +30,10 @@ inline constexpr Fp8TileCost kFp8Tiles[] = {
     {64, 128, 1, 2, 0.335, 0.27, 2.1}};
 // For fp32 output, whose widened operands run at the bf16 rate and do not fit
 // beside the accumulators of a larger tile:
-//   56160 x 1920 x 5120   900  989 1572 1799  955
-//   1560 x 5120 x 5120    114  103  118  140   80
-//   3001 x 1000 x 1936     26.6 18.4 29.6 28.1 35.6
-//   256 x 1920 x 5120      53   32   27.5 18.7 76
+//   56160 x 1920 x 5120   950 1054 1647 1762  979
+//   1560 x 5120 x 5120    120  107  126  138   82
+//   3001 x 1000 x 1936     27.0 18.9 29.7 27.9 34.3
+//   256 x 1920 x 5120      54   32   27.5 19.3 73
 // (128 x 128 without groups, on eight waves: 1126, 117, 21.9 and 40).
 inline constexpr Fp8TileCost kFp8WideTiles[] = {
     {256, 128, 1, 1, 1.53, 1.23, 4.5}, {128, 128, 1, 2, 0.87, 0.66, 2.2}, {64, 64, 2, 1, 0.70, 0.57, 1.2},

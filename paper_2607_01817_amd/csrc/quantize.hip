@@ -11,9 +11,12 @@
 //
 // What bounds it: bytes, each element read once, whatever is made of it.  bf16,
 // read and written bytes: 56160 x 5120 by rows 146 us (5.9 TB/s), with the
-// transpose 228 (5.0); 7800 x 5120 19.4 (6.2 TB/s) and 28 (5.7); 1560 x 5120 5.5
-// and 9.4.  The rows alone have a kernel of their own, without the tile's detour:
-// 7800 x 5120 20.7 us against the tile's 22.5 for the same bytes.
+// transpose 230 (5.0); 7800 x 5120 19.4 (6.2 TB/s) and 28 (5.7); 1560 x 5120 5.4
+// and 9.4; fp32 7800 x 5120 by rows 29.5 (6.8).  The rows alone have a kernel of
+// their own, without the tile's detour; by rows, that kernel and the tile: bf16
+// 56160 x 5120 146 and 159 us, 7800 x 5120 19.5 and 20.5, 7800 x 1920 8.4 and 10.3,
+// 1560 x 5120 5.4 and 6.7 (56160 x 640 20.4 and 19.8; fp32 7800 x 5120 29.6 and 30.4,
+// 56160 x 5120 262 and 254).
 #include "fp8.h"
 #include "hcms_internal.h"
 
