@@ -805,6 +805,136 @@ HCMS_API int hcms_rope_frequencies(int pairs, double base, int scaling, double f
 HCMS_API int hcms_rope_table_freqs(float *table, const int *grid, const int *axis_pairs, int n_axes,
                                    const double *freqs, double magnitude, void *stream);
 
+/*
+ * Norm of each query and key head vector and its rotation, in one pass: per head
+ * vector x of d elements with the side's weight w [d],
+ *   y = T (x / sqrt(mean(x^2) + eps) * w)
+ * with T the rotation of hcms_rope (which takes the same table, grid, axis_pairs,
+ * positions and layout, and the same sides, in place too), computed in fp32 and
+ * rounded once.
+ *   q_weight, k_weight : device, [d] of weight_dtype (of a side without heads: any)
+ * hcms_qk_norm_rope_backward: its gradients from its inputs, with r = 1 / sqrt(mean(x^2)
+ * + eps), n = x r and g = T^t dy:
+ *   dx = r (g w - n mean(g w n)),  dw = sum over tokens and heads of g n
+ *   dq, dk    : sides: x the gradient of the forward's output, y that of its input
+ *               (which may be the gradient itself: same address and strides)
+ *   q, k      : the forward's inputs (their y is not looked at); dk and k are given
+ *               together or not at all
+ *   dq_weight, dk_weight : device, [d] of weight_dtype (zeros for a side without
+ *               heads or tokens), or NULL
+ *   partial   : device workspace, hcms_qk_norm_rope_partials(S, heads of both sides)
+ *               rows of d floats
+ * No atomics: runs are deterministic.  Errors: as hcms_rope, plus ARG (eps).
+ * hcms_qk_norm_rope_partials is host only (errors: SHAPE).
+ */
+HCMS_API int hcms_qk_norm_rope(const hcms_rope_heads *q, const hcms_rope_heads *k, const void *q_weight,
+                               const void *k_weight, const float *table, const int *grid,
+                               const int *axis_pairs, int n_axes, const void *positions,
+                               int position_bytes, int S, int d, int layout, float eps, int dtype,
+                               int weight_dtype, void *stream);
+HCMS_API int hcms_qk_norm_rope_partials(int S, int heads);
+HCMS_API int hcms_qk_norm_rope_backward(const hcms_rope_heads *dq, const hcms_rope_heads *dk,
+                                        const hcms_rope_heads *q, const hcms_rope_heads *k,
+                                        const void *q_weight, const void *k_weight, void *dq_weight,
+                                        void *dk_weight, float *partial, const float *table,
+                                        const int *grid, const int *axis_pairs, int n_axes,
+                                        const void *positions, int position_bytes, int S, int d,
+                                        int layout, float eps, int dtype, int weight_dtype,
+                                        void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* A paged cache of keys and values in 4 bits, and attention over it          */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The cache holds keys and values of `heads` key heads of d = 64 or 128 elements in
+ * pages of `page` tokens, a multiple of 64.  Values are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4,
+ * 6 and their negatives) times a power of two for each 32 consecutive elements of a
+ * head vector, held as its exponent byte b = e + 127 (e8m0): the smallest one from
+ * 2^-126 on that brings the block's largest magnitude to at most 6.  They are rounded
+ * to the nearest, ties to the even code; a block that holds an infinity or a NaN gets
+ * the scale NaN (byte 255), and so do all its values.  With t the token's place in
+ * its chunk of 64 tokens:
+ *   k       : [pages][heads][page][d / 2]            elements 2 c and 2 c + 1 in byte c,
+ *                                                    the first in its low half
+ *   k_scale : [pages][heads][page / 64][d / 32][64]  token t at 4 (t % 16) + t / 16
+ *   v       : [pages][heads][page / 64][d / 2][64]   elements 2 c and 2 c + 1 of token t
+ *                                                    in byte [c][16 (t / 4 % 4) + 4 (t / 16) + t % 4]
+ *   v_scale : [pages][heads][page / 64][d / 32][64]  token t as in v
+ * each 16-byte aligned.  A copied page is the page.
+ *
+ * A batch of B sequences over it: sequence b holds lengths[b] tokens, token p in page
+ * page_table[b][p / page] at place p % page, and its rows of the packed tensors of a
+ * call are [starts[b], starts[b + 1]), which are its last tokens.
+ *   page_table : device, [B][W] int32;  lengths : device, [B] int32;  starts : device,
+ *                [B + 1] int32, from 0 on, not decreasing, at most the call's rows T
+ * They are read on the device: a captured call follows what they hold when it is
+ * replayed.  Lengths include the call's own rows.  Rows from starts[B] on belong to
+ * no sequence.  What breaks these rules never leads outside the buffers: a sequence
+ * longer than W pages, or with a page outside the cache among those that it reads,
+ * gives NaN rows, and tokens without a page are not appended.  T + 2 B <= 2^22, W >= 1.
+ */
+typedef struct hcms_kv_cache {
+    void *k, *v, *k_scale, *v_scale;
+    int pages, heads, d, page;
+} hcms_kv_cache;
+typedef struct hcms_kv_batch {
+    const int *page_table, *lengths, *starts;
+    int B, W;
+} hcms_kv_batch;
+/* T rows of heads: row t and head h at x + t token + h head (strides in elements, at
+   most 2^40, and all rows within 2^60). */
+typedef struct hcms_kv_rows {
+    const void *x;
+    int64_t token, head;
+} hcms_kv_rows;
+
+/*
+ * Appends the rows of k and v to the cache: row i of sequence b is its token lengths[b]
+ * - (starts[b + 1] - starts[b]) + i.  Other tokens stay as they are.  Pages that take
+ * tokens belong to one sequence each.
+ *   table : NULL (keys as they come), or device: keys are turned by it as hcms_rope
+ *           turns them (grid, axis_pairs, n_axes, layout), for a token's place p in its
+ *           sequence at place p of the row-major grid, or
+ *   positions : at these coordinates: device, [T][n_axes] of position_bytes 4 or 8
+ *           (NULL and 0: none).  A position outside the grid makes the turned blocks NaN.
+ *           The rotation is exact to fp64, so a key next to the border of two 4-bit
+ *           values falls on its own side.
+ *   k_held, v_held : NULL, or device, [T][heads][d]: what the cache then holds of the
+ *           rows (of rows that are not appended: as it was)
+ * Buffers of rows need the alignment of their elements only.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, ARG, HIP.
+ */
+HCMS_API int hcms_append_kv(const hcms_kv_cache *cache, const hcms_kv_batch *batch,
+                            const hcms_kv_rows *k, const hcms_kv_rows *v, void *k_held, void *v_held,
+                            int T, const float *table, const int *grid, const int *axis_pairs,
+                            int n_axes, const void *positions, int position_bytes, int layout,
+                            int dtype, void *stream);
+
+/*
+ * Attention of T packed rows of H query heads over the cache; H is a multiple of its
+ * heads, and query heads h of a key head are the H / heads ones in a row.  Row i of a
+ * sequence with n rows and length L sees the tokens [begin, end) of it:
+ *   end = L - n + i + 1 (causal) or L,  begin = max(0, end - window) (window 0: 0)
+ *   out[t][h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale <q[t][h], k_j>)
+ * A row that sees nothing gives zeros; rows of no sequence stay as they were.  A value
+ * that is not finite (or a block's scale of 2^126 or more) makes the rows that see it
+ * NaN, and no others.
+ *   out       : device, [T][H][d]
+ *   workspace : device, hcms_cache_attention_workspace bytes for the same cache, B, W, T,
+ *               H and window (none for 0), 16-byte aligned
+ * Scores, maxima, sums and outputs are kept in fp32.  bf16: probabilities are rounded to
+ * bf16 for their product; fp32: products are those of fp32.  Deterministic: work is split
+ * along long sequences by sizes alone, and joined in a fixed order.
+ * T H / heads <= 2^26, finite scale.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, ARG (scale,
+ * window < 0), HIP.  hcms_cache_attention_workspace is host only (errors: NULL, SHAPE,
+ * DTYPE).
+ */
+HCMS_API int hcms_cache_attention_workspace(const hcms_kv_cache *cache, const hcms_kv_batch *batch, int T,
+                                            int H, int window, int dtype, int64_t *bytes);
+HCMS_API int hcms_cache_attention(const hcms_kv_cache *cache, const hcms_kv_batch *batch,
+                                  const hcms_kv_rows *q, void *out, void *workspace, int T, int H,
+                                  float scale, int causal, int window, int dtype, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

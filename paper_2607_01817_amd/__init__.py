@@ -108,6 +108,13 @@ def load():
         "hcms_rope": ([vp, vp, vp, ip, ip, i, vp, i, i, i, i, i, i, vp], i),
         "hcms_rope_frequencies": ([i, d, i, d, d, d, d, dp, dp], i),
         "hcms_rope_table_freqs": ([vp, ip, ip, i, dp, d, vp], i),
+        "hcms_qk_norm_rope": ([vp, vp, vp, vp, vp, ip, ip, i, vp, i, i, i, i, f, i, i, vp], i),
+        "hcms_qk_norm_rope_partials": ([i, i], i),
+        "hcms_qk_norm_rope_backward": ([vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ip, ip, i, vp, i, i, i, i, f,
+                                        i, i, vp], i),
+        "hcms_append_kv": ([vp, vp, vp, vp, vp, vp, i, vp, ip, ip, i, vp, i, i, i, vp], i),
+        "hcms_cache_attention_workspace": ([vp, vp, i, i, i, i, ctypes.POINTER(i64)], i),
+        "hcms_cache_attention": ([vp, vp, vp, vp, vp, i, i, f, i, i, i, vp], i),
         "hcms_layer_forward": ([vp, vp, vp, vp, vp, ip, ip, i, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                 i, i, i, i, i, f, ip, i, i, i, vp, vp, vp], i),
     }
@@ -770,6 +777,7 @@ class HcmsAttention(torch.autograd.Function):
         return dq, dk, dv, None, None, None, None, None
 
 
-from .operators import (E4M3, E8M0, SCALE_BLOCK, Fp8Linear, RmsNorm, Rope, linear_fp8,  # noqa: E402,F401
-                        quantize_fp8, rms_norm, rms_norm_backward, rms_norm_fp8, rope,
-                        rope_frequencies, rope_table_freqs)
+from .operators import (E4M3, E8M0, SCALE_BLOCK, Fp8Linear, KvCache, QkNormRope, RmsNorm, Rope,  # noqa: E402,F401
+                        append_kv, cache_attention, kv_cache, linear_fp8, qk_norm_rope, quantize_fp8,
+                        rms_norm, rms_norm_backward, rms_norm_fp8, rope, rope_frequencies,
+                        rope_table_freqs)

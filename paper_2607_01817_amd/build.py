@@ -24,8 +24,9 @@ TORCH_SOURCE = "torch_ops.cpp"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-SOURCES = ["api.cpp", "ops.cpp", "model.cpp", "pack.hip", "attention.hip", "attention_bwd.hip", "linear.hip",
-           "linear_fp8.hip", "quantize.hip", "rmsnorm.hip", "rope.hip"]
+SOURCES = ["api.cpp", "ops.cpp", "cache_ops.cpp", "model.cpp", "pack.hip", "attention.hip", "attention_bwd.hip", "linear.hip",
+           "linear_fp8.hip", "quantize.hip", "rmsnorm.hip", "rope.hip", "head_norm.hip", "kv_append.hip",
+           "cache_attention.hip"]
 
 COMMON = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -17,6 +17,7 @@ inline int hip_fail(hipError_t e, const char *what) {
 
 inline int elem_bytes(int dtype) { return dtype == HCMS_BF16 ? 2 : 4; }
 
+inline bool aligned(const void *p, int n) { return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(n - 1)) == 0; }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Byte ranges [a, a + na) and [b, b + nb) overlap.
@@ -25,6 +26,28 @@ inline bool overlaps(const void *a, int64_t na, const void *b, int64_t nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + static_cast<uintptr_t>(nb) && y < x + static_cast<uintptr_t>(na);
 }
+
+// A buffer of a call, from its first to its last byte.
+struct Buffer {
+    const char *name;
+    const void *p;
+    int64_t bytes;
+};
+
+// No output overlaps an input or another output.
+inline int check_disjoint(const Buffer *out, int n_out, const Buffer *in, int n_in) {
+    for (int i = 0; i < n_out; ++i) {
+        for (int j = 0; j < n_in; ++j)
+            if (out[i].p && in[j].p && overlaps(out[i].p, out[i].bytes, in[j].p, in[j].bytes))
+                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out[i].name, in[j].name);
+        for (int j = i + 1; j < n_out; ++j)
+            if (out[i].p && out[j].p && overlaps(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
+                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out[i].name, out[j].name);
+    }
+    return HCMS_OK;
+}
+
+inline constexpr int64_t kMostSpan = 1LL << 60;   // elements from a buffer's first to its last one, or nearly
 
 inline int check_dtype(int dtype) {
     if (dtype != HCMS_BF16 && dtype != HCMS_FP32)

@@ -158,6 +158,58 @@ struct RopeFreqs {
 hipError_t launch_rope_table_freqs(float *table, const RopeAxes &ax, const RopeFreqs &freqs, double magnitude,
                                    hipStream_t stream);
 
+// Norm of each query and key head vector (weights qw and kw [d], fp32 or bf16)
+// and its rotation, as launch_rope's.
+hipError_t launch_head_norm(const RopeSide &q, const RopeSide &k, const void *qw, const void *kw, bool w_f32,
+                            const float *table, const RopeAxes &ax, const void *positions, bool pos64, int S, int d,
+                            int R, bool half, float eps, int dtype, hipStream_t stream);
+// Its backward: q and k as the forward read them, dq and dk the gradients of its
+// outputs (x) and of its inputs (y); dqw and dkw [d] (NULL: not wanted); partial:
+// head_norm_partials(S, heads of both sides) rows of 2 d floats.
+int head_norm_partials(int64_t S, int64_t heads);
+hipError_t launch_head_norm_backward(const RopeSide &q, const RopeSide &k, const RopeSide &dq, const RopeSide &dk,
+                                     const void *qw, const void *kw, bool w_f32, void *dqw, void *dkw, float *partial,
+                                     const float *table, const RopeAxes &ax, const void *positions, bool pos64, int S,
+                                     int d, int R, bool half, float eps, int dtype, hipStream_t stream);
+
+// A paged cache of keys and values in 4 bits (kv_cache.h), and a batch of
+// sequences over it: W page ids and a length for each of B sequences, and the
+// first of its rows in packed tensors (B + 1 of them).
+struct KvCache {
+    unsigned char *k, *v, *k_scale, *v_scale;
+    int pages, heads, d, page;
+};
+struct KvBatch {
+    const int *page_table, *lengths, *starts;
+    int B, W;
+};
+// Packed rows of heads to append: keys (turned by the table, if there is one) and
+// values, and, unless NULL, what the cache then holds of them.
+struct KvRows {
+    const void *k, *v;
+    int64_t k_token, k_head, v_token, v_head;
+    void *k_held, *v_held;
+    int T;
+};
+hipError_t launch_append_kv(const KvCache &cache, const KvBatch &batch, const KvRows &rows, const float *table,
+                            const RopeAxes &ax, const void *positions, bool pos64, int R, bool half, int dtype,
+                            hipStream_t stream);
+
+// Attention of T packed rows of H query heads over the cache.  workspace:
+// cache_attention_workspace bytes for the same sizes (none for 0).
+struct KvQueries {
+    const void *q;
+    int64_t q_token, q_head;
+    void *out;
+    int T, H;
+    float scale;
+    bool causal;
+    int window;   // 0: none
+};
+int64_t cache_attention_workspace(const KvCache &cache, const KvBatch &batch, int T, int H, int window, int dtype);
+hipError_t launch_cache_attention(const KvCache &cache, const KvBatch &batch, const KvQueries &rows, void *workspace,
+                                  int dtype, hipStream_t stream);
+
 // Largest D of the norm and its backward (rows are held in registers).
 int rms_norm_max_width();
 // RMS norm of rows of h = x + r (r NULL: h = x, not stored), in the storage

@@ -1,0 +1,217 @@
+// Appends keys and values to the paged 4-bit cache, the keys turned by their
+// positions on the way:
+//   k' = T k,  s = the smallest power of two with max |block of 32| <= 6 s,
+//   codes = k' / s rounded to the nearest e2m1 value, ties to the even code.
+// The rotation is in fp64 and rounded to fp32 with the lost bits kept in the last
+// one, so that a value next to the border of two codes falls on its own side of it.
+//
+// What bounds it: bytes, k and v once in, 17 / 32 of a byte for each element out,
+// and what the cache holds of them where it is asked for.  A workgroup takes the new
+// tokens of a sequence in one chunk of 64 of the cache, for one head: keys are
+// written as they come, values and scales are put in order in LDS.
+#include <algorithm>
+
+#include "fp8.h"
+#include "hcms_internal.h"
+#include "kv_cache.h"
+#include "rope_place.h"
+
+namespace hcms {
+namespace {
+
+using fp8::f32x8;
+using kv::kChunk;
+
+// x in fp32 rounded toward zero with the last bit set if that lost something: on
+// the same side as x of every value of fewer bits.  Past fp32's range: infinity.
+__device__ inline float to_odd(double x) {
+    const float f = static_cast<float>(x);
+    if (static_cast<double>(f) == x || __builtin_isinf(f)) return f;
+    unsigned b = __builtin_bit_cast(unsigned, f);
+    if (__builtin_fabs(static_cast<double>(f)) > __builtin_fabs(x)) --b;
+    return __builtin_bit_cast(float, b | 1u);
+}
+
+__device__ inline unsigned max4(unsigned v) {   // over four lanes that share a scale
+    v = max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x4E, 0xF, 0xF, true)));
+    return max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0xB1, 0xF, 0xF, true)));
+}
+
+// 8 elements in 4 bits and their block's scale; called by all four lanes of a block.
+struct Coded {
+    unsigned bytes, scale;
+};
+__device__ inline Coded encode(const float (&x)[8]) {
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, fp8::magnitude(x[i]));
+    Coded c;
+    c.scale = kv::scale_byte(max4(top));
+    const float by = fp8::inverse_scale(c.scale);
+    c.bytes = 0;
+    if (c.scale == 255u) return c;
+#define HCMS_PAIR(i) \
+    c.bytes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c.bytes, x[2 * i] * by, x[2 * i + 1] * by, 1.0f, i)
+    HCMS_PAIR(0);
+    HCMS_PAIR(1);
+    HCMS_PAIR(2);
+    HCMS_PAIR(3);
+#undef HCMS_PAIR
+    return c;
+}
+// The values that they stand for.
+__device__ inline f32x8 decode(const Coded &c) {
+    const float s = c.scale == 255u ? __builtin_nanf("") : __builtin_bit_cast(float, c.scale << 23);
+    f32x8 v;
+#define HCMS_PAIR(i) \
+    { \
+        const auto p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c.bytes, 1.0f, i); \
+        v[2 * i] = p[0] * s; \
+        v[2 * i + 1] = p[1] * s; \
+    }
+    HCMS_PAIR(0)
+    HCMS_PAIR(1)
+    HCMS_PAIR(2)
+    HCMS_PAIR(3)
+#undef HCMS_PAIR
+    return v;
+}
+
+// D: elements of a head vector; T: type of the rows; HALF: layout of the pairs.
+template <typename T, int D, bool HALF>
+__global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch batch, KvRows rows, const float *table,
+                                                        RopeAxes ax, const void *positions, bool pos64, int R) {
+    constexpr int UNITS = D / 8, PER = 256 / UNITS;   // lanes of a token, tokens at once
+    __shared__ unsigned char values[D / 2][kChunk];
+    __shared__ unsigned char scales[2][D / kv::kBlock][kChunk];
+    int b, tile;
+    kv::Sequence seq;
+    const int64_t room = static_cast<int64_t>(batch.W) * cache.page;
+    // Chunks that hold new tokens with a place.
+    const auto chunks = [&](const kv::Sequence &s) {
+        const int64_t lo = max(s.length - s.n, 0), hi = min(static_cast<int64_t>(s.length), room);
+        return lo >= hi ? 0 : static_cast<int>((hi + kChunk - 1) / kChunk - lo / kChunk);
+    };
+    if (!kv::find_tile(batch, rows.T, blockIdx.x, chunks, &b, &tile, &seq)) return;
+    const int head = blockIdx.y;
+    const int lo = max(seq.length - seq.n, 0);
+    const int chunk = lo / kChunk + tile;
+    const int64_t at = static_cast<int64_t>(chunk) * kChunk;   // the chunk's first token
+    const int t0 = static_cast<int>(max<int64_t>(lo - at, 0));
+    const int t1 = static_cast<int>(min<int64_t>(min(static_cast<int64_t>(seq.length), room) - at, kChunk));
+    const int per_page = cache.page / kChunk;
+    const int page = batch.page_table[static_cast<int64_t>(b) * batch.W + chunk / per_page];
+    if (page < 0 || page >= cache.pages) return;   // the whole workgroup
+    const int64_t block = (static_cast<int64_t>(page) * cache.heads + head) * per_page + chunk % per_page;
+    unsigned char *const ck = cache.k + block * kChunk * (D / 2);
+    unsigned char *const cv = cache.v + block * kChunk * (D / 2);
+    unsigned char *const sk = cache.k_scale + block * kChunk * (D / kv::kBlock);
+    unsigned char *const sv = cache.v_scale + block * kChunk * (D / kv::kBlock);
+    const int u = threadIdx.x % UNITS, e = u * 8;
+
+    // Every lane of a group of UNITS takes the same way, so those of a block stay together.
+    for (int t = t0 + static_cast<int>(threadIdx.x) / UNITS; t < t1; t += PER) {
+        const int place = static_cast<int>(at + t);
+        const int64_t row = seq.first + (place - (seq.length - seq.n));
+        const T *k = static_cast<const T *>(rows.k) + row * rows.k_token + head * rows.k_head;
+        const T *v = static_cast<const T *>(rows.v) + row * rows.v_token + head * rows.v_head;
+        const f32x8 xk = widen(load_raw(k + e)), xv = widen(load_raw(v + e));
+        float y[8], z[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            y[i] = xk[i];
+            z[i] = xv[i];
+        }
+        // Comparisons with R anew for each token, as those of rope_place.
+        int turning = R;
+        asm volatile("" : "+s"(turning));
+        if (e < turning) {
+            const RopePlace rp = rope_place(ax, positions, pos64, row, place);
+            if constexpr (HALF) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (e + i >= turning) continue;
+                    const bool first = e + i < turning / 2;
+                    const int p = first ? e + i : e + i - turning / 2;
+                    const float2 cs = rope_entry(table, rp, p);
+                    const double mine = xk[i], other = static_cast<float>(k[first ? p + turning / 2 : p]);
+                    y[i] = to_odd(mine * cs.x + (first ? -other : other) * cs.y);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    if (e + i >= turning) continue;
+                    const float2 cs = rope_entry(table, rp, (e + i) / 2);
+                    const double a = xk[i], o = xk[i + 1];
+                    y[i] = to_odd(a * cs.x - o * cs.y);
+                    y[i + 1] = to_odd(a * cs.y + o * cs.x);
+                }
+            }
+        }
+        const Coded ek = encode(y), ev = encode(z);
+        *reinterpret_cast<unsigned *>(ck + t * (D / 2) + e / 2) = ek.bytes;
+        const int pv = kv::value_place(t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) values[e / 2 + i][pv] = static_cast<unsigned char>(ev.bytes >> (8 * i));
+        if (u % 4 == 0) {
+            scales[0][u / 4][kv::key_scale_place(t)] = static_cast<unsigned char>(ek.scale);
+            scales[1][u / 4][pv] = static_cast<unsigned char>(ev.scale);
+        }
+        if (rows.k_held) {
+            const int64_t o = (row * cache.heads + head) * D + e;
+            store_8(static_cast<T *>(rows.k_held) + o, decode(ek));
+            store_8(static_cast<T *>(rows.v_held) + o, decode(ev));
+        }
+    }
+    __syncthreads();
+    // What the chunk's other tokens hold stays: whole chunks in 16 bytes, else byte by byte.
+    if (t1 - t0 == kChunk) {
+        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+        constexpr int V16 = D / 2 * kChunk / 16, S16 = D / kv::kBlock * kChunk / 16;
+        for (int i = threadIdx.x; i < V16; i += 256)
+            reinterpret_cast<u32x4 *>(cv)[i] = reinterpret_cast<const u32x4 *>(&values[0][0])[i];
+        for (int i = threadIdx.x; i < 2 * S16; i += 256) {
+            const int side = i / S16, j = i % S16;
+            reinterpret_cast<u32x4 *>(side ? sv : sk)[j] = reinterpret_cast<const u32x4 *>(&scales[side][0][0])[j];
+        }
+        return;
+    }
+    const int n = t1 - t0;
+    for (int i = threadIdx.x; i < n * (D / 2); i += 256) {
+        const int t = t0 + i % n, c = i / n, p = kv::value_place(t);
+        cv[c * kChunk + p] = values[c][p];
+    }
+    for (int i = threadIdx.x; i < n * 2 * (D / kv::kBlock); i += 256) {
+        const int t = t0 + i % n, j = i / n, side = j % 2, c = j / 2;
+        const int p = side ? kv::value_place(t) : kv::key_scale_place(t);
+        (side ? sv : sk)[c * kChunk + p] = scales[side][c][p];
+    }
+}
+
+}  // namespace
+
+hipError_t launch_append_kv(const KvCache &cache, const KvBatch &batch, const KvRows &rows, const float *table,
+                            const RopeAxes &ax, const void *positions, bool pos64, int R, bool half, int dtype,
+                            hipStream_t stream) {
+    if (rows.T == 0 || batch.B == 0 || cache.heads == 0) return hipSuccess;
+    // Chunks that n new tokens of a sequence can lie in: at most n, and n / 64 + 2.
+    const int64_t tiles = std::min<int64_t>(rows.T, rows.T / kChunk + 2LL * batch.B);
+    const dim3 grid(static_cast<unsigned>(tiles), cache.heads);
+#define HCMS_RUN(T, D, HALF) \
+    append_kv_kernel<T, D, HALF><<<grid, 256, 0, stream>>>(cache, batch, rows, table, ax, positions, pos64, R)
+#define HCMS_TYPED(T) \
+    if (cache.d == 128 && half) HCMS_RUN(T, 128, true); \
+    else if (cache.d == 128) HCMS_RUN(T, 128, false); \
+    else if (half) HCMS_RUN(T, 64, true); \
+    else HCMS_RUN(T, 64, false)
+    if (dtype == 0) {
+        HCMS_TYPED(__bf16);
+    } else {
+        HCMS_TYPED(float);
+    }
+#undef HCMS_TYPED
+#undef HCMS_RUN
+    return hipGetLastError();
+}
+
+}  // namespace hcms

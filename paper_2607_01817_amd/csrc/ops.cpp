@@ -1,6 +1,7 @@
 // C entry points of the operators beside the chunk loop: the RMS norm, the
-// 8-bit product with its quantisation, and the rotary positions.  Declarations
-// and the contract live in hcms.h.
+// 8-bit product with its quantisation, the rotary positions, and the norm and
+// rotation of head vectors in one pass.  Declarations and the contract live in
+// hcms.h.
 #include "hcms.h"
 
 #include <hip/hip_runtime.h>
@@ -16,38 +17,17 @@
 
 namespace {
 
+using hcms::aligned;
 using hcms::aligned16;
+using hcms::Buffer;
+using hcms::check_disjoint;
 using hcms::check_dtype;
 using hcms::elem_bytes;
 using hcms::fail;
 using hcms::hip_fail;
+using hcms::kMostSpan;
 using hcms::ok;
-using hcms::overlaps;
 using hcms::rope_axes;
-
-bool aligned(const void *p, int n) { return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(n - 1)) == 0; }
-
-// A buffer of a call, from its first to its last byte.
-struct Buffer {
-    const char *name;
-    const void *p;
-    int64_t bytes;
-};
-
-// No output overlaps an input or another output.
-int check_disjoint(const Buffer *out, int n_out, const Buffer *in, int n_in) {
-    for (int i = 0; i < n_out; ++i) {
-        for (int j = 0; j < n_in; ++j)
-            if (out[i].p && in[j].p && overlaps(out[i].p, out[i].bytes, in[j].p, in[j].bytes))
-                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out[i].name, in[j].name);
-        for (int j = i + 1; j < n_out; ++j)
-            if (out[i].p && out[j].p && overlaps(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
-                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out[i].name, out[j].name);
-    }
-    return HCMS_OK;
-}
-
-constexpr int64_t kMostSpan = 1LL << 60;   // elements from a buffer's first to its last one, or nearly
 
 // Bytes from the first to the last element of M rows of n, ld elements apart.
 int64_t span_bytes(int64_t M, int64_t n, int64_t ld, int es) { return M < 1 ? 0 : ((M - 1) * ld + n) * es; }
@@ -55,15 +35,19 @@ int64_t span_bytes(int64_t M, int64_t n, int64_t ld, int es) { return M < 1 ? 0 
 // Bytes of the scales of `rows` rows (or blocks of rows) of K elements.
 int64_t scale_bytes(int64_t rows, int64_t K) { return (K + hcms::fp8::kGroup - 1) / hcms::fp8::kGroup * rows * 4; }
 
+int check_eps(float eps) {
+    if (!std::isfinite(eps) || eps < 0.0f)
+        return fail(HCMS_ERR_ARG, "eps must be finite and >= 0 (got %g)", static_cast<double>(eps));
+    return HCMS_OK;
+}
+
 int check_norm_shape(int M, int D, int dtype, int weight_dtype, float eps) {
     int st;
     if ((st = check_dtype(dtype)) != HCMS_OK || (st = check_dtype(weight_dtype)) != HCMS_OK) return st;
     if (M < 0) return fail(HCMS_ERR_SHAPE, "need M >= 0 (M=%d)", M);
     if (D < 8 || D > hcms::rms_norm_max_width())
         return fail(HCMS_ERR_SHAPE, "D=%d must be in [8, %d]", D, hcms::rms_norm_max_width());
-    if (!std::isfinite(eps) || eps < 0.0f)
-        return fail(HCMS_ERR_ARG, "eps must be finite and >= 0 (got %g)", static_cast<double>(eps));
-    return HCMS_OK;
+    return check_eps(eps);
 }
 
 // M rows of n elements, ld apart: the span of any type's bytes fits 63 bits.
@@ -103,6 +87,110 @@ int norm_forward(const void *x, const void *residual, const void *weight, void *
                                                ldx, ldr, eps, dtype, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "rms norm launch");
     return ok();
+}
+
+// A rotation's axes, positions and head dimension; *pairs of it and its table's
+// *entries.
+int check_rotation(const int *grid, const int *axis_pairs, int n_axes, const void *positions, int position_bytes, int S,
+                   int d, int layout, hcms::RopeAxes *ax, int64_t *pairs, int64_t *entries) {
+    int64_t tokens = 0;
+    const int st = rope_axes(grid, axis_pairs, n_axes, ax, &tokens, pairs, entries);
+    if (st != HCMS_OK) return st;
+    if (S < 0 || d < 2 || d > 2 * hcms::kRopeMaxPairs || 2 * *pairs > d)
+        return fail(HCMS_ERR_SHAPE, "need S >= 0, 2 <= d <= %d and at most d / 2 pairs (S=%d d=%d pairs=%lld)",
+                    2 * hcms::kRopeMaxPairs, S, d, static_cast<long long>(*pairs));
+    if (layout != HCMS_ROPE_INTERLEAVED && layout != HCMS_ROPE_HALF) return fail(HCMS_ERR_ARG, "layout=%d", layout);
+    if (positions ? position_bytes != 4 && position_bytes != 8 : position_bytes != 0)
+        return fail(HCMS_ERR_ARG, "position_bytes=%d: 4 or 8 with positions, 0 without", position_bytes);
+    if (!positions && S > tokens)
+        return fail(HCMS_ERR_SHAPE, "S=%d tokens on a grid of %lld", S, static_cast<long long>(tokens));
+    return HCMS_OK;
+}
+
+// The heads of a side that are read: count, address, strides, alignment.
+int check_heads_in(const hcms_rope_heads *h, int S, int es, int i) {
+    if (h->heads < 0 || h->heads > (1 << 16)) return fail(HCMS_ERR_SHAPE, "heads=%d", h->heads);
+    if (!h->x) return fail(HCMS_ERR_NULL, "the %s heads' input is NULL", i ? "key" : "query");
+    for (const int64_t s : {h->x_token, h->x_head})
+        if (s < 0 || s > (1LL << 40)) return fail(HCMS_ERR_SHAPE, "strides must be in [0, 2^40]");
+    if (S > 1 && h->x_token > kMostSpan / (S - 1))
+        return fail(HCMS_ERR_SHAPE, "%d tokens %lld elements apart span more than 2^60 elements", S,
+                    static_cast<long long>(h->x_token));
+    if (!aligned(h->x, es)) return fail(HCMS_ERR_ALIGN, "buffers must be aligned to their elements");
+    return HCMS_OK;
+}
+
+// What a norm of head vectors reads beside them: the table, the positions and the
+// weights of the sides that have heads.
+int check_norm_rope_inputs(const hcms_rope_heads *const (&sides)[2], const void *const (&weights)[2], const float *table,
+                           int64_t entries, const void *positions, int position_bytes, int n_axes, int S, int d,
+                           int weight_dtype, Buffer *in) {
+    if (S > 0 && !table) return fail(HCMS_ERR_NULL, "table is NULL");
+    if (!aligned(table, 8) || !aligned(positions, position_bytes ? position_bytes : 1))
+        return fail(HCMS_ERR_ALIGN, "table must be 8-byte aligned, positions to their elements");
+    in[0] = {"table", table, entries * 8};
+    in[1] = {"positions", positions, static_cast<int64_t>(S) * n_axes * position_bytes};
+    static const char *const name[2] = {"q_weight", "k_weight"};
+    const int ws = elem_bytes(weight_dtype);
+    for (int i = 0; i < 2; ++i) {
+        const bool used = S > 0 && sides[i] && sides[i]->heads > 0;
+        if (used && !weights[i]) return fail(HCMS_ERR_NULL, "%s is NULL", name[i]);
+        if (!aligned(weights[i], ws)) return fail(HCMS_ERR_ALIGN, "%s must be aligned to its elements", name[i]);
+        in[2 + i] = {name[i], weights[i], static_cast<int64_t>(d) * ws};
+    }
+    return HCMS_OK;
+}
+
+// The sides of a rotation, queries and keys, of S tokens and head vectors of d, whose
+// outputs overlap none of the `shared` buffers, nor each other or the other's input.
+int check_sides(const hcms_rope_heads *q, const hcms_rope_heads *k, const Buffer *shared, int n_shared, int S, int d,
+                int dtype, hcms::RopeSide (&side)[2]) {
+    int st;
+    const int es = elem_bytes(dtype);
+    const hcms_rope_heads *sides[2] = {q, k};
+    static const char *const in_name[2] = {"q", "k"}, *const out_name[2] = {"the rotated q", "the rotated k"};
+    hcms::HeadBlock in[2], out[2];   // of the sides that have heads
+    bool in_place[2] = {};
+    for (int i = 0; i < 2; ++i) {
+        const hcms_rope_heads *h = sides[i];
+        if (!h) continue;
+        if (h->heads < 0 || h->heads > (1 << 16)) return fail(HCMS_ERR_SHAPE, "heads=%d", h->heads);
+        if (h->heads == 0 || S == 0) continue;
+        if (!h->x || !h->y) return fail(HCMS_ERR_NULL, "the %s heads' input or output is NULL", i ? "key" : "query");
+        const int64_t strides[4] = {h->x_token, h->x_head, h->y_token, h->y_head};
+        for (const int64_t s : strides)
+            if (s < 0 || s > (1LL << 40)) return fail(HCMS_ERR_SHAPE, "strides must be in [0, 2^40]");
+        for (const int64_t s : {h->x_token, h->y_token})
+            if (S > 1 && s > kMostSpan / (S - 1))
+                return fail(HCMS_ERR_SHAPE, "%d tokens %lld elements apart span more than 2^60 elements", S,
+                            static_cast<long long>(s));
+        // Distinct heads and tokens of the output do not overlap.
+        const bool by_token = h->y_token >= h->y_head;
+        if (h->y_head < d && h->heads > 1) return fail(HCMS_ERR_SHAPE, "output heads overlap");
+        if (S > 1 && (h->y_token < d || (by_token ? h->y_token < (h->heads - 1) * h->y_head + d
+                                                  : h->y_head < (S - 1) * h->y_token + d && h->heads > 1)))
+            return fail(HCMS_ERR_SHAPE, "output tokens overlap");
+        if (!aligned(h->x, es) || !aligned(h->y, es))
+            return fail(HCMS_ERR_ALIGN, "buffers must be aligned to their elements");
+        side[i] = {h->x, h->y, h->x_token, h->x_head, h->y_token, h->y_head, h->heads};
+        in[i] = {reinterpret_cast<uintptr_t>(h->x), h->x_token * es, h->x_head * es, S, d * es, h->heads};
+        out[i] = {reinterpret_cast<uintptr_t>(h->y), h->y_token * es, h->y_head * es, S, d * es, h->heads};
+        // The strides of a single token and of a single head say nothing.
+        in_place[i] = h->x == h->y && (S == 1 || h->x_token == h->y_token) && (h->heads == 1 || h->x_head == h->y_head);
+        const Buffer y[] = {{out_name[i], h->y, hcms::heads_span(out[i])}};
+        if ((st = check_disjoint(y, 1, shared, n_shared)) != HCMS_OK) return st;
+    }
+    // A head is written by one workgroup and read by it alone.  Heads are compared, not
+    // a side's first and last byte: both sides may lie in one packed buffer.
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2; ++j) {
+            if (side[i].H == 0 || side[j].H == 0) continue;
+            if ((i != j || !in_place[i]) && hcms::heads_meet(out[i], in[j]))
+                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out_name[i], in_name[j]);
+            if (i < j && hcms::heads_meet(out[i], out[j]))
+                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out_name[i], out_name[j]);
+        }
+    return HCMS_OK;
 }
 
 }  // namespace
@@ -290,71 +378,123 @@ int hcms_rope(const hcms_rope_heads *q, const hcms_rope_heads *k, const float *t
     if (!q) return fail(HCMS_ERR_NULL, "q is NULL");
     if ((st = check_dtype(dtype)) != HCMS_OK) return st;
     hcms::RopeAxes ax;
-    int64_t tokens = 0, pairs = 0, entries = 0;
-    if ((st = rope_axes(grid, axis_pairs, n_axes, &ax, &tokens, &pairs, &entries)) != HCMS_OK) return st;
-    if (S < 0 || d < 2 || d > 2 * hcms::kRopeMaxPairs || 2 * pairs > d)
-        return fail(HCMS_ERR_SHAPE, "need S >= 0, 2 <= d <= %d and at most d / 2 pairs (S=%d d=%d pairs=%lld)",
-                    2 * hcms::kRopeMaxPairs, S, d, static_cast<long long>(pairs));
-    if (layout != HCMS_ROPE_INTERLEAVED && layout != HCMS_ROPE_HALF) return fail(HCMS_ERR_ARG, "layout=%d", layout);
-    if (positions ? position_bytes != 4 && position_bytes != 8 : position_bytes != 0)
-        return fail(HCMS_ERR_ARG, "position_bytes=%d: 4 or 8 with positions, 0 without", position_bytes);
-    if (!positions && S > tokens)
-        return fail(HCMS_ERR_SHAPE, "S=%d tokens on a grid of %lld", S, static_cast<long long>(tokens));
-    const int es = elem_bytes(dtype);
-    const hcms_rope_heads *sides[2] = {q, k};
-    static const char *const in_name[2] = {"q", "k"}, *const out_name[2] = {"the rotated q", "the rotated k"};
-    hcms::RopeSide side[2] = {};
-    hcms::HeadBlock in[2], out[2];   // of the sides that have heads
-    bool in_place[2] = {};
+    int64_t pairs = 0, entries = 0;
+    if ((st = check_rotation(grid, axis_pairs, n_axes, positions, position_bytes, S, d, layout, &ax, &pairs, &entries)) !=
+        HCMS_OK)
+        return st;
     if (S > 0 && !table) return fail(HCMS_ERR_NULL, "table is NULL");
     if (!aligned(table, 8) || !aligned(positions, position_bytes ? position_bytes : 1))
         return fail(HCMS_ERR_ALIGN, "table must be 8-byte aligned, positions to their elements");
     const Buffer shared[2] = {{"table", table, entries * 8},
                               {"positions", positions, static_cast<int64_t>(S) * n_axes * position_bytes}};
-    for (int i = 0; i < 2; ++i) {
-        const hcms_rope_heads *h = sides[i];
-        if (!h) continue;
-        if (h->heads < 0 || h->heads > (1 << 16)) return fail(HCMS_ERR_SHAPE, "heads=%d", h->heads);
-        if (h->heads == 0 || S == 0) continue;
-        if (!h->x || !h->y) return fail(HCMS_ERR_NULL, "the %s heads' input or output is NULL", i ? "key" : "query");
-        const int64_t strides[4] = {h->x_token, h->x_head, h->y_token, h->y_head};
-        for (const int64_t s : strides)
-            if (s < 0 || s > (1LL << 40)) return fail(HCMS_ERR_SHAPE, "strides must be in [0, 2^40]");
-        for (const int64_t s : {h->x_token, h->y_token})
-            if (S > 1 && s > kMostSpan / (S - 1))
-                return fail(HCMS_ERR_SHAPE, "%d tokens %lld elements apart span more than 2^60 elements", S,
-                            static_cast<long long>(s));
-        // Distinct heads and tokens of the output do not overlap.
-        const bool by_token = h->y_token >= h->y_head;
-        if (h->y_head < d && h->heads > 1) return fail(HCMS_ERR_SHAPE, "output heads overlap");
-        if (S > 1 && (h->y_token < d || (by_token ? h->y_token < (h->heads - 1) * h->y_head + d
-                                                  : h->y_head < (S - 1) * h->y_token + d && h->heads > 1)))
-            return fail(HCMS_ERR_SHAPE, "output tokens overlap");
-        if (!aligned(h->x, es) || !aligned(h->y, es))
-            return fail(HCMS_ERR_ALIGN, "buffers must be aligned to their elements");
-        side[i] = {h->x, h->y, h->x_token, h->x_head, h->y_token, h->y_head, h->heads};
-        in[i] = {reinterpret_cast<uintptr_t>(h->x), h->x_token * es, h->x_head * es, S, d * es, h->heads};
-        out[i] = {reinterpret_cast<uintptr_t>(h->y), h->y_token * es, h->y_head * es, S, d * es, h->heads};
-        // The strides of a single token and of a single head say nothing.
-        in_place[i] = h->x == h->y && (S == 1 || h->x_token == h->y_token) && (h->heads == 1 || h->x_head == h->y_head);
-        const Buffer y[] = {{out_name[i], h->y, hcms::heads_span(out[i])}};
-        if ((st = check_disjoint(y, 1, shared, 2)) != HCMS_OK) return st;
-    }
-    // A head is written by one workgroup and read by it alone.  Heads are compared, not
-    // a side's first and last byte: both sides may lie in one packed buffer.
-    for (int i = 0; i < 2; ++i)
-        for (int j = 0; j < 2; ++j) {
-            if (side[i].H == 0 || side[j].H == 0) continue;
-            if ((i != j || !in_place[i]) && hcms::heads_meet(out[i], in[j]))
-                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out_name[i], in_name[j]);
-            if (i < j && hcms::heads_meet(out[i], out[j]))
-                return fail(HCMS_ERR_ALIAS, "%s overlaps %s", out_name[i], out_name[j]);
-        }
+    hcms::RopeSide side[2] = {};
+    if ((st = check_sides(q, k, shared, 2, S, d, dtype, side)) != HCMS_OK) return st;
     if (S == 0 || side[0].H + side[1].H == 0) return ok();
     const hipError_t e = hcms::launch_rope(side[0], side[1], table, ax, positions, position_bytes == 8, S, d,
                                            static_cast<int>(2 * pairs), layout == HCMS_ROPE_HALF, inverse != 0, dtype,
                                            static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "rope launch");
+    return ok();
+}
+
+int hcms_qk_norm_rope(const hcms_rope_heads *q, const hcms_rope_heads *k, const void *q_weight, const void *k_weight,
+                      const float *table, const int *grid, const int *axis_pairs, int n_axes, const void *positions,
+                      int position_bytes, int S, int d, int layout, float eps, int dtype, int weight_dtype,
+                      void *stream) {
+    int st;
+    if (!q) return fail(HCMS_ERR_NULL, "q is NULL");
+    if ((st = check_dtype(dtype)) != HCMS_OK || (st = check_dtype(weight_dtype)) != HCMS_OK) return st;
+    hcms::RopeAxes ax;
+    int64_t pairs = 0, entries = 0;
+    if ((st = check_rotation(grid, axis_pairs, n_axes, positions, position_bytes, S, d, layout, &ax, &pairs, &entries)) !=
+        HCMS_OK)
+        return st;
+    if ((st = check_eps(eps)) != HCMS_OK) return st;
+    Buffer shared[4];
+    const hcms_rope_heads *const sides[2] = {q, k};
+    const void *const weights[2] = {q_weight, k_weight};
+    if ((st = check_norm_rope_inputs(sides, weights, table, entries, positions, position_bytes, n_axes, S, d,
+                                     weight_dtype, shared)) != HCMS_OK)
+        return st;
+    hcms::RopeSide side[2] = {};
+    if ((st = check_sides(q, k, shared, 4, S, d, dtype, side)) != HCMS_OK) return st;
+    if (S == 0 || side[0].H + side[1].H == 0) return ok();
+    const hipError_t e = hcms::launch_head_norm(side[0], side[1], q_weight, k_weight, weight_dtype == HCMS_FP32, table,
+                                                ax, positions, position_bytes == 8, S, d, static_cast<int>(2 * pairs),
+                                                layout == HCMS_ROPE_HALF, eps, dtype, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "head norm launch");
+    return ok();
+}
+
+int hcms_qk_norm_rope_partials(int S, int heads) {
+    if (S < 0 || heads < 0) return fail(HCMS_ERR_SHAPE, "need S >= 0 and heads >= 0 (S=%d heads=%d)", S, heads);
+    ok();
+    return hcms::head_norm_partials(S, heads);
+}
+
+int hcms_qk_norm_rope_backward(const hcms_rope_heads *dq, const hcms_rope_heads *dk, const hcms_rope_heads *q,
+                               const hcms_rope_heads *k, const void *q_weight, const void *k_weight, void *dq_weight,
+                               void *dk_weight, float *partial, const float *table, const int *grid,
+                               const int *axis_pairs, int n_axes, const void *positions, int position_bytes, int S,
+                               int d, int layout, float eps, int dtype, int weight_dtype, void *stream) {
+    int st;
+    if (!dq || !q) return fail(HCMS_ERR_NULL, "dq or q is NULL");
+    if ((dk == nullptr) != (k == nullptr)) return fail(HCMS_ERR_NULL, "k and dk are given together or not at all");
+    if ((st = check_dtype(dtype)) != HCMS_OK || (st = check_dtype(weight_dtype)) != HCMS_OK) return st;
+    hcms::RopeAxes ax;
+    int64_t pairs = 0, entries = 0;
+    if ((st = check_rotation(grid, axis_pairs, n_axes, positions, position_bytes, S, d, layout, &ax, &pairs, &entries)) !=
+        HCMS_OK)
+        return st;
+    if ((st = check_eps(eps)) != HCMS_OK) return st;
+    if (dq->heads != q->heads || (k && dk->heads != k->heads))
+        return fail(HCMS_ERR_SHAPE, "the gradients have other heads than their inputs");
+    Buffer in[6];
+    const hcms_rope_heads *const sides[2] = {q, k};
+    const void *const weights[2] = {q_weight, k_weight};
+    if ((st = check_norm_rope_inputs(sides, weights, table, entries, positions, position_bytes, n_axes, S, d,
+                                     weight_dtype, in)) != HCMS_OK)
+        return st;
+    // The inputs' heads: read only, within the strides that outputs have.
+    hcms::RopeSide of[2] = {}, side[2] = {};
+    static const char *const name[2] = {"q", "k"};
+    const int es = elem_bytes(dtype);
+    for (int i = 0; i < 2; ++i) {
+        in[4 + i] = {name[i], nullptr, 0};
+        const hcms_rope_heads *h = sides[i];
+        if (!h || h->heads == 0 || S == 0) continue;
+        if ((st = check_heads_in(h, S, es, i)) != HCMS_OK) return st;
+        of[i] = {h->x, nullptr, h->x_token, h->x_head, 0, 0, h->heads};
+        const hcms::HeadBlock b{reinterpret_cast<uintptr_t>(h->x), h->x_token * es, h->x_head * es, S, d * es, h->heads};
+        in[4 + i].p = h->x;
+        in[4 + i].bytes = hcms::heads_span(b);
+    }
+    if ((st = check_sides(dq, dk, in, 6, S, d, dtype, side)) != HCMS_OK) return st;
+    const int heads = side[0].H + side[1].H, ws = elem_bytes(weight_dtype);
+    if (heads > 0 && !partial) return fail(HCMS_ERR_NULL, "partial is NULL");
+    if (!aligned(dq_weight, ws) || !aligned(dk_weight, ws) || !aligned(partial, 4))
+        return fail(HCMS_ERR_ALIGN, "buffers must be aligned to their elements");
+    const int64_t wb = static_cast<int64_t>(d) * ws;
+    const Buffer out[] = {{"dq_weight", dq_weight, wb},
+                          {"dk_weight", dk_weight, wb},
+                          {"partial", partial, 4LL * hcms::head_norm_partials(S, heads) * d}};
+    if ((st = check_disjoint(out, 3, in, 6)) != HCMS_OK) return st;
+    // The gradients' heads, from first to last byte.
+    Buffer heads_of[4];
+    for (int i = 0; i < 2; ++i) {
+        const hcms::HeadBlock g{0, side[i].x_token * es, side[i].x_head * es, S, d * es, side[i].H};
+        const hcms::HeadBlock o{0, side[i].y_token * es, side[i].y_head * es, S, d * es, side[i].H};
+        const bool some = side[i].H > 0;
+        heads_of[2 * i] = {i ? "dk" : "dq", side[i].x, some ? hcms::heads_span(g) : 0};
+        heads_of[2 * i + 1] = {i ? "the gradient of k" : "the gradient of q", side[i].y, some ? hcms::heads_span(o) : 0};
+    }
+    if ((st = check_disjoint(out, 3, heads_of, 4)) != HCMS_OK) return st;
+    if (!dq_weight && !dk_weight && heads == 0) return ok();
+    const hipError_t e = hcms::launch_head_norm_backward(
+        of[0], of[1], side[0], side[1], q_weight, k_weight, weight_dtype == HCMS_FP32, dq_weight, dk_weight, partial,
+        table, ax, positions, position_bytes == 8, S, d, static_cast<int>(2 * pairs), layout == HCMS_ROPE_HALF, eps,
+        dtype, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "head norm backward launch");
     return ok();
 }
 

@@ -15,6 +15,7 @@
 // coordinates are read once for all of them.
 #include "fp8.h"
 #include "hcms_internal.h"
+#include "rope_place.h"
 
 namespace hcms {
 namespace {
@@ -93,36 +94,12 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeSide qs, RopeSide ks, con
     fetch(hb);   // ahead of the coordinates and the table: 8 tokens of 48 heads 3.5 us, behind them 3.8
     float c[NP], s[NP];
     if (rotates) {
-        int row[kRopeMaxAxes] = {};
-        bool inside = true;
-        if (positions) {
-            for (int a = 0; a < ax.n_axes; ++a) {
-                const int64_t i = token * ax.n_axes + a;
-                const int64_t at = pos64 ? static_cast<const int64_t *>(positions)[i]
-                                         : static_cast<int64_t>(static_cast<const int *>(positions)[i]);
-                const bool ok = at >= 0 && at < ax.grid[a];
-                inside = inside && ok;
-                row[a] = ax.tab_off[a] + (ok ? static_cast<int>(at) : 0) * ax.pairs[a] - ax.pair_start[a];
-            }
-        } else {
-            int rest = static_cast<int>(token);
-            for (int a = ax.n_axes - 1; a >= 0; --a) {
-                const int cc = rest % ax.grid[a];
-                rest /= ax.grid[a];
-                row[a] = ax.tab_off[a] + cc * ax.pairs[a] - ax.pair_start[a];
-            }
-        }
+        const RopePlace at = rope_place(ax, positions, pos64, token, static_cast<int>(token));
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int p = p0 + i;
-            int at = row[0];
-#pragma unroll
-            for (int a = 1; a < kRopeMaxAxes; ++a)
-                if (a < ax.n_axes && p >= ax.pair_start[a]) at = row[a];
-            const float2 cs = reinterpret_cast<const float2 *>(table)[at + p];
-            // A position outside the grid: NaN, never another position's angle.
-            c[i] = inside ? cs.x : __builtin_nanf("");
-            s[i] = inside ? (inverse ? -cs.y : cs.y) : __builtin_nanf("");
+            const float2 cs = rope_entry(table, at, p0 + i);
+            c[i] = cs.x;
+            s[i] = inverse ? -cs.y : cs.y;
         }
     }
     for (int h0 = hb; h0 < he; h0 += kAhead) {

@@ -456,29 +456,36 @@ void check_rope(const Tensor &q, const MaybeTensor &k, const Tensor &table, cons
     }
 }
 
-py::object rope(const Tensor &q, const MaybeTensor &k, const Tensor &table, const std::vector<int64_t> &grid,
-                const std::vector<int64_t> &pairs, const MaybeTensor &positions, bool half, bool inverse,
-                const std::optional<std::pair<MaybeTensor, MaybeTensor>> &out) {
-    const Axes ax(grid, pairs);
-    check_rope(q, k, table, ax, positions);
+// Outputs of queries and keys: new, or a caller's.
+using MaybeSides = std::optional<std::pair<MaybeTensor, MaybeTensor>>;
+std::pair<Tensor, MaybeTensor> outputs(const Tensor &q, const MaybeTensor &k, const MaybeSides &out) {
     Tensor yq;
     MaybeTensor yk;
-    if (out) {
-        value(out->first && (!k || out->second), "out must be the tensors (q, k)");
-        yq = *out->first;
-        check_side(yq, q, "out's q");
-        VALUE(yq.sizes() == q.sizes(), "out's q must match q");
-        writable(yq, "out's q");
-        if (k) {
-            yk = out->second;
-            check_side(*yk, q, "out's k");
-            VALUE(yk->sizes() == k->sizes(), "out's k must match k");
-            writable(*yk, "out's k");
-        }
-    } else {
+    if (!out) {
         yq = empty(q.sizes(), q.scalar_type(), q);
         if (k) yk = empty(k->sizes(), k->scalar_type(), *k);
+        return {yq, yk};
     }
+    value(out->first && (!k || out->second), "out must be the tensors (q, k)");
+    yq = *out->first;
+    check_side(yq, q, "out's q");
+    VALUE(yq.sizes() == q.sizes(), "out's q must match q");
+    writable(yq, "out's q");
+    if (k) {
+        yk = out->second;
+        check_side(*yk, q, "out's k");
+        VALUE(yk->sizes() == k->sizes(), "out's k must match k");
+        writable(*yk, "out's k");
+    }
+    return {yq, yk};
+}
+
+py::object rope(const Tensor &q, const MaybeTensor &k, const Tensor &table, const std::vector<int64_t> &grid,
+                const std::vector<int64_t> &pairs, const MaybeTensor &positions, bool half, bool inverse,
+                const MaybeSides &out) {
+    const Axes ax(grid, pairs);
+    check_rope(q, k, table, ax, positions);
+    const auto [yq, yk] = outputs(q, k, out);
     launch_rope(q, k, yq, yk, table, ax, positions, half, inverse);
     if (out) {
         wrote(yq);
@@ -529,6 +536,241 @@ py::object rope_train(const Tensor &q, const MaybeTensor &k, const Tensor &table
     return k ? py::object(py::make_tuple(out[0], out[1])) : py::cast(out[0]);
 }
 
+// ---------------------------------------------------------------------------
+// Norm and rotation of head vectors
+// ---------------------------------------------------------------------------
+void check_head_weights(const Tensor &q, const MaybeTensor &k, const Tensor &qw, const MaybeTensor &kw) {
+    value(k.has_value() == kw.has_value(), "k and k_weight are given together or not at all");
+    const auto one = [&](const Tensor &w, const char *name) {
+        VALUE(w.dim() == 1 && w.size(0) == q.size(2), name, " must be [d]");
+        dtype_of(w);
+        VALUE(w.scalar_type() == qw.scalar_type(), "the weights must have one dtype");
+        dense(w, name);
+        with(q, w, name);
+    };
+    one(qw, "q_weight");
+    if (kw) one(*kw, "k_weight");
+}
+
+void launch_norm_rope(const Tensor &q, const MaybeTensor &k, const Tensor &yq, const MaybeTensor &yk, const Tensor &qw,
+                      const MaybeTensor &kw, const Tensor &table, const Axes &ax, const MaybeTensor &positions, bool half,
+                      double eps) {
+    const hcms_rope_heads a = side(q, yq);
+    hcms_rope_heads b;
+    if (k) b = side(*k, *yk);
+    void *const stream = stream_of(q);
+    run([&] {
+        return hcms_qk_norm_rope(&a, k ? &b : nullptr, ptr(qw), ptr(kw), static_cast<const float *>(ptr(table)), ax.grid,
+                                 ax.pairs, ax.n, ptr(positions), positions ? positions->element_size() : 0, q.size(0),
+                                 q.size(2), half ? HCMS_ROPE_HALF : HCMS_ROPE_INTERLEAVED, static_cast<float>(eps),
+                                 dtype_of(q), dtype_of(qw), stream);
+    });
+}
+
+py::object qk_norm_rope(const Tensor &q, const MaybeTensor &k, const Tensor &qw, const MaybeTensor &kw,
+                        const Tensor &table, const std::vector<int64_t> &grid, const std::vector<int64_t> &pairs,
+                        const MaybeTensor &positions, bool half, double eps, const MaybeSides &out) {
+    const Axes ax(grid, pairs);
+    check_rope(q, k, table, ax, positions);
+    check_head_weights(q, k, qw, kw);
+    const auto [yq, yk] = outputs(q, k, out);
+    launch_norm_rope(q, k, yq, yk, qw, kw, table, ax, positions, half, eps);
+    if (out) {
+        wrote(yq);
+        wrote(yk);
+    }
+    return k ? py::object(py::make_tuple(yq, *yk)) : py::cast(yq);
+}
+
+struct QkNormRope : torch::autograd::Function<QkNormRope> {
+    static variable_list forward(AutogradContext *ctx, const Tensor &q, const MaybeTensor &k, const Tensor &qw,
+                                 const MaybeTensor &kw, const Tensor &table, const std::vector<int64_t> &grid,
+                                 const std::vector<int64_t> &pairs, const MaybeTensor &positions, bool half, double eps) {
+        ctx->set_materialize_grads(false);
+        ctx->save_for_backward({q, k.value_or(Tensor()), qw, kw.value_or(Tensor()), table, positions.value_or(Tensor())});
+        ctx->saved_data["grid"] = grid;
+        ctx->saved_data["pairs"] = pairs;
+        ctx->saved_data["half"] = half;
+        ctx->saved_data["eps"] = eps;
+        const auto [yq, yk] = outputs(q, k, std::nullopt);
+        launch_norm_rope(q, k, yq, yk, qw, kw, table, Axes(grid, pairs), positions, half, eps);
+        return k ? variable_list{yq, *yk} : variable_list{yq};
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list g) {
+        once();
+        const auto saved = ctx->get_saved_variables();
+        const Axes ax(ctx->saved_data["grid"].toIntVector(), ctx->saved_data["pairs"].toIntVector());
+        const Tensor *const x[2] = {&saved[0], &saved[1]}, *const w[2] = {&saved[2], &saved[3]};
+        Tensor dx[2], dw[2];
+        hcms_rope_heads grad[2], in[2];
+        int64_t heads = 0;
+        for (size_t i = 0; i < 2; ++i) {
+            const bool there = i < g.size() && g[i].defined();   // else this side was not used
+            if (there && g[i].numel() && g[i].stride(2) != 1) g[i] = g[i].contiguous();
+            if (there) {
+                dx[i] = empty(x[i]->sizes(), x[i]->scalar_type(), *x[i]);
+                dw[i] = empty(w[i]->sizes(), w[i]->scalar_type(), *w[i]);
+                grad[i] = side(g[i], dx[i]);
+                in[i] = side(*x[i], *x[i]);
+                heads += x[i]->size(1);
+            } else {
+                grad[i] = in[i] = hcms_rope_heads{};
+            }
+        }
+        if (dx[0].defined() || dx[1].defined()) {
+            const Tensor &q = saved[0], &any = dw[0].defined() ? saved[2] : saved[3];
+            const int rows = hcms_qk_norm_rope_partials(q.size(0), heads);
+            check(rows);
+            const Tensor partial = empty({rows, q.size(2)}, at::kFloat, q);
+            const MaybeTensor positions = maybe(saved[5]);
+            const auto p = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+            void *const stream = stream_of(q);
+            run([&] {
+                return hcms_qk_norm_rope_backward(
+                    &grad[0], &grad[1], &in[0], &in[1], p(saved[2]), p(saved[3]), p(dw[0]), p(dw[1]),
+                    static_cast<float *>(ptr(partial)), static_cast<const float *>(ptr(saved[4])), ax.grid, ax.pairs, ax.n,
+                    ptr(positions), positions ? positions->element_size() : 0, q.size(0), q.size(2),
+                    ctx->saved_data["half"].toBool() ? HCMS_ROPE_HALF : HCMS_ROPE_INTERLEAVED,
+                    static_cast<float>(ctx->saved_data["eps"].toDouble()), dtype_of(q), dtype_of(any), stream);
+            });
+        }
+        return {dx[0], dx[1], dw[0], dw[1], Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+
+py::object qk_norm_rope_train(const Tensor &q, const MaybeTensor &k, const Tensor &qw, const MaybeTensor &kw,
+                              const Tensor &table, const std::vector<int64_t> &grid, const std::vector<int64_t> &pairs,
+                              const MaybeTensor &positions, bool half, double eps) {
+    check_rope(q, k, table, Axes(grid, pairs), positions);
+    check_head_weights(q, k, qw, kw);
+    const variable_list out = QkNormRope::apply(q, k, qw, kw, table, grid, pairs, positions, half, eps);
+    return k ? py::object(py::make_tuple(out[0], out[1])) : py::cast(out[0]);
+}
+
+// ---------------------------------------------------------------------------
+// Paged cache in 4 bits
+// ---------------------------------------------------------------------------
+constexpr int64_t kKvChunk = 64, kKvBlock = 32;
+
+using CacheTensors = std::tuple<Tensor, Tensor, Tensor, Tensor>;
+
+hcms_kv_cache check_cache(const CacheTensors &c, const Tensor &x) {
+    const auto &[k, v, ks, vs] = c;
+    VALUE(k.dim() == 4, "the cache's k must be [pages][heads][page][d / 2]");
+    const int64_t pages = k.size(0), heads = k.size(1), page = k.size(2), half = k.size(3);
+    VALUE(page % kKvChunk == 0, "a page must have a multiple of ", kKvChunk, " tokens (got ", page, ")");
+    const int64_t chunks = page / kKvChunk, blocks = 2 * half / kKvBlock;
+    expect(k, {pages, heads, page, half}, at::kByte, "the cache's k");
+    expect(v, {pages, heads, chunks, half, kKvChunk}, at::kByte, "the cache's v");
+    expect(ks, {pages, heads, chunks, blocks, kKvChunk}, kE8M0, "k_scale");
+    expect(vs, {pages, heads, chunks, blocks, kKvChunk}, kE8M0, "v_scale");
+    for (const auto &[t, name] : {std::pair(&k, "the cache's k"), {&v, "the cache's v"}, {&ks, "k_scale"}, {&vs, "v_scale"}}) {
+        dense(*t, name);
+        with(x, *t, name);
+    }
+    return {ptr(k), ptr(v), ptr(ks), ptr(vs), int_of(pages, "pages"), int_of(heads, "heads"), int_of(2 * half, "d"),
+            int_of(page, "page")};
+}
+
+hcms_kv_batch check_batch(const Tensor &pages, const Tensor &lengths, const Tensor &starts, const Tensor &x) {
+    VALUE(pages.dim() == 2, "page_table must be [B][W]");
+    const int64_t B = pages.size(0), W = pages.size(1);
+    const auto one = [&](const Tensor &t, at::IntArrayRef shape, const char *name) {
+        if (t.scalar_type() != at::kInt) throw py::type_error(text(name, " must be an int32 tensor"));
+        expect(t, shape, at::kInt, name);
+        dense(t, name);
+        with(x, t, name);
+    };
+    one(pages, {B, W}, "page_table");
+    one(lengths, {B}, "lengths");
+    one(starts, {B + 1}, "starts");
+    return {static_cast<const int *>(ptr(pages)), static_cast<const int *>(ptr(lengths)),
+            static_cast<const int *>(ptr(starts)), int_of(B, "B"), int_of(W, "W")};
+}
+
+hcms_kv_rows check_kv_rows(const Tensor &x, const char *name) {
+    VALUE(x.dim() == 3, name, " must be [T][heads][d]");
+    VALUE(x.numel() == 0 || x.size(2) == 1 || x.stride(2) == 1, "the head vectors of ", name, " must be contiguous");
+    on_gpu(x, name);
+    int_of(x.size(0), "T");
+    int_of(x.size(1), "heads");
+    return {ptr(x), x.stride(0), x.stride(1)};
+}
+
+py::object append_kv(const Tensor &k, const Tensor &v, const CacheTensors &cache, const Tensor &page_table,
+                     const Tensor &lengths, const Tensor &starts, const MaybeTensor &table,
+                     const std::vector<int64_t> &grid, const std::vector<int64_t> &pairs, const MaybeTensor &positions,
+                     bool half, bool held) {
+    const hcms_kv_rows kr = check_kv_rows(k, "k"), vr = check_kv_rows(v, "v");
+    const int type = dtype_of(k);
+    const hcms_kv_cache c = check_cache(cache, k);
+    const hcms_kv_batch b = check_batch(page_table, lengths, starts, k);
+    VALUE(k.size(1) == c.heads && k.size(2) == c.d, "k must be [T][", c.heads, "][", c.d, "] as the cache's heads");
+    VALUE(v.sizes() == k.sizes() && v.scalar_type() == k.scalar_type(), "v must match k");
+    with(k, v, "v");
+    std::optional<Axes> ax;
+    if (table) {
+        ax.emplace(grid, pairs);
+        expect(*table, {ax->entries, 2}, at::kFloat, "table");
+        dense(*table, "table");
+        with(k, *table, "table");
+    }
+    if (positions) {
+        value(table.has_value(), "positions are given without a table");
+        if (positions->scalar_type() != at::kInt && positions->scalar_type() != at::kLong)
+            throw py::type_error("positions must be an int32 or int64 tensor");
+        const int64_t T = k.size(0);
+        const bool one = ax->n == 1 && positions->dim() == 1 && positions->size(0) == T;
+        value(one || (positions->dim() == 2 && positions->size(0) == T && positions->size(1) == ax->n),
+              "positions must be [T] or [T][axes]");
+        dense(*positions, "positions");
+        with(k, *positions, "positions");
+    }
+    MaybeTensor hk, hv;
+    if (held) {
+        hk = empty(k.sizes(), k.scalar_type(), k);
+        hv = empty(k.sizes(), k.scalar_type(), k);
+    }
+    void *const stream = stream_of(k);
+    run([&] {
+        return hcms_append_kv(&c, &b, &kr, &vr, ptr(hk), ptr(hv), k.size(0), static_cast<const float *>(ptr(table)),
+                              ax ? ax->grid : nullptr, ax ? ax->pairs : nullptr, ax ? ax->n : 0, ptr(positions),
+                              positions ? positions->element_size() : 0, half ? HCMS_ROPE_HALF : HCMS_ROPE_INTERLEAVED,
+                              type, stream);
+    });
+    wrote(std::get<0>(cache));
+    wrote(std::get<1>(cache));
+    wrote(std::get<2>(cache));
+    wrote(std::get<3>(cache));
+    return held ? py::object(py::make_tuple(*hk, *hv)) : py::none();
+}
+
+Tensor cache_attention(const Tensor &q, const CacheTensors &cache, const Tensor &page_table, const Tensor &lengths,
+                       const Tensor &starts, std::optional<double> scale, bool causal, int64_t window,
+                       const MaybeTensor &out) {
+    const hcms_kv_rows rows = check_kv_rows(q, "q");
+    const int type = dtype_of(q);
+    const hcms_kv_cache c = check_cache(cache, q);
+    const hcms_kv_batch b = check_batch(page_table, lengths, starts, q);
+    VALUE(q.size(2) == c.d, "q must be [T][H][", c.d, "] as the cache's heads");
+    value(window >= 0, "window must not be negative");
+    const int w = window > INT32_MAX ? 0 : static_cast<int>(window);   // longer than any sequence
+    const int T = static_cast<int>(q.size(0)), H = static_cast<int>(q.size(1));
+    const Tensor y = output(out, q.sizes(), q.scalar_type(), q, "out");
+    int64_t bytes = 0;
+    check(hcms_cache_attention_workspace(&c, &b, T, H, w, type, &bytes));
+    MaybeTensor workspace;
+    if (bytes > 0) workspace = empty({bytes}, at::kByte, q);
+    void *const stream = stream_of(q);
+    run([&] {
+        return hcms_cache_attention(&c, &b, &rows, ptr(y), ptr(workspace), T, H,
+                                    static_cast<float>(scale.value_or(1.0 / std::sqrt(static_cast<double>(c.d)))), causal,
+                                    w, type, stream);
+    });
+    wrote(out);
+    return y;
+}
+
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
@@ -541,4 +783,8 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
     m.def("fp8_linear_train", &fp8_linear_train);
     m.def("rope", &rope);
     m.def("rope_train", &rope_train);
+    m.def("qk_norm_rope", &qk_norm_rope);
+    m.def("qk_norm_rope_train", &qk_norm_rope_train);
+    m.def("append_kv", &append_kv);
+    m.def("cache_attention", &cache_attention);
 }

@@ -1,6 +1,8 @@
-"""Operators beside the chunk loop: the root-mean-square norm, 8-bit products
-and rotary positions, forward and backward (the C ABI's hcms_rms_norm*,
-hcms_quantize_fp8, hcms_linear_fp8 and hcms_rope*).
+"""Operators beside the chunk loop: the root-mean-square norm, 8-bit products and
+rotary positions, and the norm and rotation of query and key heads in one pass,
+forward and backward; a paged cache of keys and values in 4 bits and attention over
+it (the C ABI's hcms_rms_norm*, hcms_quantize_fp8, hcms_linear_fp8, hcms_rope*,
+hcms_qk_norm_rope*, hcms_append_kv and hcms_cache_attention*).
 
 8-bit tensors are ``float8_e4m3fn`` values with power-of-two scales held as
 ``float8_e8m0fnu``, one for each block of 128 elements of a row or of 128 x 128,
@@ -20,6 +22,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -27,6 +30,7 @@ from . import _PKG, _check, _gpu_device, _ints, _table_rows, load
 
 E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 SCALE_BLOCK = 128
+KV_CHUNK, KV_BLOCK = 64, 32   # tokens of a chunk of the cache, elements that share a scale
 _HALF = {"interleaved": False, "half": True}
 _SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
@@ -36,6 +40,24 @@ class RopeHeads(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_token", ctypes.c_int64),
                 ("x_head", ctypes.c_int64), ("y_token", ctypes.c_int64), ("y_head", ctypes.c_int64),
                 ("heads", ctypes.c_int)]
+
+
+class KvCachePointers(ctypes.Structure):
+    """hcms_kv_cache of the C ABI."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int), ("heads", ctypes.c_int), ("d", ctypes.c_int),
+                ("page", ctypes.c_int)]
+
+
+class KvBatch(ctypes.Structure):
+    """hcms_kv_batch of the C ABI."""
+    _fields_ = [("page_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("B", ctypes.c_int), ("W", ctypes.c_int)]
+
+
+class KvRows(ctypes.Structure):
+    """hcms_kv_rows of the C ABI."""
+    _fields_ = [("x", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
 @functools.lru_cache(maxsize=None)
@@ -202,3 +224,95 @@ class Rope:
     @staticmethod
     def apply(q, k, table, grid, axis_pairs, positions=None, layout="interleaved"):
         return _ops().rope_train(q, k, table, grid, axis_pairs, positions, _half(layout))
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight: torch.Tensor, k_weight: torch.Tensor | None,
+                 table: torch.Tensor, grid, axis_pairs, positions: torch.Tensor | None = None,
+                 layout: str = "interleaved", eps: float = 1e-6, out=None, *, stream=None):
+    """Norm of each query and key head vector and its rotation in one pass: as
+    :func:`rms_norm` of the head vectors (weights [d], one for the queries and one for
+    the keys), then :func:`rope`, rounded once.  q [S][H][d] and k [S][Hk][d] (or
+    None, with no weight) have any strides of tokens and heads; ``table``, ``grid``,
+    ``axis_pairs``, ``positions``, ``layout`` and ``out`` are those of :func:`rope`.
+    Returns (q, k), or q."""
+    if stream is not None:
+        return _under(stream, qk_norm_rope, q, k, q_weight, k_weight, table, grid, axis_pairs, positions, layout, eps,
+                      out)
+    return _ops().qk_norm_rope(q, k, q_weight, k_weight, table, grid, axis_pairs, positions, _half(layout), eps, out)
+
+
+class QkNormRope:
+    """Autograd over :func:`qk_norm_rope`: ``QkNormRope.apply(q, k, q_weight, k_weight,
+    table, grid, axis_pairs, positions, layout, eps)`` returns (q, k), or q without
+    keys.  The inputs are kept for the backward."""
+
+    @staticmethod
+    def apply(q, k, q_weight, k_weight, table, grid, axis_pairs, positions=None, layout="interleaved", eps=1e-6):
+        return _ops().qk_norm_rope_train(q, k, q_weight, k_weight, table, grid, axis_pairs, positions, _half(layout),
+                                         eps)
+
+
+class KvCache(NamedTuple):
+    """A paged cache of keys and values in 4 bits (layout: hcms.h, hcms_kv_cache):
+    uint8 ``k`` [pages][heads][page][d / 2] and ``v`` [pages][heads][page / 64][d / 2][64],
+    with ``k_scale`` and ``v_scale`` [pages][heads][page / 64][d / 32][64] of
+    float8_e8m0fnu.  :func:`kv_cache` makes one."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def kv_cache(pages: int, heads: int, d: int, page: int = 64, device="cuda", *, stream=None) -> KvCache:
+    """A cache of ``pages`` pages of ``page`` tokens (a multiple of 64) for ``heads``
+    key heads of ``d`` = 64 or 128 elements, all zeros: 17 / 32 of a byte for each
+    element.  ``device`` is the current one (that of ``stream``)."""
+    if stream is not None:
+        return _under(stream, kv_cache, pages, heads, d, page, device)
+    device = _gpu_device(device)
+    (pages, heads, d, page), _ = _ints([pages, heads, d, page])
+    if pages < 1 or heads < 1 or d not in (64, 128) or page < KV_CHUNK or page % KV_CHUNK:
+        raise ValueError(f"need pages >= 1, heads >= 1, d 64 or 128 and a page of a multiple of {KV_CHUNK} tokens "
+                         f"(got {pages}, {heads}, {d}, {page})")
+
+    def zeros(*shape):
+        return torch.zeros((pages, heads) + shape, dtype=torch.uint8, device=device)
+
+    chunks = page // KV_CHUNK
+    return KvCache(zeros(page, d // 2), zeros(chunks, d // 2, KV_CHUNK),
+                   zeros(chunks, d // KV_BLOCK, KV_CHUNK).view(E8M0), zeros(chunks, d // KV_BLOCK, KV_CHUNK).view(E8M0))
+
+
+def append_kv(k: torch.Tensor, v: torch.Tensor, cache: KvCache, page_table: torch.Tensor, lengths: torch.Tensor,
+              starts: torch.Tensor, table: torch.Tensor | None = None, grid=None, axis_pairs=None,
+              positions: torch.Tensor | None = None, layout: str = "interleaved", held: bool = False, *, stream=None):
+    """Appends packed rows k and v [T][heads][d], any strides of rows and heads, to
+    ``cache``.  Sequence b of the batch holds ``lengths``[b] tokens, these included,
+    token p in page ``page_table``[b][p // page]; rows ``starts``[b] to ``starts``[b + 1]
+    are its last ones (int32 [B][W], [B] and [B + 1], read on the device; pages that take
+    tokens belong to one sequence each).  With ``table`` (:func:`rope_table` of ``grid``
+    and ``axis_pairs``) the keys are turned as :func:`rope` turns them, for a token's
+    place in its sequence, or at ``positions``.  ``held``: returns (k, v) [T][heads][d],
+    what the cache now holds of the rows, such as the chunk loop may attend to."""
+    if stream is not None:
+        return _under(stream, append_kv, k, v, cache, page_table, lengths, starts, table, grid, axis_pairs, positions,
+                      layout, held)
+    if table is not None and (grid is None or axis_pairs is None):
+        raise ValueError("a table needs its grid and axis_pairs")
+    return _ops().append_kv(k, v, tuple(cache), page_table, lengths, starts, table, grid or [], axis_pairs or [],
+                            positions, _half(layout), held)
+
+
+def cache_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, lengths: torch.Tensor,
+                    starts: torch.Tensor, scale: float | None = None, causal: bool = False, window: int = 0,
+                    out: torch.Tensor | None = None, *, stream=None) -> torch.Tensor:
+    """Attention of packed rows q [T][H][d], any strides of rows and heads, over
+    ``cache``, whose batch is that of :func:`append_kv` (H is a multiple of the cache's
+    heads, which the query heads share in a row).  A row sees the tokens up to its own
+    place (``causal``) or all of its sequence, of these the last ``window`` (0: all).
+    ``scale`` defaults to 1 / sqrt(d).  Returns [T][H][d]; rows that see nothing are
+    zeros, rows from ``starts``[B] on are left as they are.  bfloat16 or float32; the
+    latter with products in full precision."""
+    if stream is not None:
+        return _under(stream, cache_attention, q, cache, page_table, lengths, starts, scale, causal, window, out)
+    return _ops().cache_attention(q, tuple(cache), page_table, lengths, starts, scale, bool(causal), window, out)
