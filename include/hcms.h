@@ -925,7 +925,7 @@ HCMS_API int hcms_append_kv(const hcms_kv_cache *cache, const hcms_kv_batch *bat
  * Scores, maxima, sums and outputs are kept in fp32.  bf16: probabilities are rounded to
  * bf16 for their product; fp32: products are those of fp32.  Deterministic: work is split
  * along long sequences by sizes alone, and joined in a fixed order.
- * T H / heads <= 2^26, finite scale.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, ARG (scale,
+ * T H <= 2^29, B heads <= 2^21, finite scale.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, ARG (scale,
  * window < 0), HIP.  hcms_cache_attention_workspace is host only (errors: NULL, SHAPE,
  * DTYPE).
  */

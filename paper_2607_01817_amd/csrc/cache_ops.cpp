@@ -83,12 +83,14 @@ hcms::KvCache cache_of(const hcms_kv_cache *c) {
 }
 hcms::KvBatch batch_of(const hcms_kv_batch *b) { return {b->page_table, b->lengths, b->starts, b->B, b->W}; }
 
-int check_queries(const hcms_kv_cache *c, int T, int H, int window, int dtype) {
+int check_queries(const hcms_kv_cache *c, int B, int T, int H, int window, int dtype) {
     int st;
     if ((st = check_dtype(dtype)) != HCMS_OK) return st;
     if (H < 0 || H % c->heads != 0) return fail(HCMS_ERR_SHAPE, "H=%d must be a multiple of the cache's %d heads", H, c->heads);
-    if (static_cast<int64_t>(H / c->heads) * T > (1 << 26))   // tiles of them: the grid's first axis
-        return fail(HCMS_ERR_SHAPE, "T=%d rows of %d heads a key head: at most 2^26 together", T, H / c->heads);
+    // Tiles of them and of the sequences' ends: a grid's threads along one axis.
+    if (static_cast<int64_t>(H) * T > (1 << 29) || static_cast<int64_t>(c->heads) * B > (1 << 21))
+        return fail(HCMS_ERR_SHAPE, "T=%d rows of H=%d heads: at most 2^29 together; B=%d sequences of %d key heads: 2^21", T,
+                    H, B, c->heads);
     if (window < 0) return fail(HCMS_ERR_ARG, "window=%d", window);
     return HCMS_OK;
 }
@@ -146,7 +148,7 @@ int hcms_cache_attention_workspace(const hcms_kv_cache *cache, const hcms_kv_bat
     int st;
     if ((st = check_sizes(cache, batch, T)) != HCMS_OK) return st;
     if (!bytes) return fail(HCMS_ERR_NULL, "bytes is NULL");
-    if ((st = check_queries(cache, T, H, window, dtype)) != HCMS_OK) return st;
+    if ((st = check_queries(cache, batch->B, T, H, window, dtype)) != HCMS_OK) return st;
     *bytes = hcms::cache_attention_workspace(cache_of(cache), batch_of(batch), T, H, window, dtype);
     return ok();
 }
@@ -156,7 +158,7 @@ int hcms_cache_attention(const hcms_kv_cache *cache, const hcms_kv_batch *batch,
     int st;
     if ((st = check_sizes(cache, batch, T)) != HCMS_OK) return st;
     if (!q) return fail(HCMS_ERR_NULL, "q is NULL");
-    if ((st = check_queries(cache, T, H, window, dtype)) != HCMS_OK) return st;
+    if ((st = check_queries(cache, batch->B, T, H, window, dtype)) != HCMS_OK) return st;
     if (!std::isfinite(scale)) return fail(HCMS_ERR_ARG, "scale must be finite (got %g)", static_cast<double>(scale));
     if (T == 0 || batch->B == 0 || H == 0) return ok();
     Buffer in[8], held_by[4], of_batch[3];

@@ -180,7 +180,8 @@ def test_cache_attention_refusals(lib):
 
     assert call(T=0) == OK and call(batch=_batch(B=0)) == OK and call(heads=0) == OK
     assert call(q=None) == ENULL and call(q=_rows(None)) == ENULL and call(out=None) == ENULL and call(cache=None) == ENULL
-    assert call(heads=3) == ESHAPE and call(heads=-2) == ESHAPE and call(T=1 << 21, heads=128) == ESHAPE
+    assert call(heads=3) == ESHAPE and call(heads=-2) == ESHAPE and call(T=1 << 21, heads=512) == ESHAPE
+    assert call(batch=_batch(B=1 << 20), cache=_cache(heads=4)) == ESHAPE
     assert call(cache=_cache(d=32)) == ESHAPE and call(batch=_batch(W=0)) == ESHAPE
     assert call(scale=math.nan) == EARG and call(scale=math.inf) == EARG and call(window=-1) == EARG and call(dt=3) == EDTYPE
     assert call(q=_rows(H + 1)) == EALIGN and call(out=I + 1) == EALIGN and call(ws=J + 4) == EALIGN

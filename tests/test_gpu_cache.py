@@ -195,7 +195,8 @@ ATTENDS = [((1,), (1,), 1, 1, 64, 64), ((1,), (64,), 2, 5, 128, 64), ((1,), (100
            ((1, 1, 1), (17, 4000, 650), 2, 4, 128, 128), ((3, 0, 1, 2), (3, 500, 0, 129), 3, 3, 64, 192),
            ((17,), (40,), 1, 1, 128, 64), ((40, 7), (300, 7), 2, 2, 64, 64), ((33,), (2100,), 1, 16, 128, 64),
            ((130,), (190,), 1, 3, 64, 64), ((1,) * 67, tuple(range(5, 72)), 1, 2, 64, 64), ((2,), (9000,), 1, 7, 64, 512),
-           ((300, 1), (301, 700), 2, 1, 128, 64)]
+           ((300, 1), (301, 700), 2, 1, 128, 64), ((90, 0, 1, 257, 31), (90, 5, 640, 1000, 700), 1, 2, 64, 128),
+           ((128,), (3000,), 1, 2, 128, 64)]
 
 
 @pytest.mark.parametrize("rows,lengths,heads,group,d,page", ATTENDS)
@@ -213,19 +214,21 @@ def test_attention(hcms, rows, lengths, heads, group, d, page, dtype, causal, wi
 
 @pytest.mark.parametrize("scale", [0.0, -0.2, 3.0, 1e-3])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
-def test_scales_and_peaked_rows(hcms, scale, dtype):
-    b = Batch((5,), (700,), 2, 128, seed=9)
+@pytest.mark.parametrize("rows", [5, 70])
+def test_scales_and_peaked_rows(hcms, scale, dtype, rows):
+    b = Batch((rows,), (700,), 2, 128, seed=9)
     b.cache[2][:] = 127
-    q = _randn(1, 5, 4, 128, dtype=dtype)
+    q = _randn(1, rows, 4, 128, dtype=dtype)
     got = hcms.cache_attention(q.cuda(), *b.gpu(hcms), scale=scale)
     _check(got, q, b, dtype, float(np.float32(scale)), False, 0, f"scale {scale}")
 
 
 @pytest.mark.parametrize("order", [1, -1])
-def test_scores_that_rise_and_fall_along_the_cache(hcms, order):
+@pytest.mark.parametrize("rows", [1, 40])
+def test_scores_that_rise_and_fall_along_the_cache(hcms, order, rows):
     """The running maximum moves in every chunk, or never after the first."""
-    b = Batch((1,), (3000,), 1, 64, seed=4)
-    q = torch.ones(1, 1, 64)
+    b = Batch((rows,), (3000,), 1, 64, seed=4)
+    q = torch.ones(rows, 1, 64)
     K = np.linspace(0, 1, 3000)[::order]
     for p in range(3000):
         k = np.full(64, np.float64(K[p]))
@@ -265,41 +268,64 @@ def test_rows_that_see_nothing_and_lengths_of_zero(hcms):
     assert (left == 5).all()
 
 
-def test_values_that_are_not_finite_reach_the_rows_that_see_them_only(hcms):
+@pytest.mark.parametrize("group", [2, 20])          # few rows and many
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them_only(hcms, group, d):
     """NaN in keys and values of tokens before a window, after a causal row's place, and
     behind the sequence's end in its last page."""
     for dtype in (BF16, FP32):
         for part in (2, 3):                                       # k_scale, v_scale
             for byte in (255, 254, 253):
-                b = Batch((6,), (100,), 1, 64, seed=2)
-                clean = _f64(hcms.cache_attention(_randn(1, 6, 2, 64, dtype=dtype).cuda(), *b.gpu(hcms), causal=True, window=20))
+                b = Batch((6,), (100,), 1, d, seed=2)
+                q = _randn(1, 6, group, d, dtype=dtype).cuda()
+                clean = _f64(hcms.cache_attention(q, *b.gpu(hcms), causal=True, window=20))
                 place = oc.key_scale_place if part == 2 else oc.value_place
                 for p in (97, 78, 100, 127):                      # rows 0 to 5 see [75 + i, 95 + i)
                     b.cache[part][b.page_table[0, p // 64], 0, 0, 1, place(p % 64)] = byte
-                got = _f64(hcms.cache_attention(_randn(1, 6, 2, 64, dtype=dtype).cuda(), *b.gpu(hcms), causal=True, window=20))
+                got = _f64(hcms.cache_attention(q, *b.gpu(hcms), causal=True, window=20))
                 for i in range(6):
                     seen = any(75 + i <= p < 95 + i for p in (97, 78))
                     if not seen:
                         assert np.array_equal(got[i], clean[i]), (dtype, part, byte, i)
                     elif part == 3:
-                        assert not np.isfinite(got[i][:, 32:]).any() and np.array_equal(got[i][:, :32], clean[i][:, :32])
+                        bad = slice(32, 64)
+                        assert not np.isfinite(got[i][:, bad]).any()
+                        got[i][:, bad] = clean[i][:, bad] = 0
+                        assert np.array_equal(got[i], clean[i])
                     elif byte == 255:
                         assert np.isnan(got[i]).all()
 
 
-def test_nan_in_the_middle_of_a_sequence(hcms):
-    b = Batch((1, 1), (300, 300), 1, 128, seed=2)
+@pytest.mark.parametrize("rows", [1, 90])
+def test_nan_in_the_middle_of_a_sequence(hcms, rows):
+    b = Batch((rows, rows), (300, 300), 1, 128, seed=2)
     b.cache[3][b.page_table[0, 1], 0, 0, 2, oc.value_place(7)] = 255
     b.cache[2][b.page_table[1, 1], 0, 0, 2, oc.key_scale_place(7)] = 255
-    got = _f64(hcms.cache_attention(_randn(1, 2, 1, 128).cuda(), *b.gpu(hcms)))
-    assert np.isnan(got[0, 0, 64:96]).all() and np.isfinite(got[0, 0, :64]).all() and np.isfinite(got[0, 0, 96:]).all()
-    assert np.isnan(got[1]).all()
+    got = _f64(hcms.cache_attention(_randn(1, 2 * rows, 1, 128).cuda(), *b.gpu(hcms)))
+    first = got[:rows, 0]
+    assert np.isnan(first[:, 64:96]).all() and np.isfinite(first[:, :64]).all() and np.isfinite(first[:, 96:]).all()
+    assert np.isnan(got[rows:]).all()
 
 
-def test_pages_that_there_are_not_and_sequences_past_them(hcms):
+@pytest.mark.parametrize("rows", [1, 90])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_appended_nan_comes_out(hcms, rows, dtype):
+    """A block that was not finite when it was appended (whose codes are zeros) is NaN to
+    the rows that see it."""
+    b = Batch((rows, rows), (200, 200), 1, 64, seed=2)
+    k, v = _randn(1, 2 * rows, 1, 64, dtype=dtype), _randn(2, 2 * rows, 1, 64, dtype=dtype)
+    k[0, 0, 3], v[rows, 0, 40] = float("inf"), float("nan")
+    cache, *batch = b.gpu(hcms)
+    hcms.append_kv(k.cuda(), v.cuda(), cache, *batch)
+    got = _f64(hcms.cache_attention(_randn(3, 2 * rows, 2, 64, dtype=dtype).cuda(), cache, *batch))
+    assert np.isnan(got[:rows]).all() and np.isnan(got[rows:, :, 32:]).all() and np.isfinite(got[rows:, :, :32]).all()
+
+
+@pytest.mark.parametrize("group", [3, 40])          # few rows and many
+def test_pages_that_there_are_not_and_sequences_past_them(hcms, group):
     b = Batch((2, 2, 2), (150, 150, 150), 1, 64, seed=3)
     b.page_table[0, 1], b.page_table[1, 0] = b.pages, -5
-    q = _randn(1, 6, 3, 64, dtype=BF16)
+    q = _randn(1, 6, group, 64, dtype=BF16)
     cache, pages, lengths, starts = b.gpu(hcms)
     lengths[2] = 3 * 64 + 1
     got = _f64(hcms.cache_attention(q.cuda(), cache, pages, lengths, starts, causal=True))
@@ -308,9 +334,10 @@ def test_pages_that_there_are_not_and_sequences_past_them(hcms):
     assert np.isfinite(got[:4]).all() and np.isnan(got[4:]).all()      # the lost pages are out of the window
 
 
-def test_queries_that_are_not_finite_stay_in_their_rows(hcms):
+@pytest.mark.parametrize("group", [4, 40])
+def test_queries_that_are_not_finite_stay_in_their_rows(hcms, group):
     b = Batch((3,), (200,), 1, 64, seed=3)
-    q = _randn(1, 3, 4, 64, dtype=BF16)
+    q = _randn(1, 3, group, 64, dtype=BF16)
     clean = _f64(hcms.cache_attention(q.cuda(), *b.gpu(hcms)))
     q[1, 2, 5] = float("nan")
     got = _f64(hcms.cache_attention(q.cuda(), *b.gpu(hcms)))
