@@ -41,7 +41,9 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRows = 16;    // rows of a tile, and
-constexpr int kWaves = 4;    // waves of a workgroup, each with chunks of its own, for few rows
+constexpr int kWaves = 4;    // waves of a workgroup, for few rows
+constexpr int kTeamWaves = 8;   // where they work at the same part
+constexpr int kTeamChunks = 2 * kTeamWaves;   // up to which a workgroup takes a whole tile
 constexpr int kWaveRows = 32;                                    // rows of a wave, and
 // waves of a workgroup for many: two a SIMD, or one where its registers take the room
 // of two (fp32 rows of 128)
@@ -64,52 +66,220 @@ struct Args {
     float c;          // |scale| log2(e), above 0; the queries take its sign
     int group;        // query heads of a key head
     int from, to;     // the launch takes the sequences of [from, to] rows
-    int tiles;        // at most so many tiles of them
-    int splits;       // workgroups of a tile along the tokens
-    int least;        // chunks of a split, at least
-    float *partial;   // of splits: [split][tile][key head][rows of a tile][d + 4]
+    int groups;       // workgroups
+    int least;        // chunks of a workgroup, at least, but where there are more tiles
+    bool whole;       // a workgroup a tile
+    struct Begun *begun;   // [groups]
+    float *partial;        // [2 groups][rows of a tile][d + 4]: states of parts of tiles
 };
 
-// A tile: rows [row0, row0 + n) of its sequence's n_new * group, and the chunks
-// [c0, c1) that they see.
-struct Tile {
-    int b, row0, n, c0, c1;
-    kv::Sequence seq;
-    bool lost;   // the sequence is longer than its pages: NaN
+// The tile that a workgroup begins and others end: how many workgroups work at it (0:
+// none is begun), its key head, its first row and their number in the sequence, and the
+// sequence's first row.
+struct Begun {
+    int parts, head, row0, n, first;
 };
 
+// The division of a launch's work.  A tile is some rows of a sequence and key head and
+// weighs as many chunks as they see (if `whole`, 1).  All tiles lie one behind the other,
+// the tiles of a sequence and head in a row, sequence by sequence, head by head, and each
+// workgroup takes an equal piece of that line: the end of one tile, whole ones, and the
+// beginning of another.  Lengths are read here, so the pieces are equal whatever the
+// sequences are.  Parts of tiles leave their states in `partial`, two for a workgroup.
+//
+// The weights of a sequence's tiles are taken to rise evenly from the first one's chunks
+// to the last one's, so that those before tile k are known at once; a part of a tile is
+// that part of the chunks that it has.
 __device__ inline int row_end(const Args &a, const kv::Sequence &s, int query) {
     return max(a.rows.causal ? s.length - s.n + query + 1 : s.length, 0);
 }
 __device__ inline int row_begin(const Args &a, int end) { return a.rows.window ? max(end - a.rows.window, 0) : 0; }
 
+// A tile: rows [row0, row0 + n) of its sequence's, and the chunks [c0, c1) that they see.
+struct Tile {
+    int row0, n, c0, c1;
+    bool lost;   // the sequence is longer than its pages: NaN
+};
 template <int ROWS>
-__device__ inline bool tile_at(const Args &a, int64_t at, Tile *t) {
-    int tile;
-    const auto tiles = [&](const kv::Sequence &s) {
+__device__ inline Tile tile_of(const Args &a, const kv::Sequence &s, int k) {
+    Tile t;
+    t.row0 = k * ROWS;
+    t.n = min(ROWS, s.n * a.group - t.row0);
+    t.lost = s.length > static_cast<int64_t>(a.batch.W) * a.cache.page;
+    t.c0 = t.lost ? 0 : row_begin(a, row_end(a, s, t.row0 / a.group)) / kChunk;
+    const int64_t end = row_end(a, s, (t.row0 + t.n - 1) / a.group);
+    t.c1 = t.lost ? 1 : max(static_cast<int>((end + kChunk - 1) / kChunk), t.c0);   // lost: any one chunk
+    return t;
+}
+
+// The tiles of a sequence: how many, and the weights of the first and last.  Divisions
+// are in fp64, a tenth of the instructions of those of 64-bit integers: their operands
+// are whole numbers below 2^53, and what they give grows with k as it has to.
+template <int ROWS>
+struct Tiles {
+    int count = 0, first = 0;
+    double rise = 0.0;   // of a weight, half of it from tile to tile
+    __device__ Tiles(const Args &a, const kv::Sequence &s) {
         const int rows = s.n * a.group;
-        return rows < a.from || rows > a.to ? 0 : (rows + ROWS - 1) / ROWS;
-    };
-    if (!kv::find_tile(a.batch, a.rows.T, at, tiles, &t->b, &tile, &t->seq)) return false;
-    t->row0 = tile * ROWS;
-    t->n = min(ROWS, t->seq.n * a.group - t->row0);
-    const int64_t room = static_cast<int64_t>(a.batch.W) * a.cache.page;
-    t->lost = t->seq.length > room;
-    t->c0 = row_begin(a, row_end(a, t->seq, t->row0 / a.group)) / kChunk;
-    t->c1 = static_cast<int>((static_cast<int64_t>(row_end(a, t->seq, (t->row0 + t->n - 1) / a.group)) + kChunk - 1) / kChunk);
-    if (t->lost) {   // any one chunk
-        t->c0 = 0;
-        t->c1 = 1;
+        if (rows < a.from || rows > a.to) return;
+        count = (rows + ROWS - 1) / ROWS;
+        first = 1;
+        if (a.whole) return;
+        const Tile x = tile_of<ROWS>(a, s, 0), y = tile_of<ROWS>(a, s, count - 1);
+        first = max(x.c1 - x.c0, 1);
+        rise = count < 2 ? 0.0 : static_cast<double>(max(y.c1 - y.c0 - first, 0)) / (2.0 * (count - 1));
     }
-    return true;
+    // Weights of the tiles before tile k.
+    __device__ int64_t before(int k) const {
+        return static_cast<int64_t>(k) * first + static_cast<int64_t>(rise * (static_cast<double>(k) * (k - 1)));
+    }
+    __device__ int64_t all() const { return before(count); }
+    // The tile of unit `at` of them.
+    __device__ int find(int64_t at) const {
+        int lo = 0, hi = count - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (before(mid) <= at) lo = mid;
+            else hi = mid - 1;
+        }
+        return lo;
+    }
+};
+
+// All of a launch's work: units of a head, and what the workgroups share them by.
+template <int ROWS>
+struct Work {
+    int64_t head, all;
+    int groups;    // that have some
+    double each;   // units of a group
+    Work() = default;
+    __device__ explicit Work(const Args &a) {
+        int64_t tiles;
+        kv::add_up(a.batch, a.rows.T, [&](const kv::Sequence &s, int64_t *units, int64_t *tiles) {
+            const Tiles<ROWS> t(a, s);
+            *units += t.all();
+            *tiles += t.count;
+        }, &head, &tiles);
+        all = head * a.cache.heads;
+        tiles *= a.cache.heads;
+        const int64_t fit = static_cast<int64_t>(static_cast<double>(all) / a.least);
+        groups = static_cast<int>(a.whole ? all : min(max(tiles, fit), static_cast<int64_t>(a.groups)));
+        each = static_cast<double>(all) / max(groups, 1);
+    }
+    __device__ int64_t begin(int group) const { return group < groups ? static_cast<int64_t>(group * each) : all; }
+    // The workgroup of a unit.
+    __device__ int group_of(int64_t unit) const {
+        int g = min(static_cast<int>(static_cast<double>(unit) / each), groups - 1);
+        while (begin(g + 1) <= unit) ++g;
+        while (begin(g) > unit) --g;
+        return g;
+    }
+};
+
+// A part of a tile: its place, and its part [u0, u1) of the tile's weight.
+template <int ROWS>
+struct Piece;
+template <int ROWS>
+struct Part {
+    int b, k, head;
+    kv::Sequence seq;
+    int u0, u1, weight;
+    // The part that begins at unit `at` of a line of `of_head` units a head, and ends
+    // with its tile or at `end`.
+    __device__ Part(const Args &a, int64_t of_head, int64_t at, int64_t end) {
+        head = static_cast<int>(static_cast<double>(at) / static_cast<double>(of_head));   // exact below 2^53
+        int64_t before = 0;
+        kv::find_unit(a.batch, a.rows.T, at - head * of_head, [&](const kv::Sequence &s) { return Tiles<ROWS>(a, s).all(); },
+                      &b, &before, &seq);
+        const Tiles<ROWS> t(a, seq);
+        const int64_t in = at - head * of_head - before;
+        k = t.find(in);
+        const int64_t first = t.before(k);
+        weight = static_cast<int>(t.before(k + 1) - first);
+        u0 = static_cast<int>(in - first);
+        u1 = static_cast<int>(min(static_cast<int64_t>(weight), u0 + (end - at)));
+        // Alike in all lanes, but reckoned in vector registers: scalar ones are few.
+        head = kv::uniform(head);
+        b = kv::uniform(b);
+        k = kv::uniform(k);
+        seq = {kv::uniform(seq.first), kv::uniform(seq.n), kv::uniform(seq.length)};
+        weight = kv::uniform(weight);
+        u0 = kv::uniform(u0);
+        u1 = kv::uniform(u1);
+    }
+    __device__ bool whole() const { return u0 == 0 && u1 == weight; }
+    // Its chunks.
+    __device__ int chunk(const Tile &t, int u) const {
+        return t.c0 + static_cast<int>(static_cast<double>(t.c1 - t.c0) * u / weight);   // all of them for all of it
+    }
+    // Where its state goes: a workgroup's first part that begins inside a tile, or its last.
+    __device__ int slot(const Piece<ROWS> &piece) const;
+};
+
+// A workgroup's piece of the line, in LDS between its parts, where it takes no registers.
+template <int ROWS>
+struct Piece {
+    Work<ROWS> work;
+    int64_t at, end;
+    int group;
+};
+// The kernel's arguments (its only parameter, so they lie first in its argument
+// segment), read anew for each part: they, and what is made of them (a division's
+// factors, strides in bytes), kept over all parts would take more scalar registers than
+// there are.
+__device__ inline Args arguments() {
+    typedef const __attribute__((address_space(4))) unsigned Word;
+    struct Words {
+        unsigned w[sizeof(Args) / 4];
+    } words;
+    static_assert(sizeof(Args) % 4 == 0, "whole words");
+    Word *p = (Word *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(Args) / 4; ++i) words.w[i] = p[i];
+    return __builtin_bit_cast(Args, words);
 }
-// Chunks of a split, and how many splits have some.
-__device__ inline int split_chunks(const Args &a, const Tile &t) {
-    return max(a.least, (t.c1 - t.c0 + a.splits - 1) / a.splits);
-}
-__device__ inline int split_count(const Args &a, const Tile &t) {
-    const int per = split_chunks(a, t);
-    return max((t.c1 - t.c0 + per - 1) / per, 1);
+template <int ROWS>
+__device__ inline int Part<ROWS>::slot(const Piece<ROWS> &piece) const { return 2 * piece.group + (u0 == 0 ? 1 : 0); }
+
+// Calls each(arguments, part) for the parts of a group's piece.  WAVES: all waves of a
+// workgroup call it for one group; else each wave for its own, with an `lds` of its own,
+// which all its lanes write alike.
+template <int ROWS, bool WAVES, typename F>
+__device__ inline void for_parts(int group, Piece<ROWS> &lds, F &&each) {
+    const auto sync = [] {
+        if constexpr (WAVES) __syncthreads();
+    };
+    const auto writes = [] { return !WAVES || threadIdx.x == 0; };
+    {
+        const Args a = arguments();
+        if (group >= a.groups) return;
+        const Work<ROWS> work(a);
+        if (writes()) {
+            if (!a.whole) a.begun[group].parts = 0;
+            lds.work = work;
+            lds.at = work.begin(min(group, work.groups));
+            lds.end = work.begin(min(group + 1, work.groups));
+            lds.group = group;
+        }
+    }
+    while (true) {
+        sync();
+        const int64_t at = lds.at, end = lds.end;
+        if (kv::uniform(static_cast<int>(at >= end))) return;
+        const Args a = arguments();
+        const Part<ROWS> part(a, lds.work.head, at, end);
+        sync();
+        if (writes()) {
+            lds.at = at + (part.u1 - part.u0);
+            if (part.u0 == 0 && part.u1 < part.weight) {   // the last one
+                const Tile t = tile_of<ROWS>(a, part.seq, part.k);
+                a.begun[group] = {lds.work.group_of(at + part.weight - 1) - group + 1, part.head, t.row0, t.n,
+                                  part.seq.first};
+            }
+        }
+        each(a, part);
+    }
 }
 
 // A chunk of one head as loaded: for 16-token tile i the lane's keys (D / 4 elements
@@ -316,112 +486,147 @@ __device__ inline float weight_of(float m, float all, float c) {
 }
 
 template <int ROWS, int D>
-__device__ inline float *partial_at(const Args &a, int split, int tile, int head, int row) {
-    return a.partial + (((static_cast<int64_t>(split) * a.tiles + tile) * a.cache.heads + head) * ROWS + row) * (D + 4);
+__device__ inline float *partial_at(const Args &a, int slot, int row) {
+    return a.partial + (static_cast<int64_t>(slot) * ROWS + row) * (D + 4);
 }
 template <typename T>
-__device__ inline T *out_at(const Args &a, const Tile &t, int head, int row) {
+__device__ inline T *out_at(const Args &a, int first, int head, int row) {
     return static_cast<T *>(a.rows.out) +
-           (static_cast<int64_t>(t.seq.first + row / a.group) * a.rows.H + head * a.group + row % a.group) * a.cache.d;
+           (static_cast<int64_t>(first + row / a.group) * a.rows.H + head * a.group + row % a.group) * a.cache.d;
 }
 template <typename T>
-__device__ inline const T *query_at(const Args &a, const Tile &t, int head, int row) {
-    return static_cast<const T *>(a.rows.q) + static_cast<int64_t>(t.seq.first + row / a.group) * a.rows.q_token +
+__device__ inline const T *query_at(const Args &a, const kv::Sequence &s, int head, int row) {
+    return static_cast<const T *>(a.rows.q) + static_cast<int64_t>(s.first + row / a.group) * a.rows.q_token +
            static_cast<int64_t>(head * a.group + row % a.group) * a.rows.q_head;
 }
 
+// A wave's state of a part of a tile of 16 rows: every `step`-th of its chunks.
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void cache_attention_kernel(Args a) {
-    constexpr int NP = sizeof(T) == 2 ? 1 : 3, LD = D + 4;
-    __shared__ float o_lds[kWaves][kRows][LD], m_lds[kWaves][kRows], l_lds[kWaves][kRows];
-    Tile t;
-    if (!tile_at<kRows>(a, blockIdx.x, &t)) return;
-    const int head = blockIdx.y, lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
-    const int per = split_chunks(a, t), count = split_count(a, t);
-    if (static_cast<int>(blockIdx.z) >= count) return;
-    const int first = t.c0 + static_cast<int>(blockIdx.z) * per, last = min(first + per, t.c1);
-
+__device__ inline void few_rows(const Args &a, const Part<kRows> &part, const Tile &t, int chunk, int step, State<D> &st) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3;
+    const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
+    const int last = part.chunk(t, part.u1), head = part.head;
+    if (chunk >= last) return;
     const int row = t.row0 + min(r, t.n - 1), query = row / a.group;
-    const int end = row_end(a, t.seq, query), begin = row_begin(a, end);
+    const int end = row_end(a, part.seq, query), begin = row_begin(a, end);
     // The tokens that every row of the tile sees.
-    const int all_end = row_end(a, t.seq, t.row0 / a.group);
-    const int all_begin = row_begin(a, row_end(a, t.seq, (t.row0 + t.n - 1) / a.group));
-
-    State<D> st;
-    const int *const pages = a.batch.page_table + static_cast<int64_t>(t.b) * a.batch.W;
+    const int all_end = row_end(a, part.seq, t.row0 / a.group);
+    const int all_begin = row_begin(a, row_end(a, part.seq, (t.row0 + t.n - 1) / a.group));
+    const int *const pages = a.batch.page_table + static_cast<int64_t>(part.b) * a.batch.W;
     const int per_page = a.cache.page / kChunk;
-    int chunk = first + wave;
-    if (chunk < last) {
-        Raw<D> raw;
-        raw.load(a, head, pages[chunk / per_page], chunk, lane);
-        bf16x8 q[D / 32][NP];
-        const T *qp = query_at<T>(a, t, head, row) + g * (D / 4);
-        const float sign = a.rows.scale < 0.0f ? -1.0f : 1.0f;
+    Raw<D> raw;
+    raw.load(a, head, pages[chunk / per_page], chunk, lane);
+    bf16x8 q[D / 32][NP];
+    const T *qp = query_at<T>(a, part.seq, head, row) + g * (D / 4);
+    const float sign = a.rows.scale < 0.0f ? -1.0f : 1.0f;
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
-            const fp8::f32x8 x = widen(load_raw(qp + 8 * j));
-            float y[8];
+    for (int j = 0; j < D / 32; ++j) {
+        const fp8::f32x8 x = widen(load_raw(qp + 8 * j));
+        float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = x[e] * sign;
-            take_apart<NP>(y, q[j]);
-        }
-        // The next chunk's loads ahead of this one's products, where the registers hold both.
-        constexpr bool AHEAD = NP == 1 || D == 64;
-        while (true) {
-            const int next = chunk + kWaves;
-            Raw<D> ahead;
-            if (AHEAD && next < last) ahead.load(a, head, pages[next / per_page], next, lane);
-            const int token0 = chunk * kChunk;
-            const bool masked = !t.lost && (token0 < all_begin || token0 + kChunk > all_end);
-            attend<D, NP>(a, raw, q, st, token0 + 4 * g, begin, end, masked, t.lost);
-            if (next >= last) break;
-            if constexpr (AHEAD) raw = ahead;
-            else raw.load(a, head, pages[next / per_page], next, lane);
-            chunk = next;
-        }
+        for (int e = 0; e < 8; ++e) y[e] = x[e] * sign;
+        take_apart<NP>(y, q[j]);
     }
+    // The next chunk's loads ahead of this one's products, where the registers hold both.
+    constexpr bool AHEAD = NP == 1 || D == 64;
+    while (true) {
+        const int next = chunk + step;
+        Raw<D> ahead;
+        if (AHEAD && next < last) ahead.load(a, head, pages[next / per_page], next, lane);
+        const int token0 = chunk * kChunk;
+        const bool masked = !t.lost && (token0 < all_begin || token0 + kChunk > all_end);
+        attend<D, NP>(a, raw, q, st, token0 + 4 * g, begin, end, masked, t.lost);
+        if (next >= last) break;
+        if constexpr (AHEAD) raw = ahead;
+        else raw.load(a, head, pages[next / per_page], next, lane);
+        chunk = next;
+    }
+}
 
-    // The waves' states in one, in the order of the waves.
-    const float sum = over_groups(st.sum, false);
-    if (g == 0) {
-        m_lds[wave][r] = st.m;
-        l_lds[wave][r] = sum;
-    }
+// Waves with pieces of their own: none waits for another, so that one's beginnings and
+// ends of tiles are covered by the others' loads.
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void cache_attention_kernel(Args) {
+    __shared__ Piece<kRows> pieces[kWaves];
+    const int wave = kv::uniform(static_cast<int>(threadIdx.x / 64));
+    Piece<kRows> &piece = pieces[wave];
+    for_parts<kRows, false>(blockIdx.x * kWaves + wave, piece, [&](const Args &a, const Part<kRows> &part) {
+        const Tile t = tile_of<kRows>(a, part.seq, part.k);
+        State<D> st;
+        few_rows<T, D>(a, part, t, part.chunk(t, part.u0), 1, st);
+        const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
+        const float sum = over_groups(st.sum, false);
+        if (r >= t.n) return;
+        const bool whole = part.whole();
+        float *const p = partial_at<kRows, D>(a, part.slot(piece), r);
+        T *const out = out_at<T>(a, part.seq.first, part.head, t.row0 + r);
+        const float by = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
 #pragma unroll
-    for (int b = 0; b < D / 32; ++b)
+        for (int b = 0; b < D / 32; ++b) {
+            fp8::f32x8 x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            o_lds[wave][r][32 * b + 8 * g + 2 * e] = st.o[b][0][e];
-            o_lds[wave][r][32 * b + 8 * g + 2 * e + 1] = st.o[b][1][e];
+            for (int e = 0; e < 4; ++e) {
+                x[2 * e] = st.o[b][0][e] * by;
+                x[2 * e + 1] = st.o[b][1][e] * by;
+            }
+            if (whole) store_8(out + 32 * b + 8 * g, x);
+            else store_8(p + 32 * b + 8 * g, x);
         }
-    __syncthreads();
-    constexpr int LANES = 64 * kWaves / kRows, EACH = D / LANES;   // threads of a row, elements of each
-    const int out_row = threadIdx.x / LANES, e0 = threadIdx.x % LANES * EACH;
-    if (out_row >= t.n) return;
-    float m = kNone, l = 0.0f, o[EACH] = {};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, m_lds[w][out_row]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const float by = weight_of(m_lds[w][out_row], m, a.c);
-        l = __builtin_fmaf(l_lds[w][out_row], by, l);
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) o[e] = __builtin_fmaf(o_lds[w][out_row][e0 + e], by, o[e]);
-    }
-    if (count > 1) {
-        float *p = partial_at<kRows, D>(a, blockIdx.z, blockIdx.x, head, out_row);
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) p[e0 + e] = o[e];
-        if (e0 == 0) {
-            p[D] = m;
-            p[D + 1] = l;
+        if (!whole && g == 0) {
+            p[D] = st.m;
+            p[D + 1] = sum;
         }
-        return;
-    }
-    T *out = out_at<T>(a, t, head, t.row0 + out_row) + e0;
-    const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    });
+}
+
+// Workgroups with pieces of their own, for few tiles: the chunks of a part go by turns to
+// the waves, whose states are joined in their order.
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kTeamWaves, 2) void cache_attention_team_kernel(Args) {
+    __shared__ float o_lds[kTeamWaves][kRows][D + 4], m_lds[kTeamWaves][kRows], l_lds[kTeamWaves][kRows];
+    __shared__ Piece<kRows> piece;
+    for_parts<kRows, true>(blockIdx.x, piece, [&](const Args &a, const Part<kRows> &part) {
+        const Tile t = tile_of<kRows>(a, part.seq, part.k);
+        const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
+        State<D> st;
+        few_rows<T, D>(a, part, t, part.chunk(t, part.u0) + wave, kTeamWaves, st);
+        const float mine = over_groups(st.sum, false);
+        if (g == 0) {
+            m_lds[wave][r] = st.m;
+            l_lds[wave][r] = mine;
+        }
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) out[e] = static_cast<T>(o[e] * by);
+        for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                o_lds[wave][r][32 * b + 8 * g + 2 * e] = st.o[b][0][e];
+                o_lds[wave][r][32 * b + 8 * g + 2 * e + 1] = st.o[b][1][e];
+            }
+        __syncthreads();
+        const bool whole = part.whole();
+        for (int i = threadIdx.x; i < t.n * D; i += 64 * kTeamWaves) {
+            const int row = i / D, e = i % D;
+            float m = kNone, sum = 0.0f, x = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kTeamWaves; ++w) m = fmaxf(m, m_lds[w][row]);
+#pragma unroll
+            for (int w = 0; w < kTeamWaves; ++w) {
+                const float by = weight_of(m_lds[w][row], m, a.c);
+                sum = __builtin_fmaf(l_lds[w][row], by, sum);
+                x = __builtin_fmaf(o_lds[w][row][e], by, x);
+            }
+            if (whole) {
+                out_at<T>(a, part.seq.first, part.head, t.row0 + row)[e] = static_cast<T>(sum == 0.0f ? 0.0f : x / sum);
+                continue;
+            }
+            float *const p = partial_at<kRows, D>(a, part.slot(piece), row);
+            p[e] = x;
+            if (e == 0) {
+                p[D] = m;
+                p[D + 1] = sum;
+            }
+        }
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -449,23 +654,30 @@ struct Widened {
 // 32 elements of a token each, half the values, an element pair of 16 tokens.
 template <int D>
 struct Share {
+    const unsigned char *data, *scales;   // the cache's, and
+    unsigned at, scale_at;                // its place in a chunk of it
     u32x4 x, scale;
 
-    __device__ void load_keys(const Args &a, int head, int page, int chunk, int t) {
-        const int per_page = a.cache.page / kChunk;
-        const bool bad = page < 0 || page >= a.cache.pages;
-        const int64_t block = (static_cast<int64_t>(bad ? 0 : page) * a.cache.heads + head) * per_page + chunk % per_page;
-        x = *reinterpret_cast<const u32x4 *>(a.cache.k + block * kChunk * (D / 2) + 16 * t);
-        const int token = t / (D / 32), b = t % (D / 32);
-        scale[0] = bad ? 255u : a.cache.k_scale[(block * (D / 32) + b) * kChunk + kv::key_scale_place(token)];
+    __device__ void at_keys(const Args &a, int t) {
+        data = a.cache.k;
+        scales = a.cache.k_scale;
+        at = 16 * t;
+        scale_at = t % (D / 32) * kChunk + kv::key_scale_place(t / (D / 32));
     }
-    __device__ void load_values(const Args &a, int head, int page, int chunk, int t) {
-        const int per_page = a.cache.page / kChunk;
-        const bool bad = page < 0 || page >= a.cache.pages;
-        const int64_t block = (static_cast<int64_t>(bad ? 0 : page) * a.cache.heads + head) * per_page + chunk % per_page;
-        const int c = t / 4, at = 16 * (t & 1) + 8 * (t >> 1 & 1);
-        const unsigned char *p = a.cache.v + block * kChunk * (D / 2) + c * kChunk + at;
-        const unsigned char *s = a.cache.v_scale + (block * (D / 32) + c / 16) * kChunk + at;
+    __device__ void at_values(const Args &a, int t) {
+        const int c = t / 4, in = 16 * (t & 1) + 8 * (t >> 1 & 1);
+        data = a.cache.v;
+        scales = a.cache.v_scale;
+        at = c * kChunk + in;
+        scale_at = c / 16 * kChunk + in;
+    }
+    // Chunk `block` of the cache; bad: of a page that there is not.
+    __device__ void load_keys(int64_t block, bool bad) {
+        x = *reinterpret_cast<const u32x4 *>(data + block * (kChunk * (D / 2)) + at);
+        scale[0] = bad ? 255u : (scales + block * (kChunk * (D / 32)))[scale_at];
+    }
+    __device__ void load_values(int64_t block) {
+        const unsigned char *p = data + block * (kChunk * (D / 2)) + at, *s = scales + block * (kChunk * (D / 32)) + scale_at;
         const u32x2 x0 = *reinterpret_cast<const u32x2 *>(p), x1 = *reinterpret_cast<const u32x2 *>(p + 32);
         const u32x2 s0 = *reinterpret_cast<const u32x2 *>(s), s1 = *reinterpret_cast<const u32x2 *>(s + 32);
         x = u32x4{x0[0], x0[1], x1[0], x1[1]};
@@ -518,25 +730,12 @@ __device__ inline float of_halves(float x, bool maximum) {
 // + 4 g + r % 4 in s[mt][r], of the output the elements 32 dt + 8 (r / 4) + 4 g + r % 4
 // in o[dt][r].
 template <typename T, int D>
-__global__ __launch_bounds__((64 * kPieceWaves<T, D>), (kPiecePerSimd<T, D>)) void cache_attention_piece_kernel(Args a) {
+__device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &part, const Piece<kPieceRows<T, D>> &piece, Widened<D> (&lds)[2]) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3, WAVES = kPieceWaves<T, D>, ROWS = kPieceRows<T, D>, KK = D / 16, DT = D / 32;
     constexpr int KS = Widened<D>::KS, VS = Widened<D>::VS;
-    __shared__ Widened<D> lds[2];
-
-    // Workgroup b runs on XCD b % 8; each XCD gets a range of the launch, whose
-    // neighbours are the tiles that read the same chunks.
-    const int nb = gridDim.x, id = blockIdx.x, xcd = id & 7;
-    int at = xcd * (nb >> 3) + min(xcd, nb & 7) + (id >> 3);
-    const int tile = at % a.tiles;
-    at /= a.tiles;
-    const int head = at % a.cache.heads, split = at / a.cache.heads;
-    Tile t;
-    if (!tile_at<ROWS>(a, tile, &t)) return;
-    const int per = split_chunks(a, t), count = split_count(a, t);
-    if (split >= count) return;
-    const int first = t.c0 + split * per, chunks = min(per, t.c1 - first);
-
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, li = lane % 32, g = lane / 32;
+    const Tile t = tile_of<ROWS>(a, part.seq, part.k);
+    const int head = part.head, first = part.chunk(t, part.u0), chunks = part.chunk(t, part.u1) - first;
+    const int lane = threadIdx.x % 64, wave = kv::uniform(static_cast<int>(threadIdx.x / 64)), li = lane % 32, g = lane / 32;
     const bool active = wave * kWaveRows < t.n;
     // Half of the threads take keys and half values, or each takes both.
     constexpr bool BOTH = 64 * WAVES == 2 * D;
@@ -544,9 +743,9 @@ __global__ __launch_bounds__((64 * kPieceWaves<T, D>), (kPiecePerSimd<T, D>)) vo
     const bool keys = wave < WAVES / 2;
     const int share = threadIdx.x % (2 * D);
     const int row = t.row0 + min(wave * kWaveRows + li, t.n - 1);
-    const int end = row_end(a, t.seq, row / a.group), begin = row_begin(a, end);
-    const int all_end = row_end(a, t.seq, t.row0 / a.group);
-    const int all_begin = row_begin(a, row_end(a, t.seq, (t.row0 + t.n - 1) / a.group));
+    const int end = row_end(a, part.seq, row / a.group), begin = row_begin(a, end);
+    const int all_end = row_end(a, part.seq, t.row0 / a.group);
+    const int all_begin = row_begin(a, row_end(a, part.seq, (t.row0 + t.n - 1) / a.group));
     const auto masked = [&](int j) {
         const int token0 = (first + j) * kChunk;
         return !t.lost && (token0 < all_begin || token0 + kChunk > all_end);
@@ -554,7 +753,7 @@ __global__ __launch_bounds__((64 * kPieceWaves<T, D>), (kPiecePerSimd<T, D>)) vo
 
     bf16x8 q[KK][NP];
     {
-        const T *qp = query_at<T>(a, t, head, row) + 8 * g;
+        const T *qp = query_at<T>(a, part.seq, head, row) + 8 * g;
         const float sign = a.rows.scale < 0.0f ? -1.0f : 1.0f;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
@@ -566,16 +765,24 @@ __global__ __launch_bounds__((64 * kPieceWaves<T, D>), (kPiecePerSimd<T, D>)) vo
         }
     }
 
-    const int *const pages = a.batch.page_table + static_cast<int64_t>(t.b) * a.batch.W;
+    // Chunk by chunk: the page's place in the table and the chunk's in the page.
     const int per_page = a.cache.page / kChunk;
+    const int *pages = a.batch.page_table + static_cast<int64_t>(part.b) * a.batch.W + first / per_page;
+    int in_page = first % per_page, page = t.lost || chunks == 0 ? -1 : *pages;
     Share<D> of_keys, of_values;
-    const auto page_of = [&](int j) { return t.lost ? -1 : pages[(first + min(j, chunks - 1)) / per_page]; };
-    int page = page_of(0);
-    const auto load = [&](int j) {   // chunk j's share (past the last one, that again) and the next one's page
-        const int chunk = first + min(j, chunks - 1), at = page;
-        page = page_of(j + 1);
-        if (BOTH || keys) of_keys.load_keys(a, head, at, chunk, share);
-        if (BOTH || !keys) (BOTH ? of_values : of_keys).load_values(a, head, at, chunk, share);
+    if (BOTH || keys) of_keys.at_keys(a, share);
+    if (BOTH || !keys) (BOTH ? of_values : of_keys).at_values(a, share);
+    const auto load = [&](int j) {   // chunk j's share, if there is one, and the next one's page
+        if (j >= chunks) return;
+        const bool bad = page < 0 || page >= a.cache.pages;
+        const int64_t block = (static_cast<int64_t>(bad ? 0 : page) * a.cache.heads + head) * per_page + in_page;
+        if (++in_page == per_page) {
+            in_page = 0;
+            ++pages;
+            if (j + 1 < chunks) page = *pages;
+        }
+        if (BOTH || keys) of_keys.load_keys(block, bad);
+        if (BOTH || !keys) (BOTH ? of_values : of_keys).load_values(block);
     };
     const auto store = [&](int j) {
         if (BOTH || keys) of_keys.store_keys(lds[j & 1], share);
@@ -585,99 +792,114 @@ __global__ __launch_bounds__((64 * kPieceWaves<T, D>), (kPiecePerSimd<T, D>)) vo
     const float c = a.c;
     float m = kNone, mc = 0.0f, sum = 0.0f;
     f32x16 o[DT] = {};
+    // Scores of chunk j.
+    const auto scores = [&](int j, f32x16 (&s)[2]) {
+        const __bf16 *const k = lds[j & 1].k + li * KS + 8 * g;
+        s[0] = s[1] = f32x16{};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+                const bf16x8 x = *reinterpret_cast<const bf16x8 *>(k + 32 * mt * KS + 16 * kk);
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) s[mt] = mfma32(x, q[kk][p], s[mt]);
+            }
+    };
+    // What lane g's token r of tile mt of chunk j is, and whether its row sees it.
+    const auto sees = [&](int j, int at) {
+        return static_cast<unsigned>((first + j) * kChunk + 4 * g + at - begin) < static_cast<unsigned>(end - begin);
+    };
+    const auto hide = [&](int j, f32x16 (&s)[2]) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[mt][r] = sees(j, 32 * mt + 8 * (r / 4) + r % 4) ? s[mt][r] : kNone;
+                if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // else all comparisons' masks at once
+            }
+    };
+    const auto maximum = [&](const f32x16 (&s)[2]) {   // of the chunk's scores of the row
+        float top = kNone;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, fmaxf(s[0][r], s[1][r]));
+        return of_halves(top, true);
+    };
+    const auto raise = [&](float to) {
+        const float by = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
+        sum *= by;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= by;
+        m = to;
+        mc = m == kNone ? 0.0f : m * c;
+    };
+    // As in attend: values that are not finite make the rows NaN that see them, at the end
+    // (bit dt: the elements of o[dt]).
+    unsigned lost = 0;
+    const auto note_wrong = [&](int j) {
+        const Widened<D> &buf = lds[j & 1];
+        unsigned any = 0;
+        if (lane < D / 32 * kChunk / 4) any = reinterpret_cast<const unsigned *>(&buf.wrong[0][0])[lane];
+        if (!__ballot(any != 0)) return;
+#pragma unroll 1
+        for (int i = 0; i < D / 32 * kChunk; ++i) {   // in the order of the operands
+            const int at = i % kChunk;
+            const int token = (first + j) * kChunk + at / 16 * 16 + at / 8 % 2 * 4 + at % 8 / 4 * 8 + at % 4;
+            if ((&buf.wrong[0][0])[i] && token >= begin && token < end) lost |= 1u << (i / kChunk);
+        }
+    };
+
     load(0);
-    store(0);
+    if (chunks > 0) store(0);
     load(1);
     __syncthreads();
     for (int j = 0; j < chunks; ++j) {
-        const Widened<D> &buf = lds[j & 1];
         if (j + 1 < chunks) {
             store(j + 1);
             load(j + 2);
         }
         if (active) {
-            f32x16 s[2] = {};
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-                for (int mt = 0; mt < 2; ++mt) {
-                    const bf16x8 k = *reinterpret_cast<const bf16x8 *>(buf.k + (32 * mt + li) * KS + 16 * kk + 8 * g);
-#pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) s[mt] = mfma32(k, q[kk][p], s[mt]);
-                }
+            f32x16 s[2];
+            scores(j, s);
             const bool mask = masked(j);
-            const int token0 = (first + j) * kChunk + 4 * g;
-            if (mask) {
+            if (mask) hide(j, s);
+            const float top = maximum(s);
+            if (__ballot(m == kNone ? top > kNone : (top - m) * c > kHeadroom)) raise(fmaxf(m, top));
+            // In place of the scores: their parts, three to each, only where they are used.
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
+            for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int token = token0 + 32 * mt + 8 * (r / 4) + r % 4;
-                        s[mt][r] = token >= begin && token < end ? s[mt][r] : kNone;
-                    }
-            }
-            float top = kNone;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, fmaxf(s[0][r], s[1][r]));
-            if (__ballot(m == kNone ? top > kNone : (top - m) * c > kHeadroom)) {
-                const float up = of_halves(fmaxf(top, m), true);
-                const float by = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - up) * c);
-                sum *= by;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[dt] *= by;
-                m = up;
-                mc = m == kNone ? 0.0f : m * c;
-            }
-            bf16x8 pr[4][NP];
+                for (int r = 0; r < 16; ++r) {
+                    s[mt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][r], c, -mc));
+                    sum += s[mt][r];
+                }
+            const __bf16 *const v = lds[j & 1].v + li * VS + 8 * g;
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) {
                 float x[8];
+                bf16x8 pr[NP];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ks / 2][8 * (ks % 2) + e], c, -mc));
-                    sum += x[e];
-                }
-                take_apart<NP>(x, pr[ks]);
-            }
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
+                for (int e = 0; e < 8; ++e) x[e] = s[ks / 2][8 * (ks % 2) + e];
+                take_apart<NP>(x, pr);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    const bf16x8 v = *reinterpret_cast<const bf16x8 *>(buf.v + (32 * dt + li) * VS + 16 * ks + 8 * g);
+                    const bf16x8 y = *reinterpret_cast<const bf16x8 *>(v + 32 * dt * VS + 16 * ks);
 #pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) o[dt] = mfma32(v, pr[ks][p], o[dt]);
-                }
-            if (mask) {
-                // As in attend: values that are not finite make the rows NaN that see them.
-                unsigned any = 0;
-                if (lane < D / 32 * kChunk / 4) any = reinterpret_cast<const unsigned *>(&buf.wrong[0][0])[lane];
-                if (__ballot(any != 0)) {
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        f32x16 seen = {};
-#pragma unroll
-                        for (int ks = 0; ks < 4; ++ks) {
-                            bf16x8 is, sees;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const int token = token0 + 16 * ks + 8 * (e / 4) + e % 4;
-                                is[e] = static_cast<__bf16>(buf.wrong[dt][16 * ks + 8 * g + e] ? 1.0f : 0.0f);
-                                sees[e] = static_cast<__bf16>(token >= begin && token < end ? 1.0f : 0.0f);
-                            }
-                            seen = mfma32(is, sees, seen);
-                        }
-                        o[dt] += seen[0] > 0.0f ? __builtin_nanf("") : 0.0f;
-                    }
+                    for (int p = NP - 1; p >= 0; --p) o[dt] = mfma32(y, pr[p], o[dt]);
                 }
             }
+            if (mask) note_wrong(j);
         }
         __syncthreads();
     }
 
     if (wave * kWaveRows + li >= t.n) return;
     sum = of_halves(sum, false);
-    if (count > 1) {
-        float *p = partial_at<ROWS, D>(a, split, tile, head, wave * kWaveRows + li);
+    if (lost) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] += lost >> dt & 1u ? __builtin_nanf("") : 0.0f;
+    }
+    if (!part.whole()) {
+        float *p = partial_at<ROWS, D>(a, part.slot(piece), wave * kWaveRows + li);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -688,7 +910,7 @@ __global__ __launch_bounds__((64 * kPieceWaves<T, D>), (kPiecePerSimd<T, D>)) vo
         }
         return;
     }
-    T *out = out_at<T>(a, t, head, row);
+    T *out = out_at<T>(a, part.seq.first, head, row);
     const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -696,31 +918,47 @@ __global__ __launch_bounds__((64 * kPieceWaves<T, D>), (kPiecePerSimd<T, D>)) vo
         for (int r = 0; r < 16; ++r) out[32 * dt + 8 * (r / 4) + 4 * g + r % 4] = static_cast<T>(o[dt][r] * by);
 }
 
+template <typename T, int D>
+__global__ __launch_bounds__((64 * kPieceWaves<T, D>), (kPiecePerSimd<T, D>)) void cache_attention_piece_kernel(Args) {
+    constexpr int ROWS = kPieceRows<T, D>;
+    __shared__ Widened<D> lds[2];
+    __shared__ Piece<ROWS> piece;
+    // Workgroup b runs on XCD b % 8; each XCD takes a range of the line, whose neighbours
+    // are tiles that read the same chunks.
+    const int nb = gridDim.x, id = blockIdx.x, xcd = id & 7;
+    const int group = xcd * (nb >> 3) + min(xcd, nb & 7) + (id >> 3);
+    for_parts<ROWS, true>(group, piece, [&](const Args &a, const Part<ROWS> &part) { many_rows<T, D>(a, part, piece, lds); });
+}
+
 // ---------------------------------------------------------------------------
-// The splits of a tile in one, in a fixed order
+// The parts of a tile in one, in their order
 // ---------------------------------------------------------------------------
-// A row's state over the splits z, z + by, ..., EACH elements of it from p on; `ahead`
-// splits' loads are in flight together.
+// A row's state over the parts z, z + by, ... of its tile, EACH elements of it; the loads
+// of some parts are in flight together.
 template <int EACH>
 struct Joined {
     float m = kNone, l = 0.0f, o[EACH] = {};
 
-    // p: the element of split 0, ml: its maximum and sum, `step` floats from split to split.
-    __device__ void add(const float *p, const float *ml, int64_t step, int z, int by, int count, float c) {
+    // state(z): a part's row.
+    template <typename F>
+    __device__ void add(F &&state, int e0, int d, int z, int by, int count, float c) {
         constexpr int AHEAD = 8;
         for (; z < count; z += AHEAD * by) {
             float pm[AHEAD], pl[AHEAD], po[AHEAD][EACH], up = m;
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
-                const int64_t at = min(z + i * by, count - 1) * step;
-                pm[i] = z + i * by < count ? ml[at] : kNone;
-                pl[i] = ml[at + 1];
+                const float *p = state(min(z + i * by, count - 1));
+                pm[i] = z + i * by < count ? p[d] : kNone;
+                pl[i] = p[d + 1];
 #pragma unroll
-                for (int e = 0; e < EACH; ++e) po[i][e] = p[at + e];
+                for (int e = 0; e < EACH; ++e) po[i][e] = p[e0 + e];
             }
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) up = fmaxf(up, pm[i]);
-            scale(weight_of(m, up, c));
+            const float keep = weight_of(m, up, c);
+            l *= keep;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) o[e] *= keep;
             m = up;
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
@@ -732,56 +970,51 @@ struct Joined {
             }
         }
     }
-    __device__ void scale(float by) {
-        l *= by;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) o[e] *= by;
-    }
 };
 
-// Few splits: 16 lanes a row, 16 rows a workgroup.  Many (WIDE): a workgroup a row, its
-// waves every fourth split each.
+// A workgroup joins rows of the tile that its group of the launch before has begun, 16
+// lanes a row: 16 rows, or, of tiles of many parts (WIDE), four, whose parts its waves
+// share.
 template <typename T, int D, int ROWS, bool WIDE>
-__global__ __launch_bounds__(256) void join_splits_kernel(Args a) {
-    constexpr int PER = WIDE ? 1 : 16, LANES = WIDE ? 64 : 16, EACH = D / LANES;   // rows, lanes of one, their elements
-    const int tile = blockIdx.x / (ROWS / PER), head = blockIdx.y;
-    Tile t;
-    if (!tile_at<ROWS>(a, tile, &t)) return;
-    const int count = split_count(a, t);
-    const int r = blockIdx.x % (ROWS / PER) * PER + (WIDE ? 0 : threadIdx.x / LANES);
-    if (count == 1 || r >= t.n) return;
-    const int e0 = threadIdx.x % LANES * EACH;
-    const float *const row = partial_at<ROWS, D>(a, 0, tile, head, r);
-    const int64_t step = partial_at<ROWS, D>(a, 1, tile, head, r) - row;
+__global__ __launch_bounds__(256) void join_parts_kernel(Args a) {
+    constexpr int LANES = 16, EACH = D / LANES, WAVES = 4;
+    const int group = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64, e0 = lane % LANES * EACH;
+    const int r0 = WIDE ? blockIdx.y * 4 : blockIdx.y * 16 + 4 * wave;
+    const Begun tile = a.begun[group];
+    if (tile.parts == 0 || r0 >= tile.n) return;
+    const int r = min(r0 + lane / LANES, tile.n - 1);
     Joined<EACH> j;
+    j.add([&](int z) { return partial_at<ROWS, D>(a, 2 * (group + z) + (z == 0 ? 1 : 0), r); }, e0, D, WIDE ? wave : 0,
+          WIDE ? WAVES : 1, tile.parts, a.c);
     if constexpr (!WIDE) {
-        j.add(row + e0, row + D, step, 0, 1, count, a.c);
-        T *out = out_at<T>(a, t, head, t.row0 + r) + e0;
+        if (r0 + lane / LANES >= tile.n) return;
+        T *out = out_at<T>(a, tile.first, tile.head, tile.row0 + r) + e0;
         const float by = j.l == 0.0f ? 0.0f : 1.0f / j.l;
 #pragma unroll
         for (int e = 0; e < EACH; ++e) out[e] = static_cast<T>(j.o[e] * by);
     } else {
-        __shared__ float o_lds[4][D], ml_lds[4][2];
-        const int wave = threadIdx.x / 64;
-        j.add(row + e0, row + D, step, wave, 4, count, a.c);
+        __shared__ float o_lds[WAVES][4][D], ml_lds[WAVES][4][2];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) o_lds[wave][e0 + e] = j.o[e];
+        for (int e = 0; e < EACH; ++e) o_lds[wave][lane / LANES][e0 + e] = j.o[e];
         if (e0 == 0) {
-            ml_lds[wave][0] = j.m;
-            ml_lds[wave][1] = j.l;
+            ml_lds[wave][lane / LANES][0] = j.m;
+            ml_lds[wave][lane / LANES][1] = j.l;
         }
         __syncthreads();
-        if (threadIdx.x >= D) return;
-        float all = kNone, sum = 0.0f, x = 0.0f;
+        for (int i = threadIdx.x; i < 4 * D; i += 256) {
+            const int row = i / D, e = i % D;
+            if (r0 + row >= tile.n) break;
+            float all = kNone, sum = 0.0f, x = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) all = fmaxf(all, ml_lds[w][0]);
+            for (int w = 0; w < WAVES; ++w) all = fmaxf(all, ml_lds[w][row][0]);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float by = weight_of(ml_lds[w][0], all, a.c);
-            sum = __builtin_fmaf(ml_lds[w][1], by, sum);
-            x = __builtin_fmaf(o_lds[w][threadIdx.x], by, x);
+            for (int w = 0; w < WAVES; ++w) {
+                const float by = weight_of(ml_lds[w][row][0], all, a.c);
+                sum = __builtin_fmaf(ml_lds[w][row][1], by, sum);
+                x = __builtin_fmaf(o_lds[w][row][e], by, x);
+            }
+            out_at<T>(a, tile.first, tile.head, tile.row0 + r0 + row)[e] = static_cast<T>(sum == 0.0f ? 0.0f : x / sum);
         }
-        out_at<T>(a, t, head, t.row0 + r)[threadIdx.x] = static_cast<T>(sum == 0.0f ? 0.0f : x / sum);
     }
 }
 
@@ -792,103 +1025,95 @@ __global__ __launch_bounds__(256) void join_splits_kernel(Args a) {
 // both kinds.
 constexpr int kFewRows = 32;
 
-// What writing a tile's partial state and reading it again costs, in chunks.
-constexpr int kStateChunks = 7;
-#ifndef FEW_TARGET
-#define FEW_TARGET 1024
-#endif
-
 // A launch over the sequences of [from, to] rows.
 struct Launch {
-    int from = 1, to = 0, tiles = 0, splits = 1, least = 1;
+    int from = 1, to = 0, groups = 0, least = 1;
+    bool whole = false;   // a group a tile
+    bool wide = false;    // tiles have many parts
     bool some() const { return from <= to; }
-    int64_t partial(const KvCache &cache, int rows) const {
-        return some() && splits > 1
-                   ? static_cast<int64_t>(splits) * tiles * cache.heads * rows * (cache.d + 4) : 0;
+    // Words of workspace: the states, then what has been begun (a multiple of 16 bytes).
+    int64_t partial(int d, int rows) const { return some() && !whole ? 2LL * groups * rows * (d + 4) : 0; }
+    int64_t words(int d, int rows) const {
+        return some() && !whole ? partial(d, rows) + (groups * (sizeof(Begun) / 4) + 3) / 4 * 4 : 0;
+    }
+    // `tiles` of up to n chunks: on `room` groups at once, each of at least `each` chunks
+    // but where there are more tiles; where n is at most `small`, a group a tile.
+    void divide(int64_t tiles, int64_t n, int each, int small, int room) {
+        least = each;
+        whole = n <= small;
+        const int64_t fit = std::max<int64_t>(tiles, tiles * n / each);
+        groups = static_cast<int>(whole ? tiles : std::min<int64_t>(fit, room));
+        wide = groups > 8 * tiles;
     }
 };
 struct Plan {
     Launch few, many;
+    bool team = false;   // the few rows' kernel
 };
 
 int piece_rows(int d, int dtype) { return d == 128 && dtype == 0 ? kPieceRows<__bf16, 128> : kPieceRows<float, 64>; }
-static_assert(kPieceRows<float, 128> == kPieceRows<float, 64> && kPieceRows<__bf16, 64> == kPieceRows<float, 64>, "piece_rows");
 
 Plan plan_of(const KvCache &cache, const KvBatch &batch, int T, int H, int window, int dtype) {
     Plan p;
     const int group = H / cache.heads, most = std::min(batch.B, T);
     const int64_t rows = static_cast<int64_t>(T) * group;
     const bool pieces = rows > static_cast<int64_t>(kFewRows) * batch.B;
-    const int64_t cached = static_cast<int64_t>(batch.W) * (cache.page / kChunk);
     const auto chunks = [&](int tile_rows) {   // that a tile sees, at most
-        return window ? std::min<int64_t>(cached, (static_cast<int64_t>(window) + tile_rows / group) / kChunk + 2) : cached;
+        const int64_t cached = static_cast<int64_t>(batch.W) * (cache.page / kChunk);
+        return window ? std::min<int64_t>(cached, (static_cast<int64_t>(window) + tile_rows / group) / kChunk + 3) : cached;
     };
     if (!pieces || batch.B > 1) {
-        Launch &f = p.few;
-        f.to = pieces ? kFewRows : INT32_MAX;
-        f.tiles = static_cast<int>(pieces ? std::min<int64_t>(rows, most * static_cast<int64_t>(kFewRows / kRows))
-                                          : (rows + static_cast<int64_t>(most) * (kRows - 1)) / kRows);
-        f.least = 2 * kWaves;
-        const int64_t work = static_cast<int64_t>(f.tiles) * cache.heads;
-        f.splits = static_cast<int>(std::min<int64_t>(
-            {(FEW_TARGET + work - 1) / work, std::max<int64_t>((chunks(kRows) + f.least - 1) / f.least, 1), 256}));
+        p.few.to = pieces ? kFewRows : INT32_MAX;
+        const int64_t tiles = cache.heads * (pieces ? std::min<int64_t>(rows, most * static_cast<int64_t>(kFewRows / kRows))
+                                                    : (rows + static_cast<int64_t>(most) * (kRows - 1)) / kRows);
+        // Eight waves a CU, alone or together.  Alone they divide many tiles without
+        // waiting for each other; of few tiles they would leave too many parts.
+        const int64_t n = chunks(kRows);
+        p.team = n <= kTeamChunks || tiles * 8 <= 256;
+        if (p.team) p.few.divide(tiles, n, 2 * kTeamWaves, kTeamChunks, 256);
+        else p.few.divide(tiles, n, 4, 0, 8 * 256);
     }
     if (pieces) {
-        Launch &m = p.many;
         const int each = piece_rows(cache.d, dtype);
-        m.from = batch.B > 1 ? kFewRows + 1 : 1;
-        m.to = INT32_MAX;
-        const int64_t seqs = std::min<int64_t>(most, rows / m.from);
-        m.tiles = static_cast<int>((rows + seqs * (each - 1)) / each);
-        m.least = 8;
-        // Splits by the time they take in chunks: the rounds of workgroups on 256 CUs (of
-        // sequences of equal rows), each as long as its chunks and, with splits, the
-        // states that it writes and that are read again.
-        const int64_t tiles = batch.B * ((rows / batch.B + each - 1) / each) * cache.heads, n = chunks(each);
-        const int64_t at_once = 256 * (cache.d == 128 ? 1 : 2);
-        int64_t best = 0;
-        for (int64_t z = 1; z <= 32 && (z == 1 || z * m.least <= n); ++z) {
-            const int64_t cost = (tiles * z + at_once - 1) / at_once * ((n + z - 1) / z + (z > 1 ? kStateChunks : 0));
-            if (z == 1 || cost < best) {
-                best = cost;
-                m.splits = static_cast<int>(z);
-            }
-        }
+        p.many.from = batch.B > 1 ? kFewRows + 1 : 1;
+        p.many.to = INT32_MAX;
+        const int64_t seqs = std::min<int64_t>(most, rows / p.many.from);
+        p.many.divide(cache.heads * ((rows + seqs * (each - 1)) / each), chunks(each), 8, 8, cache.d == 128 ? 256 : 512);
     }
     return p;
 }
 
-Args with(Args a, const Launch &l, float *partial) {
+Args with(Args a, const Launch &l, float *workspace, int rows) {
     a.from = l.from;
     a.to = l.to;
-    a.tiles = l.tiles;
-    a.splits = l.splits;
+    a.groups = l.groups;
     a.least = l.least;
-    a.partial = partial;
+    a.whole = l.whole;
+    a.partial = workspace;
+    a.begun = reinterpret_cast<Begun *>(workspace + l.partial(a.cache.d, rows));
     return a;
 }
 
 template <typename T, int D, int ROWS>
-void join(const Args &a, hipStream_t stream) {
-    if (a.splits == 1) return;
-    const dim3 rows(static_cast<unsigned>(a.tiles) * ROWS, a.cache.heads);
-    if (a.splits > 8) join_splits_kernel<T, D, ROWS, true><<<rows, 256, 0, stream>>>(a);
-    else join_splits_kernel<T, D, ROWS, false><<<dim3(rows.x / 16, rows.y), 256, 0, stream>>>(a);
+void join(const Args &a, const Launch &l, hipStream_t stream) {
+    if (l.whole) return;
+    if (l.wide) join_parts_kernel<T, D, ROWS, true><<<dim3(a.groups, ROWS / 4), 256, 0, stream>>>(a);
+    else join_parts_kernel<T, D, ROWS, false><<<dim3(a.groups, ROWS / 16), 256, 0, stream>>>(a);
 }
 
 template <typename T, int D>
 hipError_t run(const Args &args, const Plan &p, float *workspace, hipStream_t stream) {
-    const unsigned heads = args.cache.heads;
     if (p.few.some()) {
-        const Args a = with(args, p.few, workspace);
-        cache_attention_kernel<T, D><<<dim3(a.tiles, heads, a.splits), 64 * kWaves, 0, stream>>>(a);
-        join<T, D, kRows>(a, stream);
+        const Args a = with(args, p.few, workspace, kRows);
+        if (p.team) cache_attention_team_kernel<T, D><<<a.groups, 64 * kTeamWaves, 0, stream>>>(a);
+        else cache_attention_kernel<T, D><<<(a.groups + kWaves - 1) / kWaves, 64 * kWaves, 0, stream>>>(a);
+        join<T, D, kRows>(a, p.few, stream);
     }
     if (p.many.some()) {
-        const Args a = with(args, p.many, workspace + p.few.partial(args.cache, kRows));
-        cache_attention_piece_kernel<T, D><<<static_cast<unsigned>(a.tiles) * heads * a.splits, (64 * kPieceWaves<T, D>), 0,
-                                             stream>>>(a);
-        join<T, D, kPieceRows<T, D>>(a, stream);
+        constexpr int ROWS = kPieceRows<T, D>;
+        const Args a = with(args, p.many, workspace + p.few.words(D, kRows), ROWS);
+        cache_attention_piece_kernel<T, D><<<a.groups, (64 * kPieceWaves<T, D>), 0, stream>>>(a);
+        join<T, D, ROWS>(a, p.many, stream);
     }
     return hipGetLastError();
 }
@@ -898,7 +1123,7 @@ hipError_t run(const Args &args, const Plan &p, float *workspace, hipStream_t st
 int64_t cache_attention_workspace(const KvCache &cache, const KvBatch &batch, int T, int H, int window, int dtype) {
     if (T == 0 || batch.B == 0 || H == 0) return 0;
     const Plan p = plan_of(cache, batch, T, H, window, dtype);
-    return 4 * (p.few.partial(cache, kRows) + p.many.partial(cache, piece_rows(cache.d, dtype)));
+    return 4 * (p.few.words(cache.d, kRows) + p.many.words(cache.d, piece_rows(cache.d, dtype)));
 }
 
 hipError_t launch_cache_attention(const KvCache &cache, const KvBatch &batch, const KvQueries &rows, void *workspace,
@@ -907,7 +1132,7 @@ hipError_t launch_cache_attention(const KvCache &cache, const KvBatch &batch, co
     // At least 2^-126, which makes exp2 of any finite score 1 as a scale of 0 does, and
     // leaves masked scores at minus infinity.
     const float c = std::max(std::fabs(rows.scale) * 1.44269504088896340736f, 1.17549435e-38f);
-    const Args a{cache, batch, rows, c, rows.H / cache.heads, 0, 0, 0, 0, 0, nullptr};
+    const Args a{cache, batch, rows, c, rows.H / cache.heads, 0, 0, 0, 0, false, nullptr, nullptr};
     const Plan p = plan_of(cache, batch, rows.T, rows.H, rows.window, dtype);
     float *w = static_cast<float *>(workspace);
     if (dtype == 0) return cache.d == 128 ? run<__bf16, 128>(a, p, w, stream) : run<__bf16, 64>(a, p, w, stream);

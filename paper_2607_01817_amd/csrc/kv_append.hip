@@ -84,18 +84,21 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
     constexpr int UNITS = D / 8, PER = 256 / UNITS;   // lanes of a token, tokens at once
     __shared__ unsigned char values[D / 2][kChunk];
     __shared__ unsigned char scales[2][D / kv::kBlock][kChunk];
-    int b, tile;
+    int b;
+    int64_t before;
     kv::Sequence seq;
     const int64_t room = static_cast<int64_t>(batch.W) * cache.page;
     // Chunks that hold new tokens with a place.
     const auto chunks = [&](const kv::Sequence &s) {
         const int64_t lo = max(s.length - s.n, 0), hi = min(static_cast<int64_t>(s.length), room);
-        return lo >= hi ? 0 : static_cast<int>((hi + kChunk - 1) / kChunk - lo / kChunk);
+        return lo >= hi ? 0 : (hi + kChunk - 1) / kChunk - lo / kChunk;
     };
-    if (!kv::find_tile(batch, rows.T, blockIdx.x, chunks, &b, &tile, &seq)) return;
+    if (!kv::find_unit(batch, rows.T, blockIdx.x, chunks, &b, &before, &seq)) return;
+    b = kv::uniform(b);
+    seq = {kv::uniform(seq.first), kv::uniform(seq.n), kv::uniform(seq.length)};
     const int head = blockIdx.y;
     const int lo = max(seq.length - seq.n, 0);
-    const int chunk = lo / kChunk + tile;
+    const int chunk = lo / kChunk + kv::uniform(static_cast<int>(blockIdx.x - before));
     const int64_t at = static_cast<int64_t>(chunk) * kChunk;   // the chunk's first token
     const int t0 = static_cast<int>(max<int64_t>(lo - at, 0));
     const int t1 = static_cast<int>(min<int64_t>(min(static_cast<int64_t>(seq.length), room) - at, kChunk));

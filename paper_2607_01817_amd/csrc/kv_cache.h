@@ -58,32 +58,64 @@ __device__ inline Sequence sequence(const KvBatch &batch, int b, int rows) {
     return {s0, s1 - s0, max(batch.lengths[b], 0)};
 }
 
-// The sequence and its tile that tile `at` of a launch is, where tiles(sequence)
-// says how many a sequence has; false past the last.  Called by whole waves, all
-// lanes with the same `at`: 64 sequences at a time.
+// A value that is alike in all lanes, as a scalar.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+    const unsigned lo = __builtin_amdgcn_readfirstlane(static_cast<int>(x));
+    return static_cast<int64_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32))) << 32 | lo;
+}
+
+// Sums over a batch's sequences of what units(sequence, &a, &b) adds to a and b.
+// Called by whole waves.
 template <typename F>
-__device__ inline bool find_tile(const KvBatch &batch, int rows, int64_t at, F &&tiles, int *b, int *tile, Sequence *seq) {
+__device__ inline void add_up(const KvBatch &batch, int rows, F &&units, int64_t *a, int64_t *b) {
+    *a = *b = 0;
+    if (batch.B == 1) return units(sequence(batch, 0, rows), a, b);
+    for (int i = threadIdx.x % 64; i < batch.B; i += 64) units(sequence(batch, i, rows), a, b);
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) {
+        *a += __shfl_xor(*a, step);
+        *b += __shfl_xor(*b, step);
+    }
+}
+
+// The sequence that unit `at` of a batch belongs to, and the units before it, where
+// units(sequence) says how many a sequence has; false past the last.  Called by whole
+// waves, all lanes with the same `at`: 64 sequences at a time.
+template <typename F>
+__device__ inline bool find_unit(const KvBatch &batch, int rows, int64_t at, F &&units, int *b, int64_t *before,
+                                 Sequence *seq) {
+    if (batch.B == 1) {
+        *b = 0;
+        *before = 0;
+        *seq = sequence(batch, 0, rows);
+        return at < units(*seq);
+    }
     const int lane = threadIdx.x % 64;
+    int64_t past = 0;   // units of the sequences that have been passed
     for (int base = 0; base < batch.B; base += 64) {
         const int i = base + lane;
         Sequence s{0, 0, 0};
-        if (i < batch.B) s = sequence(batch, i, rows);
-        const int count = i < batch.B ? tiles(s) : 0;
-        int64_t upto = count;
+        int64_t count = 0;
+        if (i < batch.B) {
+            s = sequence(batch, i, rows);
+            count = units(s);
+        }
+        int64_t upto = past + count;
 #pragma unroll
         for (int step = 1; step < 64; step *= 2) {
-            const int64_t below = __shfl_up(upto, step);
+            const int64_t below = __shfl_up(upto - past, step);
             if (lane >= step) upto += below;
         }
-        const uint64_t past = __ballot(upto > at);
-        if (past) {
-            const int hit = __ffsll(static_cast<unsigned long long>(past)) - 1;
+        const uint64_t hits = __ballot(upto > at);
+        if (hits) {
+            const int hit = __ffsll(static_cast<unsigned long long>(hits)) - 1;
             *b = base + hit;
-            *tile = static_cast<int>(at - __shfl(upto - count, hit));
+            *before = __shfl(upto - count, hit);
             *seq = {__shfl(s.first, hit), __shfl(s.n, hit), __shfl(s.length, hit)};
             return true;
         }
-        at -= __shfl(upto, 63);
+        past = __shfl(upto, 63);
     }
     return false;
 }
