@@ -58,6 +58,7 @@ constexpr float kNone = -__builtin_inff();
 // How far a row's scores may pass its running maximum before O and the sum are
 // rescaled: probabilities stay below 2^8.
 constexpr float kHeadroom = 8.0f;
+constexpr float kMostSum = 256.0f;   // 2^kHeadroom, of a chunk's probabilities together
 
 struct Args {
     KvCache cache;
@@ -362,6 +363,10 @@ __device__ inline float over_groups(float x, bool maximum) {   // lanes l, l ^ 1
     return maximum ? fmaxf(x, z) : x + z;
 }
 
+// The larger one, up to fp32's largest: the median with that, one instruction, where
+// fmaxf makes each operand a quiet NaN first.  A NaN does not count.
+__device__ inline float larger(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, 3.4028235e38f); }
+
 // Bytes of x that are 253 or more: scales whose values bf16 does not hold.
 __device__ inline unsigned not_finite(unsigned x) { return ((x & 0x7F7F7F7Fu) + 0x03030303u) & x & 0x80808080u; }
 
@@ -402,11 +407,10 @@ __device__ inline void attend(const Args &a, const Raw<D> &raw, const bf16x8 (&q
                 s[i][e] = t >= begin && t < end ? s[i][e] : kNone;
             }
     }
-    float top = kNone;
+    float tops[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
+    for (int i = 0; i < 4; ++i) tops[i] = larger(larger(s[i][0], s[i][1]), larger(s[i][2], s[i][3]));
+    const float top = larger(larger(tops[0], tops[1]), larger(tops[2], tops[3]));
     if (__ballot(top > st.limit)) {
         const float m = over_groups(fmaxf(top, st.m), true);
         const float by = st.m == kNone ? 0.0f : __builtin_amdgcn_exp2f((st.m - m) * c);
@@ -726,6 +730,18 @@ __device__ inline float of_halves(float x, bool maximum) {
     return maximum ? fmaxf(lo, hi) : lo + hi;
 }
 
+// A hint to the scheduler: N operands are read from LDS, each for NP products, AHEAD of
+// them before the first product and each of the others behind another one's.
+template <int N, int NP, int AHEAD>
+__device__ inline void in_order() {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);   // LDS reads
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);   // products
+        if (i + AHEAD < N) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+}
+
 // Lane (li, g) of a wave: of a chunk's scores the row li and the tokens 32 mt + 8 (r / 4)
 // + 4 g + r % 4 in s[mt][r], of the output the elements 32 dt + 8 (r / 4) + 4 g + r % 4
 // in o[dt][r].
@@ -818,11 +834,39 @@ __device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &pa
                 if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // else all comparisons' masks at once
             }
     };
-    const auto maximum = [&](const f32x16 (&s)[2]) {   // of the chunk's scores of the row
-        float top = kNone;
+    // Probabilities against the running maximum, and the lane's sum of them.
+    const auto weights = [&](const f32x16 (&s)[2], bf16x8 (&pr)[4][NP]) {
+        float all = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, fmaxf(s[0][r], s[1][r]));
-        return of_halves(top, true);
+        for (int ks = 0; ks < 4; ++ks) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ks / 2][8 * (ks % 2) + e], c, -mc));
+                all += x[e];
+            }
+            take_apart<NP>(x, pr[ks]);
+        }
+        return all;
+    };
+    const auto product = [&](int j, const bf16x8 (&pr)[4][NP]) {
+        const __bf16 *const v = lds[j & 1].v + li * VS + 8 * g;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const bf16x8 x = *reinterpret_cast<const bf16x8 *>(v + 32 * dt * VS + 16 * ks);
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) o[dt] = mfma32(x, pr[ks][p], o[dt]);
+            }
+    };
+    const auto maximum = [&](const f32x16 (&s)[2]) {   // of the chunk's scores of the row
+        float top[2] = {kNone, kNone};
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) top[mt] = larger(top[mt], s[mt][r]);
+        return of_halves(larger(top[0], top[1]), true);
     };
     const auto raise = [&](float to) {
         const float by = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
@@ -860,33 +904,31 @@ __device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &pa
         if (active) {
             f32x16 s[2];
             scores(j, s);
+            in_order<2 * KK, NP, 6>();
             const bool mask = masked(j);
             if (mask) hide(j, s);
-            const float top = maximum(s);
-            if (__ballot(m == kNone ? top > kNone : (top - m) * c > kHeadroom)) raise(fmaxf(m, top));
-            // In place of the scores: their parts, three to each, only where they are used.
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[mt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][r], c, -mc));
-                    sum += s[mt][r];
+            if constexpr (NP == 1) {
+                // The maximum is raised, and the chunk's probabilities taken again, where their
+                // sum passes kMostSum, so that none is needed otherwise, and set by the first
+                // chunk of which a row sees something.
+                bf16x8 pr[4][NP];
+                float all = weights(s, pr);
+                const bool high = of_halves(all, false) > kMostSum;
+                if (__ballot(high || m == kNone)) {
+                    const float top = maximum(s);
+                    raise(high || m == kNone ? fmaxf(m, top) : m);
+                    all = weights(s, pr);
                 }
-            const __bf16 *const v = lds[j & 1].v + li * VS + 8 * g;
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                float x[8];
-                bf16x8 pr[NP];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = s[ks / 2][8 * (ks % 2) + e];
-                take_apart<NP>(x, pr);
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    const bf16x8 y = *reinterpret_cast<const bf16x8 *>(v + 32 * dt * VS + 16 * ks);
-#pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) o[dt] = mfma32(y, pr[p], o[dt]);
-                }
+                sum += all;
+                product(j, pr);
+            } else {
+                const float top = maximum(s);
+                if (__ballot(m == kNone ? top > kNone : (top - m) * c > kHeadroom)) raise(fmaxf(m, top));
+                bf16x8 pr[4][NP];
+                sum += weights(s, pr);
+                product(j, pr);
             }
+            in_order<4 * DT, NP, 6>();
             if (mask) note_wrong(j);
         }
         __syncthreads();
