@@ -69,7 +69,7 @@ struct Args {
     int from, to;     // the launch takes the sequences of [from, to] rows
     int groups;       // workgroups
     int least;        // chunks of a workgroup, at least, but where there are more tiles
-    bool whole;       // a workgroup a tile
+    bool whole;       // a group a tile
     struct Begun *begun;   // [groups]
     float *partial;        // [2 groups][rows of a tile][d + 4]: states of parts of tiles
 };
@@ -82,7 +82,7 @@ struct Begun {
 };
 
 // The division of a launch's work.  A tile is some rows of a sequence and key head and
-// weighs as many chunks as they see (if `whole`, 1).  All tiles lie one behind the other,
+// weighs as many chunks as they see.  All tiles lie one behind the other,
 // the tiles of a sequence and head in a row, sequence by sequence, head by head, and each
 // workgroup takes an equal piece of that line: the end of one tile, whole ones, and the
 // beginning of another.  Lengths are read here, so the pieces are equal whatever the
@@ -124,8 +124,6 @@ struct Tiles {
         const int rows = s.n * a.group;
         if (rows < a.from || rows > a.to) return;
         count = (rows + ROWS - 1) / ROWS;
-        first = 1;
-        if (a.whole) return;
         const Tile x = tile_of<ROWS>(a, s, 0), y = tile_of<ROWS>(a, s, count - 1);
         first = max(x.c1 - x.c0, 1);
         rise = count < 2 ? 0.0 : static_cast<double>(max(y.c1 - y.c0 - first, 0)) / (2.0 * (count - 1));
@@ -164,7 +162,7 @@ struct Work {
         all = head * a.cache.heads;
         tiles *= a.cache.heads;
         const int64_t fit = static_cast<int64_t>(static_cast<double>(all) / a.least);
-        groups = static_cast<int>(a.whole ? all : min(max(tiles, fit), static_cast<int64_t>(a.groups)));
+        groups = static_cast<int>(min(max(tiles, fit), static_cast<int64_t>(a.groups)));
         each = static_cast<double>(all) / max(groups, 1);
     }
     __device__ int64_t begin(int group) const { return group < groups ? static_cast<int64_t>(group * each) : all; }
@@ -185,6 +183,22 @@ struct Part {
     int b, k, head;
     kv::Sequence seq;
     int u0, u1, weight;
+    // Where a group takes a tile: the heads of a tile in a row; false past the last tile.
+    __device__ bool whole_tile(const Args &a, int group) {
+        const int unit = group / a.cache.heads;
+        int64_t before = 0;
+        if (!kv::find_unit(a.batch, a.rows.T, unit, [&](const kv::Sequence &s) {
+                const int rows = s.n * a.group;
+                return static_cast<int64_t>(rows < a.from || rows > a.to ? 0 : (rows + ROWS - 1) / ROWS);
+            }, &b, &before, &seq))
+            return false;
+        head = group % a.cache.heads;
+        k = unit - static_cast<int>(before);
+        u0 = 0;
+        u1 = weight = 1;
+        return true;
+    }
+    Part() = default;
     // The part that begins at unit `at` of a line of `of_head` units a head, and ends
     // with its tile or at `end`.
     __device__ Part(const Args &a, int64_t of_head, int64_t at, int64_t end) {
@@ -199,7 +213,9 @@ struct Part {
         weight = static_cast<int>(t.before(k + 1) - first);
         u0 = static_cast<int>(in - first);
         u1 = static_cast<int>(min(static_cast<int64_t>(weight), u0 + (end - at)));
-        // Alike in all lanes, but reckoned in vector registers: scalar ones are few.
+    }
+    // What is alike in all lanes, but reckoned in vector registers, as scalar ones are few.
+    __device__ void settle() {
         head = kv::uniform(head);
         b = kv::uniform(b);
         k = kv::uniform(k);
@@ -255,30 +271,38 @@ __device__ inline void for_parts(int group, Piece<ROWS> &lds, F &&each) {
     {
         const Args a = arguments();
         if (group >= a.groups) return;
-        const Work<ROWS> work(a);
-        if (writes()) {
-            if (!a.whole) a.begun[group].parts = 0;
-            lds.work = work;
-            lds.at = work.begin(min(group, work.groups));
-            lds.end = work.begin(min(group + 1, work.groups));
-            lds.group = group;
-        }
-    }
-    while (true) {
-        sync();
-        const int64_t at = lds.at, end = lds.end;
-        if (kv::uniform(static_cast<int>(at >= end))) return;
-        const Args a = arguments();
-        const Part<ROWS> part(a, lds.work.head, at, end);
-        sync();
-        if (writes()) {
-            lds.at = at + (part.u1 - part.u0);
-            if (part.u0 == 0 && part.u1 < part.weight) {   // the last one
-                const Tile t = tile_of<ROWS>(a, part.seq, part.k);
-                a.begun[group] = {lds.work.group_of(at + part.weight - 1) - group + 1, part.head, t.row0, t.n,
-                                  part.seq.first};
+        if (!a.whole) {
+            const Work<ROWS> work(a);
+            if (writes()) {
+                a.begun[group].parts = 0;
+                lds.work = work;
+                lds.at = work.begin(min(group, work.groups));
+                lds.end = work.begin(min(group + 1, work.groups));
+                lds.group = group;
             }
         }
+    }
+    for (bool again = false;; again = true) {
+        const Args a = arguments();
+        Part<ROWS> part;
+        if (a.whole) {
+            if (again || !part.whole_tile(a, group)) return;
+        } else {
+            sync();
+            const int64_t at = lds.at, end = lds.end;
+            if (kv::uniform(static_cast<int>(at >= end))) return;
+            part = Part<ROWS>(a, lds.work.head, at, end);
+            sync();
+            if (writes()) {
+                lds.at = at + (part.u1 - part.u0);
+                if (part.u0 == 0 && part.u1 < part.weight) {   // the last one
+                    const Tile t = tile_of<ROWS>(a, part.seq, part.k);
+                    a.begun[group] = {lds.work.group_of(at + part.weight - 1) - group + 1, part.head, t.row0, t.n,
+                                      part.seq.first};
+                }
+            }
+        }
+        part.settle();
         each(a, part);
     }
 }
@@ -1079,10 +1103,11 @@ struct Launch {
         return some() && !whole ? partial(d, rows) + (groups * (sizeof(Begun) / 4) + 3) / 4 * 4 : 0;
     }
     // `tiles` of up to n chunks: on `room` groups at once, each of at least `each` chunks
-    // but where there are more tiles; where n is at most `small`, a group a tile.
-    void divide(int64_t tiles, int64_t n, int each, int small, int room) {
+    // but where there are more tiles; where n is at most `small`, or `most` and the tiles
+    // alone fill a quarter of the room, a group a tile.
+    void divide(int64_t tiles, int64_t n, int each, int small, int most, int room) {
         least = each;
-        whole = n <= small;
+        whole = n <= small || (n <= most && 4 * tiles >= room);
         const int64_t fit = std::max<int64_t>(tiles, tiles * n / each);
         groups = static_cast<int>(whole ? tiles : std::min<int64_t>(fit, room));
         wide = groups > 8 * tiles;
@@ -1112,15 +1137,16 @@ Plan plan_of(const KvCache &cache, const KvBatch &batch, int T, int H, int windo
         // waiting for each other; of few tiles they would leave too many parts.
         const int64_t n = chunks(kRows);
         p.team = n <= kTeamChunks || tiles * 8 <= 256;
-        if (p.team) p.few.divide(tiles, n, 2 * kTeamWaves, kTeamChunks, 256);
-        else p.few.divide(tiles, n, 4, 0, 8 * 256);
+        if (p.team) p.few.divide(tiles, n, 2 * kTeamWaves, kTeamChunks, kTeamChunks, 256);
+        else p.few.divide(tiles, n, 4, 0, 0, 8 * 256);
     }
     if (pieces) {
         const int each = piece_rows(cache.d, dtype);
         p.many.from = batch.B > 1 ? kFewRows + 1 : 1;
         p.many.to = INT32_MAX;
         const int64_t seqs = std::min<int64_t>(most, rows / p.many.from);
-        p.many.divide(cache.heads * ((rows + seqs * (each - 1)) / each), chunks(each), 8, 8, cache.d == 128 ? 256 : 512);
+        p.many.divide(cache.heads * ((rows + seqs * (each - 1)) / each), chunks(each), 8, 8, 32,
+                      cache.d == 128 ? 256 : 512);
     }
     return p;
 }

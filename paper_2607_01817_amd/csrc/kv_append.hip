@@ -77,13 +77,18 @@ __device__ inline f32x8 decode(const Coded &c) {
     return v;
 }
 
-// D: elements of a head vector; T: type of the rows; HALF: layout of the pairs.
-template <typename T, int D, bool HALF>
+// Layout of the pairs: neighbours; halves that units of 8 elements do not straddle; any
+// halves.
+enum Pairs { kNeighbours, kHalves, kAnyHalves };
+
+// D: elements of a head vector; T: type of the rows.
+template <typename T, int D, Pairs PAIRS>
 __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch batch, KvRows rows, const float *table,
                                                         RopeAxes ax, const void *positions, bool pos64, int R) {
     constexpr int UNITS = D / 8, PER = 256 / UNITS;   // lanes of a token, tokens at once
     __shared__ unsigned char values[D / 2][kChunk];
     __shared__ unsigned char scales[2][D / kv::kBlock][kChunk];
+    __shared__ float turned[PAIRS == kAnyHalves ? 256 : 1][9];
     int b;
     int64_t before;
     kv::Sequence seq;
@@ -104,21 +109,30 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
     const int t1 = static_cast<int>(min<int64_t>(min(static_cast<int64_t>(seq.length), room) - at, kChunk));
     const int per_page = cache.page / kChunk;
     const int page = batch.page_table[static_cast<int64_t>(b) * batch.W + chunk / per_page];
+    const int u = threadIdx.x % UNITS, e = u * 8;
+    // A token's rows, loaded a turn ahead, the first ones ahead of the page too.
+    int t = t0 + static_cast<int>(threadIdx.x) / UNITS;
+    decltype(load_raw(static_cast<const T *>(nullptr))) raw_k, raw_v;
+    const auto row_of = [&](int t) { return seq.first + static_cast<int64_t>(at + t - (seq.length - seq.n)); };
+    const auto fetch = [&](int t) {
+        if (t >= t1) return;
+        raw_k = load_raw(static_cast<const T *>(rows.k) + row_of(t) * rows.k_token + head * rows.k_head + e);
+        raw_v = load_raw(static_cast<const T *>(rows.v) + row_of(t) * rows.v_token + head * rows.v_head + e);
+    };
+    fetch(t);
     if (page < 0 || page >= cache.pages) return;   // the whole workgroup
     const int64_t block = (static_cast<int64_t>(page) * cache.heads + head) * per_page + chunk % per_page;
     unsigned char *const ck = cache.k + block * kChunk * (D / 2);
     unsigned char *const cv = cache.v + block * kChunk * (D / 2);
     unsigned char *const sk = cache.k_scale + block * kChunk * (D / kv::kBlock);
     unsigned char *const sv = cache.v_scale + block * kChunk * (D / kv::kBlock);
-    const int u = threadIdx.x % UNITS, e = u * 8;
-
     // Every lane of a group of UNITS takes the same way, so those of a block stay together.
-    for (int t = t0 + static_cast<int>(threadIdx.x) / UNITS; t < t1; t += PER) {
+    for (; t < t1; t += PER) {
         const int place = static_cast<int>(at + t);
-        const int64_t row = seq.first + (place - (seq.length - seq.n));
+        const int64_t row = row_of(t);
         const T *k = static_cast<const T *>(rows.k) + row * rows.k_token + head * rows.k_head;
-        const T *v = static_cast<const T *>(rows.v) + row * rows.v_token + head * rows.v_head;
-        const f32x8 xk = widen(load_raw(k + e)), xv = widen(load_raw(v + e));
+        const f32x8 xk = widen(raw_k), xv = widen(raw_v);
+        if constexpr (PAIRS != kAnyHalves) fetch(t + PER);
         float y[8], z[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -130,16 +144,31 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
         asm volatile("" : "+s"(turning));
         if (e < turning) {
             const RopePlace rp = rope_place(ax, positions, pos64, row, place);
-            if constexpr (HALF) {
+            if constexpr (PAIRS == kHalves) {   // all eight are first elements of their pairs, or all second
+                const bool first = e < turning / 2;
+                const int p = first ? e : e - turning / 2;
+                const f32x8 other = widen(load_raw(k + (first ? p + turning / 2 : p)));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    if (e + i >= turning) continue;
+                    const float2 cs = rope_entry(table, rp, p + i);
+                    const double by = first ? -cs.y : cs.y;
+                    y[i] = to_odd(static_cast<double>(xk[i]) * cs.x + static_cast<double>(other[i]) * by);
+                }
+            } else if constexpr (PAIRS == kAnyHalves) {
+                // One element behind the other, in LDS: unrolled, their comparisons take more
+                // scalar registers than there are.
+#pragma unroll
+                for (int i = 0; i < 8; ++i) turned[threadIdx.x][i] = y[i];
+#pragma unroll 1
+                for (int i = 0; i < min(8, turning - e); ++i) {
                     const bool first = e + i < turning / 2;
                     const int p = first ? e + i : e + i - turning / 2;
                     const float2 cs = rope_entry(table, rp, p);
-                    const double mine = xk[i], other = static_cast<float>(k[first ? p + turning / 2 : p]);
-                    y[i] = to_odd(mine * cs.x + (first ? -other : other) * cs.y);
+                    const double mine = turned[threadIdx.x][i], other = static_cast<float>(k[first ? p + turning / 2 : p]);
+                    turned[threadIdx.x][i] = to_odd(mine * cs.x + other * (first ? -cs.y : cs.y));
                 }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = turned[threadIdx.x][i];
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
@@ -165,6 +194,7 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
             store_8(static_cast<T *>(rows.k_held) + o, decode(ek));
             store_8(static_cast<T *>(rows.v_held) + o, decode(ev));
         }
+        if constexpr (PAIRS == kAnyHalves) fetch(t + PER);
     }
     __syncthreads();
     // What the chunk's other tokens hold stays: whole chunks in 16 bytes, else byte by byte.
@@ -200,19 +230,22 @@ hipError_t launch_append_kv(const KvCache &cache, const KvBatch &batch, const Kv
     // Chunks that n new tokens of a sequence can lie in: at most n, and n / 64 + 2.
     const int64_t tiles = std::min<int64_t>(rows.T, rows.T / kChunk + 2LL * batch.B);
     const dim3 grid(static_cast<unsigned>(tiles), cache.heads);
-#define HCMS_RUN(T, D, HALF) \
-    append_kv_kernel<T, D, HALF><<<grid, 256, 0, stream>>>(cache, batch, rows, table, ax, positions, pos64, R)
-#define HCMS_TYPED(T) \
-    if (cache.d == 128 && half) HCMS_RUN(T, 128, true); \
-    else if (cache.d == 128) HCMS_RUN(T, 128, false); \
-    else if (half) HCMS_RUN(T, 64, true); \
-    else HCMS_RUN(T, 64, false)
-    if (dtype == 0) {
-        HCMS_TYPED(__bf16);
+#define HCMS_RUN(T, D, PAIRS) \
+    append_kv_kernel<T, D, PAIRS><<<grid, 256, 0, stream>>>(cache, batch, rows, table, ax, positions, pos64, R)
+#define HCMS_PAIRS(T, D) \
+    if (!half) HCMS_RUN(T, D, kNeighbours); \
+    else if (R % 16 == 0) HCMS_RUN(T, D, kHalves); \
+    else HCMS_RUN(T, D, kAnyHalves)
+    if (dtype == 0 && cache.d == 128) {
+        HCMS_PAIRS(__bf16, 128);
+    } else if (dtype == 0) {
+        HCMS_PAIRS(__bf16, 64);
+    } else if (cache.d == 128) {
+        HCMS_PAIRS(float, 128);
     } else {
-        HCMS_TYPED(float);
+        HCMS_PAIRS(float, 64);
     }
-#undef HCMS_TYPED
+#undef HCMS_PAIRS
 #undef HCMS_RUN
     return hipGetLastError();
 }
