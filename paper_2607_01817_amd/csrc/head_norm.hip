@@ -23,7 +23,7 @@
 namespace hcms {
 namespace {
 
-constexpr int kAhead = 4;           // heads whose loads are in flight together
+constexpr int kAhead = 4;           // heads whose loads are in flight together, at least
 constexpr int kMostPartials = 1024;  // workgroups of the backward
 
 using fp8::f32x8;
@@ -60,6 +60,14 @@ struct Side {
     int64_t dy_token, dy_head;
     const void *w;
 };
+// 1 / sqrt(x) to an ulp: the hardware's with one step of Newton's, a fifth of the
+// instructions of an exact root and division.  Infinity gives 0.
+__device__ inline float inverse_root(float x) {
+    const float r = __builtin_amdgcn_rsqf(x);
+    const float better = __builtin_fmaf(0.5f * r, __builtin_fmaf(-x * r, r, 1.0f), r);
+    return x < __builtin_inff() ? better : r;
+}
+
 // What a launch works on.  A workgroup takes up to `each` heads of one side: its
 // second index counts the queries' groups of heads, then the keys'.
 struct Args {
@@ -128,9 +136,9 @@ __device__ inline void get(float (&v)[8], f32x8 x, bool keep) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = keep ? x[i] : 0.0f;
 }
-template <typename T>
+template <bool ONCE, typename T>
 __device__ inline void put(T *p, const float (&v)[8]) {
-    store_8(p, f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
+    store_8_if<ONCE>(p, f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
 }
 template <bool HALF>
 __device__ inline float dot(const float (&a)[8], const float (&b)[8], const float (&x)[8], const float (&y)[8]) {
@@ -144,7 +152,9 @@ __device__ inline float dot(const float (&a)[8], const float (&b)[8], const floa
     return sum;
 }
 
-template <typename T, bool HALF, int LP>
+// ONCE: head vectors past the caches' keeping.  AHEAD: heads whose loads are in flight
+// together.
+template <typename T, bool HALF, int LP, bool ONCE, int AHEAD>
 __global__ __launch_bounds__(256) void head_norm_kernel(Args a) {
     const int lane = threadIdx.x % LP;
     const int64_t token = block_index() * (256 / LP) + threadIdx.x / LP;
@@ -155,14 +165,14 @@ __global__ __launch_bounds__(256) void head_norm_kernel(Args a) {
     const T *const x = static_cast<const T *>(side.heads.x) + token * side.heads.x_token;
     T *const y = static_cast<T *>(side.heads.y) + token * side.heads.y_token;
     using Raw = decltype(load_raw(static_cast<const T *>(nullptr)));
-    Raw ra[kAhead], rb[kAhead];
-    // Loads of kAhead heads, none behind a branch; heads past the last read it again.
+    Raw ra[AHEAD], rb[AHEAD];
+    // Loads of AHEAD heads, none behind a branch; heads past the last read it again.
     const auto fetch = [&](int h0) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
+        for (int j = 0; j < AHEAD; ++j) {
             const T *p = x + min(h0 + j, group.he - 1) * side.heads.x_head;
-            ra[j] = load_raw(p + sh.e0);
-            if constexpr (HALF) rb[j] = load_raw(p + sh.e1);
+            ra[j] = load_raw_if<ONCE>(p + sh.e0);
+            if constexpr (HALF) rb[j] = load_raw_if<ONCE>(p + sh.e1);
         }
     };
     fetch(group.hb);
@@ -171,15 +181,15 @@ __global__ __launch_bounds__(256) void head_norm_kernel(Args a) {
     if constexpr (HALF) load_weight(w1, side.w, a.w_f32, sh.e1);
     angles<HALF, LP>(c, s, a, sh, token);
     const float of_d = 1.0f / static_cast<float>(a.d);
-    for (int h0 = group.hb; h0 < group.he; h0 += kAhead) {
+    for (int h0 = group.hb; h0 < group.he; h0 += AHEAD) {
         if (h0 > group.hb) fetch(h0);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
+        for (int j = 0; j < AHEAD; ++j) {
             if (h0 + j >= group.he) break;
             float u[8], v[8];
             get(u, widen(ra[j]), sh.some);
             if constexpr (HALF) get(v, widen(rb[j]), sh.two);
-            const float r = 1.0f / __builtin_sqrtf(group_sum<LP>(dot<HALF>(u, v, u, v)) * of_d + a.eps);
+            const float r = inverse_root(group_sum<LP>(dot<HALF>(u, v, u, v)) * of_d + a.eps);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 u[i] = u[i] * r * w0[i];
@@ -187,13 +197,13 @@ __global__ __launch_bounds__(256) void head_norm_kernel(Args a) {
             }
             if (sh.turns) turn<HALF, false>(u, v, c, s);
             T *p = y + (h0 + j) * side.heads.y_head;
-            if (sh.some) put(p + sh.e0, u);
-            if (sh.two) put(p + sh.e1, v);
+            if (sh.some) put<false>(p + sh.e0, u);
+            if (sh.two) put<false>(p + sh.e1, v);
         }
     }
 }
 
-template <typename T, bool HALF, int LP>
+template <typename T, bool HALF, int LP, bool ONCE>
 __global__ __launch_bounds__(256) void head_norm_backward_kernel(Args a, float *partial) {
     constexpr int PER = 256 / LP;
     __shared__ float lds[256 * 16];
@@ -214,13 +224,21 @@ __global__ __launch_bounds__(256) void head_norm_backward_kernel(Args a, float *
         const T *x = static_cast<const T *>(side.heads.x) + token * side.heads.x_token + group.hb * side.heads.x_head;
         const T *dy = static_cast<const T *>(side.dy) + token * side.dy_token + group.hb * side.dy_head;
         T *dx = static_cast<T *>(side.heads.y) + token * side.heads.y_token + group.hb * side.heads.y_head;
-        for (int h = group.hb; h < group.he; ++h, x += side.heads.x_head, dy += side.dy_head, dx += side.heads.y_head) {
-            const Raw x0 = load_raw(x + sh.e0), g0 = load_raw(dy + sh.e0);
-            Raw x1, g1;
+        // The next head's loads ahead of this one's sums, none behind a branch: the last head
+        // is read again.  (fp32 halves take two registers for each of bf16's.)
+        constexpr bool AHEAD = !HALF || sizeof(T) == 2;
+        Raw x0, x1, g0, g1;
+        const auto fetch = [&] {
+            x0 = load_raw_if<ONCE>(x + sh.e0);
+            g0 = load_raw_if<ONCE>(dy + sh.e0);
             if constexpr (HALF) {
-                x1 = load_raw(x + sh.e1);
-                g1 = load_raw(dy + sh.e1);
+                x1 = load_raw_if<ONCE>(x + sh.e1);
+                g1 = load_raw_if<ONCE>(dy + sh.e1);
             }
+        };
+        if (AHEAD) fetch();
+        for (int h = group.hb; h < group.he; ++h, dx += side.heads.y_head) {
+            if (!AHEAD) fetch();
             float u[8], v[8], du[8], dv[8];
             get(u, widen(x0), sh.some);
             get(du, widen(g0), sh.some);
@@ -228,8 +246,13 @@ __global__ __launch_bounds__(256) void head_norm_backward_kernel(Args a, float *
                 get(v, widen(x1), sh.two);
                 get(dv, widen(g1), sh.two);
             }
+            if (h + 1 < group.he) {
+                x += side.heads.x_head;
+                dy += side.dy_head;
+            }
+            if (AHEAD) fetch();
             if (sh.turns) turn<HALF, true>(du, dv, c, s);
-            const float r = 1.0f / __builtin_sqrtf(group_sum<LP>(dot<HALF>(u, v, u, v)) * of_d + a.eps);
+            const float r = inverse_root(group_sum<LP>(dot<HALF>(u, v, u, v)) * of_d + a.eps);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 u[i] *= r;
@@ -247,8 +270,8 @@ __global__ __launch_bounds__(256) void head_norm_backward_kernel(Args a, float *
                 du[i] = r * (du[i] - u[i] * m);
                 if constexpr (HALF) dv[i] = r * (dv[i] - v[i] * m);
             }
-            if (sh.some) put(dx + sh.e0, du);
-            if (sh.two) put(dx + sh.e1, dv);
+            if (sh.some) put<ONCE>(dx + sh.e0, du);
+            if (sh.two) put<ONCE>(dx + sh.e1, dv);
         }
     }
     // The workgroup's sums: a row of d.
@@ -312,7 +335,7 @@ __global__ __launch_bounds__(256) void head_norm_any_kernel(Args a, bool half, f
             if (BACKWARD) du[i] = at[i] < 0 ? 0.0f : static_cast<float>(dy[at[i]]);
             sum = __builtin_fmaf(u[i], u[i], sum);
         }
-        const float r = 1.0f / __builtin_sqrtf(wave_sum(sum) * of_d + a.eps);
+        const float r = inverse_root(wave_sum(sum) * of_d + a.eps);
 #pragma unroll
         for (int i = 0; i < N; ++i) u[i] *= BACKWARD ? r : r * w[i];
 #pragma unroll
@@ -406,20 +429,30 @@ dim3 backward_grid(Args &a, int64_t blocks) {
     return dim3(static_cast<unsigned>(x), groups_of(a, a.each));
 }
 
-template <typename T, bool HALF, int LP>
+template <typename T, bool HALF, int LP, bool ONCE>
 hipError_t run_wide(Args &a, float *partial, dim3 *grid, hipStream_t stream) {
     const int per = 256 / LP;
     const int64_t blocks = (a.S + static_cast<int64_t>(per) - 1) / per;
     if (partial) {
         *grid = backward_grid(a, blocks);
-        head_norm_backward_kernel<T, HALF, LP><<<*grid, 256, 0, stream>>>(a, partial);
+        head_norm_backward_kernel<T, HALF, LP, ONCE><<<*grid, 256, 0, stream>>>(a, partial);
     } else {
         a.each = heads_each(a, blocks);
         *grid = grid_of(blocks);
         grid->y = groups_of(a, a.each);
-        head_norm_kernel<T, HALF, LP><<<*grid, 256, 0, stream>>>(a);
+        // Four heads at a time or five, as leaves fewer of the last turn's loads for nothing.
+        const int n = std::min(a.each, std::max(a.q.heads.H, a.k.heads.H));
+        if ((n + 3) / 4 * 4 > (n + 4) / 5 * 5) head_norm_kernel<T, HALF, LP, ONCE, 5><<<*grid, 256, 0, stream>>>(a);
+        else head_norm_kernel<T, HALF, LP, ONCE, kAhead><<<*grid, 256, 0, stream>>>(a);
     }
     return hipGetLastError();
+}
+// Vectors that the 256 MiB of last-level cache do not hold are read past it.
+template <typename T, bool HALF, int LP>
+hipError_t run_lanes(Args &a, float *partial, dim3 *grid, hipStream_t stream) {
+    const int64_t bytes = static_cast<int64_t>(sizeof(T)) * a.S * (a.q.heads.H + a.k.heads.H) * a.d * (partial ? 3 : 2);
+    if (bytes > int64_t{256} << 20) return run_wide<T, HALF, LP, true>(a, partial, grid, stream);
+    return run_wide<T, HALF, LP, false>(a, partial, grid, stream);
 }
 
 // The forward, or the backward where `partial` is given, which writes a row for
@@ -428,7 +461,7 @@ template <typename T>
 hipError_t run(Args &a, bool half, float *partial, dim3 *grid, hipStream_t stream) {
     if (by_eight(a, half)) {
         const int lanes = lanes_of(a.d, a.R, half);
-#define HCMS_RUN(LP) half ? run_wide<T, true, LP>(a, partial, grid, stream) : run_wide<T, false, LP>(a, partial, grid, stream)
+#define HCMS_RUN(LP) half ? run_lanes<T, true, LP>(a, partial, grid, stream) : run_lanes<T, false, LP>(a, partial, grid, stream)
         return lanes == 8 ? HCMS_RUN(8) : lanes == 16 ? HCMS_RUN(16) : lanes == 32 ? HCMS_RUN(32) : HCMS_RUN(64);
 #undef HCMS_RUN
     }
