@@ -68,22 +68,22 @@ __device__ inline float inverse_root(float x) {
     return x < __builtin_inff() ? better : r;
 }
 
-// What a launch works on.  A workgroup takes up to `each` heads of one side: its
-// second index counts the queries' groups of heads, then the keys'.
+// What a launch works on.  A workgroup takes up to `each` heads of one side: the
+// queries' groups of heads are counted first, then the keys'.
 struct Args {
     Side q, k;
     const float *table;
     RopeAxes ax;
     const void *positions;
     bool pos64, w_f32;
-    int S, d, R, each;
+    int S, d, R, each, groups;
     float eps;
 };
 struct Group {
     bool key;
     int hb, he;   // its heads
-    __device__ explicit Group(const Args &a) {
-        const int of_q = (a.q.heads.H + a.each - 1) / a.each, y = blockIdx.y;
+    __device__ Group(const Args &a, int y) {
+        const int of_q = (a.q.heads.H + a.each - 1) / a.each;
         key = y >= of_q;
         hb = (key ? y - of_q : y) * a.each;
         he = min(hb + a.each, key ? a.k.heads.H : a.q.heads.H);
@@ -157,10 +157,12 @@ __device__ inline float dot(const float (&a)[8], const float (&b)[8], const floa
 template <typename T, bool HALF, int LP, bool ONCE, int AHEAD>
 __global__ __launch_bounds__(256) void head_norm_kernel(Args a) {
     const int lane = threadIdx.x % LP;
-    const int64_t token = block_index() * (256 / LP) + threadIdx.x / LP;
+    // The groups of a token side by side, as its heads often lie in memory.
+    const int64_t id = block_index();
+    const int64_t token = id / a.groups * (256 / LP) + threadIdx.x / LP;
     if (token >= a.S) return;
     const Share<HALF, LP> sh(lane, a.d, a.R);
-    const Group group(a);
+    const Group group(a, static_cast<int>(id % a.groups));
     const Side side = group.key ? a.k : a.q;
     const T *const x = static_cast<const T *>(side.heads.x) + token * side.heads.x_token;
     T *const y = static_cast<T *>(side.heads.y) + token * side.heads.y_token;
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(256) void head_norm_backward_kernel(Args a, float *
     __shared__ float lds[256 * 16];
     const int lane = threadIdx.x % LP, slot = threadIdx.x / LP;
     const Share<HALF, LP> sh(lane, a.d, a.R);
-    const Group group(a);
+    const Group group(a, blockIdx.y);
     const Side side = group.key ? a.k : a.q;
     const float of_d = 1.0f / static_cast<float>(a.d);
     float w0[8], w1[8], acc0[8] = {}, acc1[8] = {};
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(256) void head_norm_any_kernel(Args a, bool half, f
     __shared__ float lds[4 * 2 * kRopeMaxPairs];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int pairs = a.R / 2;
-    const Group group(a);
+    const Group group(a, blockIdx.y);
     const Side side = group.key ? a.k : a.q;
     const float of_d = 1.0f / static_cast<float>(a.d);
     constexpr int N = 2 * kPairs + kOthers;
@@ -438,8 +440,8 @@ hipError_t run_wide(Args &a, float *partial, dim3 *grid, hipStream_t stream) {
         head_norm_backward_kernel<T, HALF, LP, ONCE><<<*grid, 256, 0, stream>>>(a, partial);
     } else {
         a.each = heads_each(a, blocks);
-        *grid = grid_of(blocks);
-        grid->y = groups_of(a, a.each);
+        a.groups = groups_of(a, a.each);
+        *grid = grid_of(blocks * a.groups);
         // Four heads at a time or five, as leaves fewer of the last turn's loads for nothing.
         const int n = std::min(a.each, std::max(a.q.heads.H, a.k.heads.H));
         if ((n + 3) / 4 * 4 > (n + 4) / 5 * 5) head_norm_kernel<T, HALF, LP, ONCE, 5><<<*grid, 256, 0, stream>>>(a);
@@ -484,7 +486,7 @@ hipError_t launch_head_norm(const RopeSide &q, const RopeSide &k, const void *qw
                             const float *table, const RopeAxes &ax, const void *positions, bool pos64, int S, int d,
                             int R, bool half, float eps, int dtype, hipStream_t stream) {
     if (S == 0 || q.H + k.H == 0) return hipSuccess;
-    Args a{{q, nullptr, 0, 0, qw}, {k, nullptr, 0, 0, kw}, table, ax, positions, pos64, w_f32, S, d, R, 0, eps};
+    Args a{{q, nullptr, 0, 0, qw}, {k, nullptr, 0, 0, kw}, table, ax, positions, pos64, w_f32, S, d, R, 0, 0, eps};
     dim3 grid;
     return dtype == 0 ? run<__bf16>(a, half, nullptr, &grid, stream) : run<float>(a, half, nullptr, &grid, stream);
 }
@@ -498,7 +500,7 @@ hipError_t launch_head_norm_backward(const RopeSide &q, const RopeSide &k, const
         const auto side = [](const RopeSide &x, const RopeSide &g, const void *w) {
             return Side{{x.x, g.y, x.x_token, x.x_head, g.y_token, g.y_head, x.H}, g.x, g.x_token, g.x_head, w};
         };
-        Args a{side(q, dq, qw), side(k, dk, kw), table, ax, positions, pos64, w_f32, S, d, R, 0, eps};
+        Args a{side(q, dq, qw), side(k, dk, kw), table, ax, positions, pos64, w_f32, S, d, R, 0, 0, eps};
         dim3 grid;
         const hipError_t e = dtype == 0 ? run<__bf16>(a, half, partial, &grid, stream)
                                         : run<float>(a, half, partial, &grid, stream);
