@@ -7,7 +7,7 @@ holds it: D-wide tokens, H local heads of dimension d.
 
     h     = x + residual                     the residual stream's next value
     q,k,v = norm(h) w_qkv                    8-bit product
-    q, k  = rope(norm(q)), rope(norm(k))     norms of each head vector
+    q, k  = rope(norm(q)), rope(norm(k))     norms of each head vector, in the same pass
     y     = attention(q, k, v) w_o           chunk loop, 8-bit product
 
 ``serve`` quantises the weights once and each activation where it is made (the
@@ -63,9 +63,9 @@ class Block(torch.nn.Module):
         S, H, d = x.shape[0], self.H, self.d
         n, n_scale, h = hcms.rms_norm_fp8(x, self.norm, self.eps, residual=residual)
         q, k, v = hcms.linear_fp8(n, n_scale, *self.qkv8, parts=3)
-        q = hcms.rms_norm(q.view(S * H, d), self.q_norm, self.eps).view(S, H, d)
-        k = hcms.rms_norm(k.view(S * H, d), self.k_norm, self.eps).view(S, H, d)
-        hcms.rope(q, k, self.table, self.grid, self.axis_pairs, out=(q, k))
+        q, k = q.view(S, H, d), k.view(S, H, d)
+        hcms.qk_norm_rope(q, k, self.q_norm, self.k_norm, self.table, self.grid, self.axis_pairs, eps=self.eps,
+                          out=(q, k))
         o = self.ctx.forward(q, k, v.view(S, H, d), self.P, self.scale, self.chunk_sizes)
         return hcms.linear_fp8(*hcms.quantize_fp8(o.view(S, H * d)), *self.o8), h
 
@@ -74,9 +74,8 @@ class Block(torch.nn.Module):
         S, H, d = x.shape[0], self.H, self.d
         n, h = hcms.RmsNorm.apply(x, self.norm, self.eps, residual)
         q, k, v = hcms.Fp8Linear.apply(n, self.w_qkv).view(S, 3, H, d).unbind(1)
-        q = hcms.RmsNorm.apply(q.reshape(S * H, d), self.q_norm, self.eps).view(S, H, d)
-        k = hcms.RmsNorm.apply(k.reshape(S * H, d), self.k_norm, self.eps).view(S, H, d)
-        q, k = hcms.Rope.apply(q, k, self.table, self.grid, self.axis_pairs)
+        q, k = hcms.QkNormRope.apply(q, k, self.q_norm, self.k_norm, self.table, self.grid, self.axis_pairs, None,
+                                     "interleaved", self.eps)
         o = hcms.HcmsAttention.apply(q, k, v, self.ctx, self.P, self.scale, self.chunk_sizes)
         return hcms.Fp8Linear.apply(o.view(S, H * d), self.w_o), h
 
