@@ -872,7 +872,8 @@ HCMS_API int hcms_qk_norm_rope_backward(const hcms_rope_heads *dq, const hcms_ro
  * replayed.  Lengths include the call's own rows.  Rows from starts[B] on belong to
  * no sequence.  What breaks these rules never leads outside the buffers: a sequence
  * longer than W pages, or with a page outside the cache among those that it reads,
- * gives NaN rows, and tokens without a page are not appended.  T + 2 B <= 2^22, W >= 1.
+ * gives NaN rows, and tokens without a page are not appended.  T + 2 B <= 2^22, W >= 1,
+ * W page <= 2^31 - 1024.
  */
 typedef struct hcms_kv_cache {
     void *k, *v, *k_scale, *v_scale;
@@ -923,8 +924,8 @@ HCMS_API int hcms_append_kv(const hcms_kv_cache *cache, const hcms_kv_batch *bat
  *   workspace : device, hcms_cache_attention_workspace bytes for the same cache, B, W, T,
  *               H and window (none for 0), 16-byte aligned
  * Scores, maxima, sums and outputs are kept in fp32.  bf16: probabilities are rounded to
- * bf16 for their product; fp32: products are those of fp32.  Deterministic: work is split
- * along long sequences by sizes alone, and joined in a fixed order.
+ * bf16 for their product; fp32: products are those of fp32.  Deterministic: work is divided
+ * by the sizes and lengths alone, and joined in a fixed order.
  * T H <= 2^29, B heads <= 2^21, finite scale.  Errors: NULL, SHAPE, DTYPE, ALIGN, ALIAS, ARG (scale,
  * window < 0), HIP.  hcms_cache_attention_workspace is host only (errors: NULL, SHAPE,
  * DTYPE).

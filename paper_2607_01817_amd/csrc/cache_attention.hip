@@ -1090,6 +1090,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Args a) {
 // Sequences of more rows than this are taken by the kernel for many, where there are
 // both kinds.
 constexpr int kFewRows = 32;
+constexpr int kManyRows = 256;   // that make its launch worth while
 
 // A launch over the sequences of [from, to] rows.
 struct Launch {
@@ -1124,7 +1125,11 @@ Plan plan_of(const KvCache &cache, const KvBatch &batch, int T, int H, int windo
     Plan p;
     const int group = H / cache.heads, most = std::min(batch.B, T);
     const int64_t rows = static_cast<int64_t>(T) * group;
-    const bool pieces = rows > static_cast<int64_t>(kFewRows) * batch.B;
+    // Rows for the kernel for many: of sequences alike, or, as lengths are not known here,
+    // where one sequence may well have them beside others' next tokens.  Batches of up to
+    // four tokens a sequence are taken for next tokens: an empty launch costs 5 us.
+    const bool pieces = rows > static_cast<int64_t>(kFewRows) * batch.B ||
+                        (T > 4LL * batch.B && (static_cast<int64_t>(T) - batch.B) * group > kManyRows);
     const auto chunks = [&](int tile_rows) {   // that a tile sees, at most
         const int64_t cached = static_cast<int64_t>(batch.W) * (cache.page / kChunk);
         return window ? std::min<int64_t>(cached, (static_cast<int64_t>(window) + tile_rows / group) / kChunk + 3) : cached;

@@ -35,6 +35,9 @@ int check_sizes(const hcms_kv_cache *c, const hcms_kv_batch *b, int T) {
         return fail(HCMS_ERR_SHAPE, "need pages >= 1 and heads in [1, 2^15] (pages=%d heads=%d)", c->pages, c->heads);
     if (T < 0 || b->B < 0 || b->W < 1)
         return fail(HCMS_ERR_SHAPE, "need T >= 0, B >= 0 and W >= 1 (T=%d B=%d W=%d)", T, b->B, b->W);
+    // Tokens' places are counted in 32 bits, a chunk past the last one's too.
+    if (static_cast<int64_t>(b->W) * c->page > INT32_MAX - 1023)
+        return fail(HCMS_ERR_SHAPE, "W=%d pages of %d tokens: at most 2^31 - 1024 tokens", b->W, c->page);
     // The grids' first axis, in threads.
     if (static_cast<int64_t>(T) + 2LL * b->B > (1 << 22))
         return fail(HCMS_ERR_SHAPE, "T=%d rows and B=%d sequences: at most 2^22 rows and half as many sequences", T, b->B);

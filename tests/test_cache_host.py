@@ -165,6 +165,7 @@ def test_append_kv_refusals(lib):
         assert call(cache=c) == ESHAPE
     assert call(T=-1) == ESHAPE and call(batch=_batch(B=-1)) == ESHAPE and call(batch=_batch(W=0)) == ESHAPE
     assert call(T=(1 << 22) + 1) == ESHAPE and call(batch=_batch(B=1 << 21)) == ESHAPE
+    assert call(batch=_batch(W=1 << 25)) == ESHAPE and call(cache=_cache(page=1 << 20), batch=_batch(W=2048)) == ESHAPE
     assert call(pairs=(33,)) == ESHAPE and call(k=_rows(H, token=-1)) == ESHAPE and call(v=_rows(I, head=1 << 41)) == ESHAPE
     assert call(layout=3) == EARG and call(pos=E, pb=2) == EARG and call(pb=4) == EARG and call(dt=2) == EDTYPE
     assert call(cache=_cache(k=A + 8)) == EALIGN and call(cache=_cache(vs=D + 4)) == EALIGN

@@ -196,7 +196,8 @@ ATTENDS = [((1,), (1,), 1, 1, 64, 64), ((1,), (64,), 2, 5, 128, 64), ((1,), (100
            ((17,), (40,), 1, 1, 128, 64), ((40, 7), (300, 7), 2, 2, 64, 64), ((33,), (2100,), 1, 16, 128, 64),
            ((130,), (190,), 1, 3, 64, 64), ((1,) * 67, tuple(range(5, 72)), 1, 2, 64, 64), ((2,), (9000,), 1, 7, 64, 512),
            ((300, 1), (301, 700), 2, 1, 128, 64), ((90, 0, 1, 257, 31), (90, 5, 640, 1000, 700), 1, 2, 64, 128),
-           ((128,), (3000,), 1, 2, 128, 64)]
+           ((128,), (3000,), 1, 2, 128, 64), ((1, 300) + (1,) * 10, (70, 400) + tuple(range(100, 900, 80)), 1, 2, 128, 64),
+           ((3,) * 9, tuple(range(200, 1100, 100)), 2, 1, 64, 64)]
 
 
 @pytest.mark.parametrize("rows,lengths,heads,group,d,page", ATTENDS)
