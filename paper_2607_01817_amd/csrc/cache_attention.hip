@@ -43,7 +43,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kRows = 16;    // rows of a tile, and
 constexpr int kWaves = 4;    // waves of a workgroup, for few rows
 constexpr int kTeamWaves = 8;   // where they work at the same part
-constexpr int kTeamChunks = 2 * kTeamWaves;   // up to which a workgroup takes a whole tile
+constexpr int kTeamChunks = 4 * kTeamWaves;     // up to which they take a whole tile
 constexpr int kWaveRows = 32;                                    // rows of a wave, and
 // waves of a workgroup for many: two a SIMD, or one where its registers take the room
 // of two (fp32 rows of 128)
@@ -161,8 +161,14 @@ struct Work {
         }, &head, &tiles);
         all = head * a.cache.heads;
         tiles *= a.cache.heads;
-        const int64_t fit = static_cast<int64_t>(static_cast<double>(all) / a.least);
-        groups = static_cast<int>(min(max(tiles, fit), static_cast<int64_t>(a.groups)));
+        // Groups of at least so many units, or a whole number of groups to a tile, where a
+        // group then has at most as many units more as it has at least: parts of tiles alike
+        // begin and end with groups, and a group's second part costs about those units
+        // (12 sequences of 8 key heads of 128: 3840 tokens 25.7 us in equal pieces and 22.8 in
+        // two groups a tile, 32768 92 and 102).
+        const double room = a.groups, some = static_cast<double>(tiles), units = static_cast<double>(all);
+        const double fit = min(units / a.least, room), even = some * floor(fit / some);
+        groups = static_cast<int>(even > 0.0 && units / even - units / fit <= a.least ? even : min(max(some, fit), room));
         each = static_cast<double>(all) / max(groups, 1);
     }
     __device__ int64_t begin(int group) const { return group < groups ? static_cast<int64_t>(group * each) : all; }
@@ -1087,10 +1093,10 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Args a) {
 // ---------------------------------------------------------------------------
 // What is launched
 // ---------------------------------------------------------------------------
-// Sequences of more rows than this are taken by the kernel for many, where there are
-// both kinds.
-constexpr int kFewRows = 32;
-constexpr int kManyRows = 256;   // that make its launch worth while
+// Beside sequences of many rows, those of up to this many are next tokens: the kernel
+// for few takes them (16 sequences of 8192 tokens, 8 key heads of 128, in both kernels:
+// 64 rows 102 and 124 us, 96 rows 143 and 131).
+constexpr int kFewRows = 64;
 
 // A launch over the sequences of [from, to] rows.
 struct Launch {
@@ -1103,15 +1109,18 @@ struct Launch {
     int64_t words(int d, int rows) const {
         return some() && !whole ? partial(d, rows) + (groups * (sizeof(Begun) / 4) + 3) / 4 * 4 : 0;
     }
-    // `tiles` of up to n chunks: on `room` groups at once, each of at least `each` chunks
-    // but where there are more tiles; where n is at most `small`, or `most` and the tiles
-    // alone fill a quarter of the room, a group a tile.
-    void divide(int64_t tiles, int64_t n, int each, int small, int most, int room) {
+    // At most `tiles`, `alike` if the sequences are, of up to n chunks: on `room` groups
+    // at once, each of at least `each` chunks but where there are more tiles.  A group a
+    // tile, which joins nothing, where n is at most `small`, or `more` and the tiles fill
+    // a quarter of the room, or `most` and they fill it (teams, 64 tiles of 24 chunks: 13 us
+    // against 21, 256 of 64 29 against 33, but 64 of them 26 against 18; many rows of 64, 256
+    // tiles of 20 chunks 31 against 40, 128 of 32 50 against 39).
+    void divide(int64_t tiles, int64_t alike, int64_t n, int each, int small, int more, int most, int room) {
         least = each;
-        whole = n <= small || (n <= most && 4 * tiles >= room);
+        whole = n <= small || (n <= more && 4 * alike >= room) || (n <= most && alike >= room);
         const int64_t fit = std::max<int64_t>(tiles, tiles * n / each);
         groups = static_cast<int>(whole ? tiles : std::min<int64_t>(fit, room));
-        wide = groups > 8 * tiles;
+        wide = groups > 8 * alike;
     }
 };
 struct Plan {
@@ -1125,32 +1134,47 @@ Plan plan_of(const KvCache &cache, const KvBatch &batch, int T, int H, int windo
     Plan p;
     const int group = H / cache.heads, most = std::min(batch.B, T);
     const int64_t rows = static_cast<int64_t>(T) * group;
-    // Rows for the kernel for many: of sequences alike, or, as lengths are not known here,
-    // where one sequence may well have them beside others' next tokens.  Batches of up to
-    // four tokens a sequence are taken for next tokens: an empty launch costs 5 us.
-    const bool pieces = rows > static_cast<int64_t>(kFewRows) * batch.B ||
-                        (T > 4LL * batch.B && (static_cast<int64_t>(T) - batch.B) * group > kManyRows);
     const auto chunks = [&](int tile_rows) {   // that a tile sees, at most
         const int64_t cached = static_cast<int64_t>(batch.W) * (cache.page / kChunk);
         return window ? std::min<int64_t>(cached, (static_cast<int64_t>(window) + tile_rows / group) / kChunk + 3) : cached;
     };
+    // Tiles of a key head: at most, of rows in sequences of which each has a multiple of
+    // the group, and of sequences alike.
+    const auto tiles_of = [&](int64_t seqs, int each) {
+        int step = 1;
+        while (2 * step <= each && group % (2 * step) == 0) step *= 2;
+        return (rows + seqs * (each - step)) / each;
+    };
+    const auto alike_of = [&](int64_t seqs, int each) { return seqs * std::max<int64_t>((rows / seqs + each - 1) / each, 1); };
+    // Rows for the kernel for many: of sequences alike, or where one may well have them
+    // beside others' next tokens, and enough of them for its start and its tiles of 128
+    // or 256 rows, which the long sequences pay back first (8 key heads of 128, in both
+    // kernels: 8192 tokens of 512 rows 50 and 81 us, of 1024 99 and 85; 32768 tokens of 256
+    // 88 and 111, of 512 159 and 137; 1024 tokens of 1024 24 and 46, of 4096 84 and 48).
+    const int64_t n = chunks(kRows);
+    const double beyond = static_cast<double>((static_cast<int64_t>(T) - batch.B) * H / kRows);   // tiles
+    const bool pieces = (rows > static_cast<int64_t>(kFewRows) * batch.B || T > 8LL * batch.B) && T > batch.B &&
+                        beyond * beyond * static_cast<double>(n) >= 3 << 23;
     if (!pieces || batch.B > 1) {
         p.few.to = pieces ? kFewRows : INT32_MAX;
         const int64_t tiles = cache.heads * (pieces ? std::min<int64_t>(rows, most * static_cast<int64_t>(kFewRows / kRows))
-                                                    : (rows + static_cast<int64_t>(most) * (kRows - 1)) / kRows);
-        // Eight waves a CU, alone or together.  Alone they divide many tiles without
-        // waiting for each other; of few tiles they would leave too many parts.
-        const int64_t n = chunks(kRows);
-        p.team = n <= kTeamChunks || tiles * 8 <= 256;
-        if (p.team) p.few.divide(tiles, n, 2 * kTeamWaves, kTeamChunks, kTeamChunks, 256);
-        else p.few.divide(tiles, n, 4, 0, 0, 8 * 256);
+                                                    : tiles_of(most, kRows));
+        const int64_t alike = cache.heads * (pieces ? most : alike_of(most, kRows));
+        // Eight waves a CU, alone or together.  Together they share what starting and
+        // joining a part costs, up to a tile a CU, and of short tiles; of more tiles, waves
+        // alone have whole ones and wait for nothing (8192 tokens of 16 sequences, 8 key heads,
+        // 128: 128 tiles 35 us together and 45 alone, 256 55 and 70, 440 84 and 83, 1024 165
+        // both; 1000 tiles of 18 chunks, fp32, 64: 50 and 41).
+        p.team = n <= kTeamChunks / 2 || alike <= 256;
+        if (p.team) p.few.divide(tiles, alike, n, 2 * kTeamWaves, kTeamChunks, kTeamChunks, 2 * kTeamChunks, 256);
+        else p.few.divide(tiles, alike, n, 4, 0, 0, 0, 8 * 256);
     }
     if (pieces) {
         const int each = piece_rows(cache.d, dtype);
         p.many.from = batch.B > 1 ? kFewRows + 1 : 1;
         p.many.to = INT32_MAX;
-        const int64_t seqs = std::min<int64_t>(most, rows / p.many.from);
-        p.many.divide(cache.heads * ((rows + seqs * (each - 1)) / each), chunks(each), 8, 8, 32,
+        const int64_t seqs = std::min<int64_t>(most, std::max<int64_t>(rows / p.many.from, 1));
+        p.many.divide(cache.heads * tiles_of(seqs, each), cache.heads * alike_of(seqs, each), chunks(each), 8, 8, 24, 32,
                       cache.d == 128 ? 256 : 512);
     }
     return p;
