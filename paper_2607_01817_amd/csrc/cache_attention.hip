@@ -8,15 +8,20 @@
 // share it.  Scores are computed transposed, S^T = K Q^T, so each lane of the
 // accumulator holds one row and some tokens, which is what O^T += V^T P^T takes as its
 // operand: probabilities never leave the lane.  Two kernels:
-//   * few rows (the next tokens): tiles of 16 rows.  The cache's layout gives both
+//   * few rows (the next tokens; bounded by the cache's bytes): tiles of 16 rows.  The cache's layout gives both
 //     products' operands in 16-byte loads from global memory (the contraction of K Q^T
 //     runs through the elements in an order of its own), so each wave streams chunks of
 //     its own through registers, and the states of a workgroup's waves, and of workgroups
-//     that share a long sequence, are joined at the end;
-//   * many rows (a prompt's piece, a frame): tiles of 32 rows a wave.  A workgroup
-//     widens each chunk once into LDS, in the order of the operands, and all its waves
-//     read it there; a wave computes the next chunk's scores while it takes the
-//     exponentials of this one's.
+//     that share a long sequence, are joined at the end.  bf16, 8 key heads of 128 shared
+//     by five: 64 next tokens, sequences of up to 8192 tokens 64 us (286 MB, 4.5 TB/s), two
+//     of 131072 58 us (4.9 TB/s), one of 1001 11 us, a launch, the search for its place
+//     and loads that depend on each other;
+//   * many rows (a prompt's piece, a frame; bounded by the matrix units, whose LDS reads
+//     and exponentials take as long and overlap in part): tiles of 32 rows a wave.  A
+//     workgroup widens each chunk once into LDS, in the order of the operands, and all its
+//     waves read it there.  bf16, 128: 2 x 2048 rows of 40 heads over 16384 tokens 1215 us
+//     in all (1.06 PFLOP/s), 1560 of 5 heads over 56160 253 us (0.89: the last of 7 tiles
+//     has 24 of 256 rows).
 // Widening is one instruction for two elements, exact in bf16.
 //
 // fp32 rows: Q and P are taken apart into three bf16 each, whose sum is exact, and

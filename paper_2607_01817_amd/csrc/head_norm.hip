@@ -14,6 +14,9 @@
 // weights in registers.  dw is kept in registers over all the tokens of a lane,
 // then added over a workgroup's lanes through LDS and over the workgroups by a
 // second kernel, all in a fixed order.
+//
+// bf16, heads of 128: 56160 tokens of 10 heads 61 us, 4.7 TB/s of x and y; 7800 of 80
+// heads 55 us, its backward 97, 4.9 TB/s, and the sum of dw 5.
 #include <algorithm>
 
 #include "fp8.h"
@@ -417,7 +420,8 @@ int groups_of(const Args &a, int each) {
     return (a.q.heads.H + each - 1) / each + (a.k.heads.H + each - 1) / each;
 }
 // Heads of a workgroup: all of a side once the tokens alone make 1024 workgroups,
-// down to kAhead for a few tokens.
+// down to kAhead for a few tokens: a turn's loads are in flight together anyway, and
+// more heads reuse the table's entries and the weights.
 int heads_each(const Args &a, int64_t blocks) {
     int each = std::max(a.q.heads.H, a.k.heads.H);
     while (each > kAhead && groups_of(a, each) * blocks < 1024) each = (each + 1) / 2;
@@ -442,14 +446,17 @@ hipError_t run_wide(Args &a, float *partial, dim3 *grid, hipStream_t stream) {
         a.each = heads_each(a, blocks);
         a.groups = groups_of(a, a.each);
         *grid = grid_of(blocks * a.groups);
-        // Four heads at a time or five, as leaves fewer of the last turn's loads for nothing.
+        // Four heads at a time or five, as leaves fewer of the last turn's loads for nothing (five
+        // key and five query heads: 61 us for 64).
         const int n = std::min(a.each, std::max(a.q.heads.H, a.k.heads.H));
         if ((n + 3) / 4 * 4 > (n + 4) / 5 * 5) head_norm_kernel<T, HALF, LP, ONCE, 5><<<*grid, 256, 0, stream>>>(a);
         else head_norm_kernel<T, HALF, LP, ONCE, kAhead><<<*grid, 256, 0, stream>>>(a);
     }
     return hipGetLastError();
 }
-// Vectors that the 256 MiB of last-level cache do not hold are read past it.
+// Vectors that the 256 MiB of last-level cache do not hold are read past it, and what the
+// backward reads for the last time, x and dy, too (56160 tokens of 10 heads of 128 64 us
+// for 67; 7800 of 80, both directions, 164 for 172).
 template <typename T, bool HALF, int LP>
 hipError_t run_lanes(Args &a, float *partial, dim3 *grid, hipStream_t stream) {
     const int64_t bytes = static_cast<int64_t>(sizeof(T)) * a.S * (a.q.heads.H + a.k.heads.H) * a.d * (partial ? 3 : 2);

@@ -8,7 +8,11 @@
 // What bounds it: bytes, k and v once in, 17 / 32 of a byte for each element out,
 // and what the cache holds of them where it is asked for.  A workgroup takes the new
 // tokens of a sequence in one chunk of 64 of the cache, for one head: keys are
-// written as they come, values and scales are put in order in LDS.
+// written as they come, values and scales are put in order in LDS.  A row's loads are
+// ahead of the turn before, and of the page's place for the first.  1560 tokens of 40
+// heads of 128, bf16, with the held values: 21 us, 3.4 TB/s, the rotation
+// in fp64 and the rounding's comparisons beside them; one token of 8 heads 5 us, a
+// launch and the dependent loads to its place.
 #include <algorithm>
 
 #include "fp8.h"
