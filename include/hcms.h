@@ -922,7 +922,7 @@ HCMS_API int hcms_append_kv(const hcms_kv_cache *cache, const hcms_kv_batch *bat
  * NaN, and no others.
  *   out       : device, [T][H][d]
  *   workspace : device, hcms_cache_attention_workspace bytes for the same cache, B, W, T,
- *               H and window (none for 0), 16-byte aligned
+ *               H, window and dtype (none for 0), 16-byte aligned
  * Scores, maxima, sums and outputs are kept in fp32.  bf16: probabilities are rounded to
  * bf16 for their product; fp32: products are those of fp32.  Deterministic: work is divided
  * by the sizes and lengths alone, and joined in a fixed order.

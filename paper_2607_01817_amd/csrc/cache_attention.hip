@@ -176,7 +176,10 @@ struct Work {
         groups = static_cast<int>(even > 0.0 && units / even - units / fit <= a.least ? even : min(max(some, fit), room));
         each = static_cast<double>(all) / max(groups, 1);
     }
-    __device__ int64_t begin(int group) const { return group < groups ? static_cast<int64_t>(group * each) : all; }
+    // Rounded up a little, so that a whole number of groups to a tile ends with the tile.
+    __device__ int64_t begin(int group) const {
+        return group < groups ? static_cast<int64_t>(__builtin_fma(static_cast<double>(group), each, 0x1p-20)) : all;
+    }
     // The workgroup of a unit.
     __device__ int group_of(int64_t unit) const {
         int g = min(static_cast<int>(static_cast<double>(unit) / each), groups - 1);

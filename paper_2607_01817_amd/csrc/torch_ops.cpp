@@ -8,9 +8,13 @@
 // Every call runs through the C ABI (hcms.h), whose refusals become HcmsError.
 #include <ATen/hip/EmptyTensor.h>
 #include <torch/extension.h>
+#include <torch/csrc/autograd/function.h>
 
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <hip/hip_runtime.h>
+
+#include <unordered_set>
 
 #include "hcms.h"
 
@@ -233,6 +237,28 @@ std::pair<Tensor, Tensor> rms_norm_backward(const Tensor &dy, const Tensor &x, c
 // A gradient of a gradient would silently be wrong: the backwards here are not
 // differentiable.
 void once() { TORCH_CHECK(!at::GradMode::is_enabled(), "these operators are differentiable once (create_graph)"); }
+
+// A backward pass under capture hands a leaf's gradient to the stream on which the leaf was
+// first used by a graph that is still alive.  If that is a stream outside the capture, the
+// wait for it ends the process: refused here, ahead of it.
+void check_captured_leaves(void *stream) {
+    hipStreamCaptureStatus status;
+    if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &status) != hipSuccess) (void)hipGetLastError();
+    else if (status == hipStreamCaptureStatusNone) return;
+    std::vector<torch::autograd::Node *> todo{torch::autograd::get_current_node().get()};
+    std::unordered_set<torch::autograd::Node *> seen;
+    const auto current = c10::hip::getCurrentHIPStream(c10::hip::current_device()).id();
+    while (!todo.empty()) {
+        torch::autograd::Node *const node = todo.back();
+        todo.pop_back();
+        if (!node || !seen.insert(node).second) continue;
+        for (const auto &edge : node->next_edges()) todo.push_back(edge.function.get());
+        const auto at = node->stream();
+        TORCH_CHECK(!at || at->id() == current,
+                    "gradients under capture: a leaf belongs to a graph that was made on another stream and is still "
+                    "alive; drop that graph before the capture");
+    }
+}
 
 MaybeTensor maybe(const Tensor &t) { return t.defined() ? MaybeTensor(t) : std::nullopt; }
 
@@ -625,6 +651,7 @@ struct QkNormRope : torch::autograd::Function<QkNormRope> {
             const MaybeTensor positions = maybe(saved[5]);
             const auto p = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
             void *const stream = stream_of(q);
+            check_captured_leaves(stream);
             run([&] {
                 return hcms_qk_norm_rope_backward(
                     &grad[0], &grad[1], &in[0], &in[1], p(saved[2]), p(saved[3]), p(dw[0]), p(dw[1]),

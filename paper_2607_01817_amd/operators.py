@@ -244,7 +244,8 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight: torch.Tensor
 class QkNormRope:
     """Autograd over :func:`qk_norm_rope`: ``QkNormRope.apply(q, k, q_weight, k_weight,
     table, grid, axis_pairs, positions, layout, eps)`` returns (q, k), or q without
-    keys.  The inputs are kept for the backward."""
+    keys.  The inputs are kept for the backward, which may be captured into a graph where
+    no other autograd graph of the leaves, made on another stream, is alive."""
 
     @staticmethod
     def apply(q, k, q_weight, k_weight, table, grid, axis_pairs, positions=None, layout="interleaved", eps=1e-6):
@@ -293,7 +294,8 @@ def append_kv(k: torch.Tensor, v: torch.Tensor, cache: KvCache, page_table: torc
     tokens belong to one sequence each).  With ``table`` (:func:`rope_table` of ``grid``
     and ``axis_pairs``) the keys are turned as :func:`rope` turns them, for a token's
     place in its sequence, or at ``positions``.  ``held``: returns (k, v) [T][heads][d],
-    what the cache now holds of the rows, such as the chunk loop may attend to."""
+    what the cache now holds of the rows, such as the chunk loop may attend to (rows that
+    are not appended, from ``starts``[B] on or without a page, are not set)."""
     if stream is not None:
         return _under(stream, append_kv, k, v, cache, page_table, lengths, starts, table, grid, axis_pairs, positions,
                       layout, held)
@@ -311,8 +313,8 @@ def cache_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, l
     heads, which the query heads share in a row).  A row sees the tokens up to its own
     place (``causal``) or all of its sequence, of these the last ``window`` (0: all).
     ``scale`` defaults to 1 / sqrt(d).  Returns [T][H][d]; rows that see nothing are
-    zeros, rows from ``starts``[B] on are left as they are.  bfloat16 or float32; the
-    latter with products in full precision."""
+    zeros, rows from ``starts``[B] on are left as they are (of a new tensor: not set).
+    bfloat16 or float32; the latter with products in full precision."""
     if stream is not None:
         return _under(stream, cache_attention, q, cache, page_table, lengths, starts, scale, causal, window, out)
     return _ops().cache_attention(q, tuple(cache), page_table, lengths, starts, scale, bool(causal), window, out)

@@ -221,3 +221,49 @@ def test_extremes_and_a_gradient_of_a_gradient(hcms):
         q.add_(1)                      # what the backward needs
     with pytest.raises(RuntimeError, match="modified"):
         y.sum().backward()
+
+
+def _step(hcms, leaves, table, dq, dk):
+    q, k, qw, kw = leaves
+    y = hcms.QkNormRope.apply(q, k, qw, kw, table, [50], [32], None, "half", EPS)
+    return [*y, *torch.autograd.grad(y, leaves, (dq, dk))]
+
+
+def test_a_training_step_in_a_graph(hcms):
+    """Forward and backward captured and replayed, bit for bit the eager ones; while an
+    eager graph of the same leaves is alive the captured backward is refused, and the
+    process and the leaves go on."""
+    leaves = [_randn(1, 50, 4, 64, dtype=BF16).cuda(), _randn(2, 50, 2, 64, dtype=BF16).cuda(),
+              *(1 + 0.3 * _randn(3 + i, 64, dtype=BF16).cuda() for i in (0, 1))]
+    leaves = [t.requires_grad_() for t in leaves]
+    dq, dk = _randn(5, 50, 4, 64, dtype=BF16).cuda(), _randn(6, 50, 2, 64, dtype=BF16).cuda()
+    table = hcms.rope_table([50], [32])
+    _step(hcms, leaves, table, dq, dk)
+    torch.cuda.synchronize()
+    log("[graph] capture")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _step(hcms, leaves, table, dq, dk)
+    for i in range(4):
+        with torch.no_grad():
+            leaves[0].copy_(_randn(10 + i, 50, 4, 64, dtype=BF16))
+            dk.copy_(_randn(20 + i, 50, 2, 64, dtype=BF16))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        for a, b in zip(got, _step(hcms, leaves, table, dq, dk)):
+            assert torch.equal(bits(a.detach()), bits(b.detach()))
+    del out, got, graph, a, b
+    log("[graph] beside an eager graph of the leaves")
+    alive = hcms.QkNormRope.apply(*leaves, table, [50], [32], None, "half", EPS)
+    torch.cuda.synchronize()
+    other, flag = torch.cuda.CUDAGraph(), torch.zeros(1, device="cuda")
+    with torch.cuda.graph(other):
+        flag.add_(1.0)
+        with pytest.raises(RuntimeError, match="drop that graph"):
+            _step(hcms, leaves, table, dq, dk)
+    other.replay()
+    torch.cuda.synchronize()
+    assert flag.item() == 1.0
+    for t in torch.autograd.grad(alive, leaves, (dq, dk)):
+        assert torch.isfinite(t).all()
