@@ -167,13 +167,16 @@ struct Work {
         all = head * a.cache.heads;
         tiles *= a.cache.heads;
         // Groups of at least so many units, or a whole number of groups to a tile, where a
-        // group then has at most as many units more as it has at least: parts of tiles alike
-        // begin and end with groups, and a group's second part costs about those units
-        // (12 sequences of 8 key heads of 128: 3840 tokens 25.7 us in equal pieces and 22.8 in
-        // two groups a tile, 32768 92 and 102).
+        // group then has at most as many units more as it has at least, or, of many rows, not
+        // half as many: parts of tiles alike begin and end with groups, and a group's second
+        // part costs about those units (12 sequences of 8 key heads of 128: 3840 tokens 25.7 us
+        // in equal pieces and 22.8 in two groups a tile, 32768 92 and 102; of 5 heads 1560 rows
+        // over 32768 203 and 189, 1536 184 and 204).
+        constexpr double MORE = ROWS > kRows ? 0.45 : 1.0;
         const double room = a.groups, some = static_cast<double>(tiles), units = static_cast<double>(all);
         const double fit = min(units / a.least, room), even = some * floor(fit / some);
-        groups = static_cast<int>(even > 0.0 && units / even - units / fit <= a.least ? even : min(max(some, fit), room));
+        const bool whole_number = even > 0.0 && units / even - units / fit <= a.least * MORE;
+        groups = static_cast<int>(whole_number ? even : min(max(some, fit), room));
         each = static_cast<double>(all) / max(groups, 1);
     }
     // Rounded up a little, so that a whole number of groups to a tile ends with the tile.
