@@ -10,9 +10,9 @@
 // tokens of a sequence in one chunk of 64 of the cache, for one head: keys are
 // written as they come, values and scales are put in order in LDS.  A row's loads are
 // ahead of the turn before, and of the page's place for the first.  1560 tokens of 40
-// heads of 128, bf16, with the held values: 21 us, 3.4 TB/s, the rotation
-// in fp64 and the rounding's comparisons beside them; one token of 8 heads 5 us, a
-// launch and the dependent loads to its place.
+// heads of 128, bf16, with the held values: 21 us, 3.7 TB/s (as they come
+// 13.6: the rotation takes the rest); one token of 8 heads 5 us, a launch and the
+// dependent loads to its place.
 #include <algorithm>
 
 #include "fp8.h"
@@ -34,6 +34,23 @@ __device__ inline float to_odd(double x) {
     unsigned b = __builtin_bit_cast(unsigned, f);
     if (__builtin_fabs(static_cast<double>(f)) > __builtin_fabs(x)) --b;
     return __builtin_bit_cast(float, b | 1u);
+}
+
+// to_odd, where that matters: borders of codes and of scales have at most three bits of
+// mantissa, and x rounded to the nearest is on x's side of each but the one that it is.
+// The first n elements.
+__device__ inline void to_sides(const double (&w)[8], int n, float (&y)[8]) {
+    unsigned least = ~0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) {
+            y[i] = static_cast<float>(w[i]);
+            least = min(least, __builtin_bit_cast(unsigned, y[i]) << 12);
+        }
+    if (least) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) y[i] = to_odd(w[i]);
 }
 
 __device__ inline unsigned max4(unsigned v) {   // over four lanes that share a scale
@@ -92,6 +109,8 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
     constexpr int UNITS = D / 8, PER = 256 / UNITS;   // lanes of a token, tokens at once
     __shared__ unsigned char values[D / 2][kChunk];
     __shared__ unsigned char scales[2][D / kv::kBlock][kChunk];
+    __shared__ __attribute__((aligned(16))) int places[kChunk][4];
+    __shared__ bool inside[kChunk];
     __shared__ float turned[PAIRS == kAnyHalves ? 256 : 1][9];
     int b;
     int64_t before;
@@ -124,6 +143,20 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
         raw_v = load_raw(static_cast<const T *>(rows.v) + row_of(t) * rows.v_token + head * rows.v_head + e);
     };
     fetch(t);
+    // The places of the chunk's tokens on the grid, whose divisions each of a token's lanes
+    // would do again (1560 tokens of 40 heads 21.3 us so, 19.8 from LDS).
+    if (R > 0) {
+        const int i = threadIdx.x;
+        if (i >= t0 && i < t1) {
+            const RopePlace rp = rope_place(ax, positions, pos64, row_of(i), static_cast<int>(at + i));
+            places[i][0] = rp.r0;
+            places[i][1] = rp.r1;
+            places[i][2] = rp.r2;
+            places[i][3] = rp.r3;
+            inside[i] = rp.inside;
+        }
+        __syncthreads();
+    }
     if (page < 0 || page >= cache.pages) return;   // the whole workgroup
     const int64_t block = (static_cast<int64_t>(page) * cache.heads + head) * per_page + chunk % per_page;
     unsigned char *const ck = cache.k + block * kChunk * (D / 2);
@@ -132,7 +165,6 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
     unsigned char *const sv = cache.v_scale + block * kChunk * (D / kv::kBlock);
     // Every lane of a group of UNITS takes the same way, so those of a block stay together.
     for (; t < t1; t += PER) {
-        const int place = static_cast<int>(at + t);
         const int64_t row = row_of(t);
         const T *k = static_cast<const T *>(rows.k) + row * rows.k_token + head * rows.k_head;
         const f32x8 xk = widen(raw_k), xv = widen(raw_v);
@@ -147,7 +179,10 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
         int turning = R;
         asm volatile("" : "+s"(turning));
         if (e < turning) {
-            const RopePlace rp = rope_place(ax, positions, pos64, row, place);
+            RopePlace rp{places[t][0], places[t][1], places[t][2], places[t][3]};
+            rope_starts(ax, &rp);
+            rp.inside = inside[t];
+            double w[8];
             if constexpr (PAIRS == kHalves) {   // all eight are first elements of their pairs, or all second
                 const bool first = e < turning / 2;
                 const int p = first ? e : e - turning / 2;
@@ -156,8 +191,9 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
                 for (int i = 0; i < 8; ++i) {
                     const float2 cs = rope_entry(table, rp, p + i);
                     const double by = first ? -cs.y : cs.y;
-                    y[i] = to_odd(static_cast<double>(xk[i]) * cs.x + static_cast<double>(other[i]) * by);
+                    w[i] = static_cast<double>(xk[i]) * cs.x + static_cast<double>(other[i]) * by;
                 }
+                to_sides(w, 8, y);
             } else if constexpr (PAIRS == kAnyHalves) {
                 // One element behind the other, in LDS: unrolled, their comparisons take more
                 // scalar registers than there are.
@@ -179,9 +215,10 @@ __global__ __launch_bounds__(256) void append_kv_kernel(KvCache cache, KvBatch b
                     if (e + i >= turning) continue;
                     const float2 cs = rope_entry(table, rp, (e + i) / 2);
                     const double a = xk[i], o = xk[i + 1];
-                    y[i] = to_odd(a * cs.x - o * cs.y);
-                    y[i + 1] = to_odd(a * cs.y + o * cs.x);
+                    w[i] = a * cs.x - o * cs.y;
+                    w[i + 1] = a * cs.y + o * cs.x;
                 }
+                to_sides(w, turning - e, y);
             }
         }
         const Coded ek = encode(y), ev = encode(z);

@@ -20,21 +20,24 @@ struct RopePlace {
     int s1, s2, s3;
     bool inside = true;
 };
-
-// The place of the token whose coordinates are positions[index], or, without
-// positions, of place `place` of the row-major grid.
-__device__ inline RopePlace rope_place(const RopeAxes &ax, const void *positions, bool pos64, int64_t index, int place) {
-    RopePlace at;
-    // Read anew for each token: comparisons of pairs with them that a loop over
-    // tokens kept would take more scalar registers than there are.
+// Where the axes' pairs begin.  Read anew for each token: comparisons of pairs with them
+// that a loop over tokens kept would take more scalar registers than there are.
+__device__ inline void rope_starts(const RopeAxes &ax, RopePlace *at) {
     const auto start = [&](int a) {
         int s = a < ax.n_axes ? ax.pair_start[a] : kRopeMaxPairs;
         asm volatile("" : "+s"(s));
         return s;
     };
-    at.s1 = start(1);
-    at.s2 = start(2);
-    at.s3 = start(3);
+    at->s1 = start(1);
+    at->s2 = start(2);
+    at->s3 = start(3);
+}
+
+// The place of the token whose coordinates are positions[index], or, without
+// positions, of place `place` of the row-major grid.
+__device__ inline RopePlace rope_place(const RopeAxes &ax, const void *positions, bool pos64, int64_t index, int place) {
+    RopePlace at;
+    rope_starts(ax, &at);
     const auto row = [&](int a, int c) { return ax.tab_off[a] + c * ax.pairs[a] - ax.pair_start[a]; };
     if (positions) {
         const auto axis = [&](int a) {

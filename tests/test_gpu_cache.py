@@ -118,6 +118,41 @@ def test_every_code_and_tie(hcms):
         assert np.array_equal(h.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("layout,pairs", [("interleaved", 32), ("half", 32), ("interleaved", 27), ("half", 24), ("half", 12)])
+def test_turned_keys_next_to_borders(hcms, layout, pairs):
+    """Keys that the rotation moves off a border of two codes, or of two scales, by less
+    than fp32 can hold, to either side: cos 1 and sin +-2^-28 on edges of at least 0.25,
+    whose half steps are 2^-26 at least."""
+    edges = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0])
+    exps = [-126, -100, 0, 60, 123]
+    rows = []
+    for e in exps:
+        for top in (4.0, 6.0):                     # blocks whose largest value is a code, or the border itself
+            for sign in (1.0, -1.0):
+                first = np.where(edges[np.arange(pairs) % 8] > top, 3.5, edges[np.arange(pairs) % 8])
+                second = sign * np.where(np.arange(pairs) % 2, 1.0, -1.0)
+                x = np.zeros(64)
+                at = (slice(0, 2 * pairs, 2), slice(1, 2 * pairs, 2)) if layout == "interleaved" else (
+                    slice(0, pairs), slice(pairs, 2 * pairs))
+                x[at[0]], x[at[1]] = first, second
+                rows.append(np.ldexp(x, e))
+    x = np.stack(rows).astype(np.float32)
+    assert np.array_equal(x.astype(np.float64), np.stack(rows))
+    n = len(x)
+    table = torch.zeros(n * pairs, 2)
+    table[:, 0] = 1.0
+    table[:, 1] = 2.0 ** -28 * (1 - 2 * (torch.arange(n * pairs) // 3 % 2)).float()
+    b = Batch((n,), (n,), 1, 64)
+    cache, *batch = b.gpu(hcms)
+    t = torch.from_numpy(x)[:, None].cuda()
+    hcms.append_kv(t, t, cache, *batch, table=table.cuda(), grid=[n], axis_pairs=[pairs], layout=layout)
+    z = oc.factors(_f64(table), [n], [pairs], np.arange(n)[:, None])
+    b.store(oc.turn(_f64(t), z, layout), _f64(t))
+    got = numpy_of(cache)
+    assert np.array_equal(got[2], b.cache[2]) and np.array_equal(got[3], b.cache[3])
+    assert same_values(got[0], b.cache[0]) and same_values(got[1], b.cache[1])
+
+
 def test_appended_blocks_that_are_not_finite(hcms):
     b = Batch((3,), (3,), 1, 128)
     cache, *batch = b.gpu(hcms)
