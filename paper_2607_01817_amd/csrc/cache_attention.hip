@@ -26,7 +26,7 @@
 //
 // fp32 rows: Q and P are taken apart into three bf16 each, whose sum is exact, and
 // K and V are exact anyway, so the products are those of fp32.  bf16 rows: P is
-// rounded to bf16, 2^-9 relative at most, where its sum is not.
+// rounded to bf16, 2^-8 relative at most, where its sum is not.
 #include <algorithm>
 #include <cmath>
 

@@ -248,11 +248,58 @@ def test_attention(hcms, rows, lengths, heads, group, d, page, dtype, causal, wi
     assert torch.equal(bits(got), bits(again))
 
 
+# Pages that sequences may have, of which these have a few: enough for the kernel for many
+# rows from some hundred rows on, and for waves alone from some hundred sequences on.
+WIDE = 1 << 17
+
+
+@pytest.mark.parametrize("rows,lengths,heads,group,d,page", [
+    ((130,), (190,), 1, 3, 64, 64), ((300, 1), (301, 700), 2, 1, 128, 64), ((128,), (3000,), 1, 2, 128, 64),
+    ((90, 0, 1, 257, 31), (90, 5, 640, 1000, 700), 1, 2, 64, 128), ((520, 300), (900, 2500), 2, 4, 128, 192),
+    ((257, 70, 64, 65), (2000, 64, 500, 65), 3, 1, 64, 64), ((1, 300) + (1,) * 10, (70, 400) + tuple(range(100, 900, 80)), 1, 2, 128, 64)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_of_many_rows(hcms, rows, lengths, heads, group, d, page, dtype, causal):
+    log(f"[many rows] rows={rows} lengths={lengths} heads={heads}x{group} d={d} {dtype} causal={causal}")
+    b = Batch(rows, lengths, heads, d, page, seed=sum(lengths) + d, width=WIDE)
+    q = _randn(7, b.T, heads * group, d, dtype=dtype)
+    got = hcms.cache_attention(q.cuda(), *b.gpu(hcms), causal=causal)
+    _check(got, q, b, dtype, d ** -0.5, causal, 0, "out")
+    again = hcms.cache_attention(q.cuda(), *b.gpu(hcms), causal=causal)
+    assert torch.equal(bits(got), bits(again))
+
+
+@pytest.mark.parametrize("rows,lengths", [((660,), (700,)), ((403, 3, 0, 300), (600, 3, 70, 500))])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 100), (False, 65), (True, 1)])
+def test_many_rows_on_short_caches_and_in_windows(hcms, rows, lengths, d, dtype, causal, window):
+    """A workgroup takes whole tiles of many rows."""
+    log(f"[many rows, short] rows={rows} lengths={lengths} d={d} {dtype} causal={causal} {window}")
+    b = Batch(rows, lengths, 2, d, 64, seed=sum(lengths) + d)
+    q = _randn(7, b.T, 96, d, dtype=dtype)
+    got = hcms.cache_attention(q.cuda(), *b.gpu(hcms), causal=causal, window=window)
+    _check(got, q, b, dtype, d ** -0.5, causal, window, "out")
+
+
+@pytest.mark.parametrize("rows,lengths,heads,group,d", [
+    ((1,) * 300, tuple(range(300)), 1, 3, 128), ((1, 0, 3, 1) * 80, (40, 7, 1900, 1) * 80, 2, 8, 64)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 1500)])
+def test_attention_of_many_sequences(hcms, rows, lengths, heads, group, d, dtype, causal, window):
+    """More tiles than workgroups: waves with pieces of their own."""
+    log(f"[many sequences] {len(rows)} heads={heads}x{group} d={d} {dtype} causal={causal} {window}")
+    b = Batch(rows, lengths, heads, d, 64, seed=d, width=1000)
+    q = _randn(7, b.T, heads * group, d, dtype=dtype)
+    got = hcms.cache_attention(q.cuda(), *b.gpu(hcms), causal=causal, window=window)
+    _check(got, q, b, dtype, d ** -0.5, causal, window, "out")
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 3.0, 1e-3])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
-@pytest.mark.parametrize("rows", [5, 70])
-def test_scales_and_peaked_rows(hcms, scale, dtype, rows):
-    b = Batch((rows,), (700,), 2, 128, seed=9)
+@pytest.mark.parametrize("rows,width", [(5, 0), (70, 0), (70, WIDE)])
+def test_scales_and_peaked_rows(hcms, scale, dtype, rows, width):
+    b = Batch((rows,), (700,), 2, 128, seed=9, width=width)
     b.cache[2][:] = 127
     q = _randn(1, rows, 4, 128, dtype=dtype)
     got = hcms.cache_attention(q.cuda(), *b.gpu(hcms), scale=scale)
@@ -260,10 +307,10 @@ def test_scales_and_peaked_rows(hcms, scale, dtype, rows):
 
 
 @pytest.mark.parametrize("order", [1, -1])
-@pytest.mark.parametrize("rows", [1, 40])
-def test_scores_that_rise_and_fall_along_the_cache(hcms, order, rows):
+@pytest.mark.parametrize("rows,width", [(1, 0), (40, 0), (300, WIDE)])
+def test_scores_that_rise_and_fall_along_the_cache(hcms, order, rows, width):
     """The running maximum moves in every chunk, or never after the first."""
-    b = Batch((rows,), (3000,), 1, 64, seed=4)
+    b = Batch((rows,), (3000,), 1, 64, seed=4, width=width)
     q = torch.ones(rows, 1, 64)
     K = np.linspace(0, 1, 3000)[::order]
     for p in range(3000):
@@ -288,6 +335,17 @@ def test_strided_queries_out_and_rows_of_no_sequence(hcms):
     assert torch.equal(bits(hcms.cache_attention(by_head, *b.gpu(hcms), causal=True)[:b.T]), bits(want))
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_rows_that_see_nothing(hcms, dtype, d):
+    b = Batch((70, 130, 100), (0, 2, 40), 1, d, seed=8, width=WIDE)
+    q = _randn(1, b.T, 2, d, dtype=dtype)
+    for causal in (True, False):
+        got = hcms.cache_attention(q.cuda(), *b.gpu(hcms), causal=causal)
+        assert (got[:70] == 0).all() and (not causal or ((got[70:198] == 0).all() and (got[200:260] == 0).all()))
+        _check(got, q, b, dtype, d ** -0.5, causal, 0, f"causal={causal}")
+
+
 def test_rows_that_see_nothing_and_lengths_of_zero(hcms):
     b = Batch((2, 4, 1), (0, 2, 40), 1, 64, seed=8)      # more rows than tokens: the first rows see nothing if causal
     q = _randn(1, b.T, 2, 64, dtype=FP32)
@@ -304,7 +362,7 @@ def test_rows_that_see_nothing_and_lengths_of_zero(hcms):
     assert (left == 5).all()
 
 
-@pytest.mark.parametrize("group", [2, 20])          # few rows and many
+@pytest.mark.parametrize("group", [2, 20, 12000])   # few rows and many
 @pytest.mark.parametrize("d", [64, 128])
 def test_values_that_are_not_finite_reach_the_rows_that_see_them_only(hcms, group, d):
     """NaN in keys and values of tokens before a window, after a causal row's place, and
@@ -332,9 +390,9 @@ def test_values_that_are_not_finite_reach_the_rows_that_see_them_only(hcms, grou
                         assert np.isnan(got[i]).all()
 
 
-@pytest.mark.parametrize("rows", [1, 90])
-def test_nan_in_the_middle_of_a_sequence(hcms, rows):
-    b = Batch((rows, rows), (300, 300), 1, 128, seed=2)
+@pytest.mark.parametrize("rows,width", [(1, 0), (90, 0), (90, 2 * WIDE)])
+def test_nan_in_the_middle_of_a_sequence(hcms, rows, width):
+    b = Batch((rows, rows), (300, 300), 1, 128, seed=2, width=width)
     b.cache[3][b.page_table[0, 1], 0, 0, 2, oc.value_place(7)] = 255
     b.cache[2][b.page_table[1, 1], 0, 0, 2, oc.key_scale_place(7)] = 255
     got = _f64(hcms.cache_attention(_randn(1, 2 * rows, 1, 128).cuda(), *b.gpu(hcms)))
@@ -343,12 +401,12 @@ def test_nan_in_the_middle_of_a_sequence(hcms, rows):
     assert np.isnan(got[rows:]).all()
 
 
-@pytest.mark.parametrize("rows", [1, 90])
+@pytest.mark.parametrize("rows,width", [(1, 0), (90, 0), (90, WIDE)])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
-def test_appended_nan_comes_out(hcms, rows, dtype):
+def test_appended_nan_comes_out(hcms, rows, dtype, width):
     """A block that was not finite when it was appended (whose codes are zeros) is NaN to
     the rows that see it."""
-    b = Batch((rows, rows), (200, 200), 1, 64, seed=2)
+    b = Batch((rows, rows), (200, 200), 1, 64, seed=2, width=width)
     k, v = _randn(1, 2 * rows, 1, 64, dtype=dtype), _randn(2, 2 * rows, 1, 64, dtype=dtype)
     k[0, 0, 3], v[rows, 0, 40] = float("inf"), float("nan")
     cache, *batch = b.gpu(hcms)
@@ -357,7 +415,7 @@ def test_appended_nan_comes_out(hcms, rows, dtype):
     assert np.isnan(got[:rows]).all() and np.isnan(got[rows:, :, 32:]).all() and np.isfinite(got[rows:, :, :32]).all()
 
 
-@pytest.mark.parametrize("group", [3, 40])          # few rows and many
+@pytest.mark.parametrize("group", [3, 40, 16000])   # few rows and many
 def test_pages_that_there_are_not_and_sequences_past_them(hcms, group):
     b = Batch((2, 2, 2), (150, 150, 150), 1, 64, seed=3)
     b.page_table[0, 1], b.page_table[1, 0] = b.pages, -5
@@ -370,9 +428,9 @@ def test_pages_that_there_are_not_and_sequences_past_them(hcms, group):
     assert np.isfinite(got[:4]).all() and np.isnan(got[4:]).all()      # the lost pages are out of the window
 
 
-@pytest.mark.parametrize("group", [4, 40])
-def test_queries_that_are_not_finite_stay_in_their_rows(hcms, group):
-    b = Batch((3,), (200,), 1, 64, seed=3)
+@pytest.mark.parametrize("group,width", [(4, 0), (40, 0), (64, 8 * WIDE)])
+def test_queries_that_are_not_finite_stay_in_their_rows(hcms, group, width):
+    b = Batch((3,), (200,), 1, 64, seed=3, width=width)
     q = _randn(1, 3, group, 64, dtype=BF16)
     clean = _f64(hcms.cache_attention(q.cuda(), *b.gpu(hcms)))
     q[1, 2, 5] = float("nan")

@@ -223,6 +223,29 @@ def test_extremes_and_a_gradient_of_a_gradient(hcms):
         y.sum().backward()
 
 
+@pytest.mark.parametrize("pairs,layout", [(64, "interleaved"), (27, "half")])
+def test_past_32_bits(hcms, pairs, layout):
+    """More than 2^31 elements: the last tokens bit for bit as alone, both directions."""
+    S, H, d, n = 66000, 256, 128, 700
+    q = torch.randn(S, H, d, generator=torch.Generator("cuda").manual_seed(1), dtype=BF16, device="cuda")
+    assert q.numel() > 1 << 31
+    w, table = torch.full((d,), 1.5, dtype=BF16, device="cuda"), hcms.rope_table([50], [pairs])
+    at = torch.arange(S, device="cuda") % 50
+    log(f"[2^31] {pairs} pairs {layout}")
+    with torch.no_grad():
+        y = hcms.qk_norm_rope(q, None, w, None, table, [50], [pairs], at, layout)
+        alone = hcms.qk_norm_rope(q[-n:], None, w, None, table, [50], [pairs], at[-n:], layout)
+    assert torch.equal(bits(y[-n:]), bits(alone))
+    log("[2^31] backward")
+
+    def dx(x, dy, places):
+        x = x.detach().requires_grad_()
+        out = hcms.QkNormRope.apply(x, None, w, None, table, [50], [pairs], places, layout)
+        return torch.autograd.grad(out, x, dy)[0]
+
+    assert torch.equal(bits(dx(q, y, at)[-n:]), bits(dx(q[-n:], y[-n:], at[-n:])))
+
+
 def _step(hcms, leaves, table, dq, dk):
     q, k, qw, kw = leaves
     y = hcms.QkNormRope.apply(q, k, qw, kw, table, [50], [32], None, "half", EPS)
