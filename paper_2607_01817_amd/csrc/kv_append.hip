@@ -10,7 +10,7 @@
 // tokens of a sequence in one chunk of 64 of the cache, for one head: keys are
 // written as they come, values and scales are put in order in LDS.  A row's loads are
 // ahead of the turn before, and of the page's place for the first.  1560 tokens of 40
-// heads of 128, bf16, with the held values: 21 us, 3.7 TB/s (as they come
+// heads of 128, bf16, with the held values: 19.7 us, 3.7 TB/s (as they come
 // 13.6: the rotation takes the rest); one token of 8 heads 5 us, a launch and the
 // dependent loads to its place.
 #include <algorithm>
