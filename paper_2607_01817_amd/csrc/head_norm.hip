@@ -63,12 +63,15 @@ struct Side {
     int64_t dy_token, dy_head;
     const void *w;
 };
-// 1 / sqrt(x) to an ulp: the hardware's with one step of Newton's, a fifth of the
-// instructions of an exact root and division.  Infinity gives 0.
+// 1 / sqrt(x) to an ulp: the hardware's with one step of Newton's, a quarter of the
+// instructions of an exact root and division.  The hardware's takes what is below 2^-126
+// as 0, so that goes in as 2^24 x.  0 gives infinity, and infinity 0.
 __device__ inline float inverse_root(float x) {
-    const float r = __builtin_amdgcn_rsqf(x);
-    const float better = __builtin_fmaf(0.5f * r, __builtin_fmaf(-x * r, r, 1.0f), r);
-    return x < __builtin_inff() ? better : r;
+    const bool small = x < 0x1p-126f;
+    const float y = small ? x * 0x1p24f : x;
+    const float r = __builtin_amdgcn_rsqf(y);
+    const float better = __builtin_fmaf(0.5f * r, __builtin_fmaf(-y * r, r, 1.0f), r);
+    return (r > 0.0f && r < __builtin_inff() ? better : r) * (small ? 0x1p12f : 1.0f);
 }
 
 // What a launch works on.  A workgroup takes up to `each` heads of one side: the

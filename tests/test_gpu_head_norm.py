@@ -223,6 +223,43 @@ def test_extremes_and_a_gradient_of_a_gradient(hcms):
         y.sum().backward()
 
 
+@pytest.mark.parametrize("S,H,Hk,d,pairs,grid,layout", [SHAPES[i] for i in (0, 1, 2, 5, 7, 8, 9, 11, 12, 15)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("eps", [0.0, float(np.float32(1e-40))])
+def test_mean_squares_below_2_to_the_minus_126(hcms, S, H, Hk, d, pairs, grid, layout, dtype, eps):
+    """Head vectors so small that mean(x^2) + eps is subnormal, and with an eps of its own
+    zeros among them, whose outputs are zeros and whose gradients are finite.  Of the mean,
+    each square and the product with 1 / d are off by 2^-150 at most, half a step, so it is
+    within 2^-149; of r, n and dx that takes at most a half, a half and three halves of the
+    relative error, all counted as two."""
+    log(f"[head norm, small] S={S} H={H},{Hk} d={d} pairs={pairs} {layout} {dtype} eps={eps}")
+    _, q, k, qw, kw, table, z = _case(S, H, Hk, d, pairs, grid, layout, dtype, S + d, hcms)
+    q, k = (t * 2.0 ** -66 for t in (q, k))
+    assert ((q.double() ** 2).mean(-1) + eps < 2.0 ** -126).all() and ((q.double() ** 2).mean(-1) > 2.0 ** -142).all()
+    zero = eps > 0 and S > 1
+    if zero:
+        q[1], k[1, 0] = 0, 0
+    leaves = [t.cuda().requires_grad_(True) for t in (q, k, qw, kw)]
+    y = hcms.QkNormRope.apply(*leaves, table, grid, pairs, None, layout, eps)
+    dys = _randn(5, S, H, d, dtype=dtype), _randn(6, S, Hk, d, dtype=dtype)
+    grads = torch.autograd.grad(y, leaves, [t.cuda() for t in dys])
+    if zero:
+        assert (y[0][1] == 0).all() and (y[1][1, 0] == 0).all()
+    for i, (x, w, dy) in enumerate(((q, qw, dys[0]), (k, kw, dys[1]))):
+        X, W, DY, side = _f64(x), _f64(w), _f64(dy), "qk"[i]
+        mean = (X * X).mean(-1, keepdims=True) + eps
+        n, r = np.abs(X) / np.sqrt(mean), 1 / np.sqrt(mean)
+        rel = 2.0 ** -17 + 2 * 2.0 ** -149 / mean
+        _within(y[i], oc.head_norm(X, W, eps, z, layout), ROUND[dtype] * np.abs(oc.head_norm(X, W, eps, z, layout)) +
+                rel * _spread(n * W, z, layout) + 1e-30, side)
+        dx, dw = oc.head_norm_backward(DY, X, W, eps, z, layout)
+        g = _spread(DY, z, layout)
+        gw = g * np.abs(W)
+        _within(grads[i], dx, ROUND[dtype] * np.abs(dx) + rel * r * (gw + n * (gw * n).mean(-1, keepdims=True)), "d" + side)
+        _within(grads[2 + i], dw, ROUND[w.dtype] * np.abs(dw) +
+                ((rel + (S * X.shape[1] / 512 + 100) * 2.0 ** -24) * g * n).sum((0, 1)), "dw" + side)
+
+
 @pytest.mark.parametrize("pairs,layout", [(64, "interleaved"), (27, "half")])
 def test_past_32_bits(hcms, pairs, layout):
     """More than 2^31 elements: the last tokens bit for bit as alone, both directions."""
