@@ -853,7 +853,8 @@ HCMS_API int hcms_qk_norm_rope_backward(const hcms_rope_heads *dq, const hcms_ro
  * head vector, held as its exponent byte b = e + 127 (e8m0): the smallest one from
  * 2^-126 on that brings the block's largest magnitude to at most 6.  They are rounded
  * to the nearest, ties to the even code; a block that holds an infinity or a NaN gets
- * the scale NaN (byte 255), and so do all its values.  With t the token's place in
+ * the scale NaN (byte 255), and so do all its values.  (Magnitudes past 6 2^125 take
+ * the scale 2^126, which the attention takes as NaN.)  With t the token's place in
  * its chunk of 64 tokens:
  *   k       : [pages][heads][page][d / 2]            elements 2 c and 2 c + 1 in byte c,
  *                                                    the first in its low half
@@ -917,9 +918,11 @@ HCMS_API int hcms_append_kv(const hcms_kv_cache *cache, const hcms_kv_batch *bat
  * sequence with n rows and length L sees the tokens [begin, end) of it:
  *   end = L - n + i + 1 (causal) or L,  begin = max(0, end - window) (window 0: 0)
  *   out[t][h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale <q[t][h], k_j>)
- * A row that sees nothing gives zeros; rows of no sequence stay as they were.  A value
- * that is not finite (or a block's scale of 2^126 or more) makes the rows that see it
- * NaN, and no others.
+ * A row that sees nothing gives zeros; rows of no sequence stay as they were.  A block
+ * whose scale is NaN, or 2^126 or more, is NaN to the rows that see it, wherever its
+ * chunk lies and whatever its codes: all of a row for a key, the block's elements for a
+ * value; it changes nothing in other rows.  Values past 2^120 / L may leave fp32's range
+ * in the sums.
  *   out       : device, [T][H][d]
  *   workspace : device, hcms_cache_attention_workspace bytes for the same cache, B, W, T,
  *               H, window and dtype (none for 0), 16-byte aligned

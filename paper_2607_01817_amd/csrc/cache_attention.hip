@@ -333,6 +333,7 @@ struct Raw {
     Key k[4];
     unsigned k_scale;   // byte i: tile i
     u32x4 v[D / 32], v_scale[D / 32];
+    unsigned some;      // four bytes of v_scale: all lanes' together are all that the wave has
     bool bad;           // a page that there is not
 
     __device__ void load(const Args &a, int head, int page, int chunk, int lane) {
@@ -346,6 +347,7 @@ struct Raw {
 #pragma unroll
         for (int i = 0; i < 4; ++i) k[i] = *reinterpret_cast<const Key *>(kp + i * 16 * (D / 2));
         k_scale = *reinterpret_cast<const unsigned *>(sk);
+        some = *reinterpret_cast<const unsigned *>(sv + r / 4 % (D / 32) * kChunk + r % 4 * 4);
 #pragma unroll
         for (int b = 0; b < D / 32; ++b) {
             v[b] = *reinterpret_cast<const u32x4 *>(vp + b * 16 * kChunk);
@@ -410,6 +412,11 @@ __device__ inline float larger(float a, float b) { return __builtin_amdgcn_fmed3
 
 // Bytes of x that are 253 or more: scales whose values bf16 does not hold.
 __device__ inline unsigned not_finite(unsigned x) { return ((x & 0x7F7F7F7Fu) + 0x03030303u) & x & 0x80808080u; }
+// All ones in these bytes.
+__device__ inline unsigned not_finite_bytes(unsigned x) {
+    const unsigned y = not_finite(x);
+    return (y << 1) - (y >> 7);
+}
 
 // What a wave knows of its rows: lane l holds row l % 16, of the accumulators the
 // elements 32 b + 8 (l / 16) + 2 e + p in o[b][p][e].
@@ -426,7 +433,7 @@ __device__ inline void attend(const Args &a, const Raw<D> &raw, const bf16x8 (&q
     f32x4 s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float by = scale_of(raw.k_scale, i);
+        const float by = scale_of(raw.k_scale | not_finite_bytes(raw.k_scale), i);
         s[i] = f32x4{};
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) {
@@ -475,17 +482,9 @@ __device__ inline void attend(const Args &a, const Raw<D> &raw, const bf16x8 (&q
         }
         take_apart<NP>(x, pr[h]);
     }
-    // Where rows see different tokens of the chunk, a value that is not finite must not
-    // reach those that do not see it (0 times NaN): it counts as 0 in the product and
-    // makes those NaN that do.
-    unsigned wrong = 0;
-    if (masked) {
-#pragma unroll
-        for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) wrong |= not_finite(raw.v_scale[b][i]);
-    }
-    const bool repair = masked && __ballot(wrong != 0) != 0;
+    // A value that is not finite must not reach rows that do not see it (0 times NaN): it
+    // counts as 0 in the product and makes those NaN that see it.
+    const bool repair = __ballot(not_finite(raw.some) != 0) != 0;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) {
         u32x4 scale = raw.v_scale[b];
@@ -507,7 +506,7 @@ __device__ inline void attend(const Args &a, const Raw<D> &raw, const bf16x8 (&q
             st.o[b][0] += add;
             st.o[b][1] += add;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) scale[i] &= ~((not_finite(scale[i]) >> 7) * 0xFFu);
+            for (int i = 0; i < 4; ++i) scale[i] &= ~not_finite_bytes(scale[i]);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -730,19 +729,22 @@ struct Share {
     }
     __device__ void store_keys(Widened<D> &lds, int t) const {
         __bf16 *p = lds.k + t / (D / 32) * Widened<D>::KS + t % (D / 32) * 32;
-        const float by = scale_of(scale[0], 0);
+        const float by = scale_of(scale[0] < 253u ? scale[0] : 255u, 0);   // not finite: NaN
 #pragma unroll
         for (int j = 0; j < 4; ++j) *reinterpret_cast<bf16x8 *>(p + 8 * j) = widen8(x[j], by);
     }
     __device__ void store_values(Widened<D> &lds, int t, bool is_masked) const {
         const int c = t / 4, h = t & 1, i0 = 2 * (t >> 1 & 1);
         u32x4 s = scale;
-        if (is_masked) {
+        if (!is_masked) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] |= not_finite_bytes(s[i]);
+        } else {
             u32x4 wrong;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 wrong[i] = not_finite(s[i]) >> 7;
-                s[i] &= ~(wrong[i] * 0xFFu);
+                s[i] &= ~not_finite_bytes(s[i]);
             }
             if (c % 16 == 0)
 #pragma unroll

@@ -401,6 +401,58 @@ def test_nan_in_the_middle_of_a_sequence(hcms, rows, width):
     assert np.isnan(got[rows:]).all()
 
 
+@pytest.mark.parametrize("rows,group,width", [(1, 1, 0), (1, 8, 600), (90, 2, 0), (90, 2, 2 * WIDE)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("byte", [252, 253, 254, 255])
+def test_scales_from_2_to_the_126_on_are_nan_wherever_their_chunk_lies(hcms, rows, group, width, d, dtype, byte):
+    """In chunks that every row sees whole, that a window cuts and that the sequence's end
+    cuts; of any codes, zeros and the smallest among them.  Zeros of scale 2^125 are numbers."""
+    log(f"[large scales] rows={rows}x{group} width={width} d={d} {dtype} byte={byte}")
+    q = _randn(1, 4 * rows, group, d, dtype=dtype).cuda()
+    for code in (0x00, 0x11, 0x77):
+        for part in (2, 3):
+            if byte == 252 and (part == 2 or code):      # sums past fp32's range
+                continue
+            b = Batch((rows,) * 4, (300,) * 4, 1, d, seed=2, width=width)
+            clean = _f64(hcms.cache_attention(q, *b.gpu(hcms), window=250))
+            for s, p in enumerate((100, 60, 299)):              # the fourth sequence has none; rows see [50, 300)
+                page, t = b.page_table[s, p // 64], p % 64
+                if part == 2:
+                    b.cache[0][page, 0, t, 16:32] = code
+                    b.cache[2][page, 0, 0, 1, oc.key_scale_place(t)] = byte
+                else:
+                    b.cache[1][page, 0, 0, 16:32, oc.value_place(t)] = code
+                    b.cache[3][page, 0, 0, 1, oc.value_place(t)] = byte
+            got = _f64(hcms.cache_attention(q, *b.gpu(hcms), window=250))
+            bad = np.zeros(got.shape, bool)
+            if byte > 252:
+                bad[:3 * rows, :, slice(32, 64) if part == 3 else slice(None)] = True
+            assert np.array_equal(np.isnan(got), bad) and np.isfinite(got[~bad]).all(), (code, part)
+            same = np.ones(got.shape, bool)
+            same[:3 * rows, :, slice(32, 64) if part == 3 else slice(None)] = False
+            assert np.array_equal(got[same], clean[same]), (code, part)
+
+
+@pytest.mark.parametrize("rows,width", [(1, 0), (90, 0), (90, 2 * WIDE)])
+@pytest.mark.parametrize("x", [1e36, 2.6e38, 3.4e38])
+def test_appended_values_next_to_the_largest(hcms, rows, width, x):
+    """Past 6 2^125 = 2.55e38 a block's values are NaN to the rows that see them, in a whole
+    chunk and in one that the sequence's end cuts; 1e36, 2^-8 of the largest number, is one."""
+    b = Batch((rows, rows), (130, 200), 1, 64, seed=2, width=width)
+    k, v = _randn(1, 2 * rows, 1, 64), _randn(2, 2 * rows, 1, 64)
+    v[0, 0, 3], k[rows, 0, 40] = x, x
+    cache, *batch = b.gpu(hcms)
+    hcms.append_kv(k.cuda(), v.cuda(), cache, *batch)
+    q = _randn(3, 2 * rows, 2, 64)
+    q[..., 32:] *= 2.0 ** -20
+    got = _f64(hcms.cache_attention(q.cuda(), cache, *batch))
+    if x < 2.55e38:
+        assert np.isfinite(got[:rows]).all()
+    else:
+        assert np.isnan(got[:rows, :, :32]).all() and np.isfinite(got[:rows, :, 32:]).all() and np.isnan(got[rows:]).all()
+
+
 @pytest.mark.parametrize("rows,width", [(1, 0), (90, 0), (90, WIDE)])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_appended_nan_comes_out(hcms, rows, dtype, width):
