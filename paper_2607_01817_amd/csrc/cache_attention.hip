@@ -629,7 +629,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(64 * kTeamWaves, 2) void cache_attention_team_kernel(Args) {
     __shared__ float o_lds[kTeamWaves][kRows][D + 4], m_lds[kTeamWaves][kRows], l_lds[kTeamWaves][kRows];
     __shared__ Piece<kRows> piece;
-    for_parts<kRows, true>(blockIdx.x, piece, [&](const Args &a, const Part<kRows> &part) {
+    for_parts<kRows, true>(static_cast<int>(block_index()), piece, [&](const Args &a, const Part<kRows> &part) {
         const Tile t = tile_of<kRows>(a, part.seq, part.k);
         const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
         State<D> st;
@@ -1215,7 +1215,9 @@ template <typename T, int D>
 hipError_t run(const Args &args, const Plan &p, float *workspace, hipStream_t stream) {
     if (p.few.some()) {
         const Args a = with(args, p.few, workspace, kRows);
-        if (p.team) cache_attention_team_kernel<T, D><<<a.groups, 64 * kTeamWaves, 0, stream>>>(a);
+        // Whole tiles of 16 rows are up to 2^25 + 2^21, whose threads pass 32 bits; those of many
+        // rows, at most 2^22 of 512 threads or 2^23 of 256, do not.
+        if (p.team) cache_attention_team_kernel<T, D><<<grid_of(a.groups), 64 * kTeamWaves, 0, stream>>>(a);
         else cache_attention_kernel<T, D><<<(a.groups + kWaves - 1) / kWaves, 64 * kWaves, 0, stream>>>(a);
         join<T, D, kRows>(a, p.few, stream);
     }

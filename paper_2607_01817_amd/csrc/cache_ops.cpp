@@ -90,7 +90,7 @@ int check_queries(const hcms_kv_cache *c, int B, int T, int H, int window, int d
     int st;
     if ((st = check_dtype(dtype)) != HCMS_OK) return st;
     if (H < 0 || H % c->heads != 0) return fail(HCMS_ERR_SHAPE, "H=%d must be a multiple of the cache's %d heads", H, c->heads);
-    // Tiles of them and of the sequences' ends: a grid's threads along one axis.
+    // Rows of all heads, their tiles and those that sequences' ends cut are counted in 32 bits.
     if (static_cast<int64_t>(H) * T > (1 << 29) || static_cast<int64_t>(c->heads) * B > (1 << 21))
         return fail(HCMS_ERR_SHAPE, "T=%d rows of H=%d heads: at most 2^29 together; B=%d sequences of %d key heads: 2^21", T,
                     H, B, c->heads);

@@ -621,3 +621,16 @@ def test_past_32_bits(hcms):
     want, A, _ = oc.attention(_f64(q), _f64(hk), _f64(hv), d ** -0.5, True)
     assert (np.abs(got - want) <= (2.0 ** -8 + 2.0 ** -14) * (np.abs(want) + A) * (1 + 2.0 ** -7)).all()
     assert int(cache.k[:pages - 1].max()) == 0
+
+
+def test_more_tiles_than_a_grid_s_axis_has_threads_for(hcms):
+    """2^27 query heads on one key head: 2^23 tiles of a workgroup each, all alike."""
+    b = Batch((1,), (40,), 1, 64, seed=3)
+    args = b.gpu(hcms)
+    q, n = _randn(1, 1, 1, 64, dtype=BF16).cuda(), 1 << 27
+    one = bits(hcms.cache_attention(q, *args))
+    log(f"[grid] {n} heads")
+    out = torch.zeros(1, n, 64, dtype=BF16, device="cuda")
+    hcms.cache_attention(q.expand(1, n, 64), *args, out=out)
+    for part in out.view(torch.int16).split(n // 16, 1):
+        assert bool((part == one).all())
