@@ -874,7 +874,7 @@ HCMS_API int hcms_qk_norm_rope_backward(const hcms_rope_heads *dq, const hcms_ro
  * no sequence.  What breaks these rules never leads outside the buffers: a sequence
  * longer than W pages, or with a page outside the cache among those that it reads,
  * gives NaN rows, and tokens without a page are not appended.  T + 2 B <= 2^22, W >= 1,
- * W page <= 2^31 - 1024.
+ * W page <= 2^31 - 1024, pages heads page <= 2^48.
  */
 typedef struct hcms_kv_cache {
     void *k, *v, *k_scale, *v_scale;

@@ -24,6 +24,7 @@ using hcms::hip_fail;
 using hcms::ok;
 
 constexpr int kMostHeads = 1 << 15;   // the second axis of a grid
+constexpr int64_t kMostCache = 1LL << 48;   // tokens of all heads: their bytes fit 63 bits
 
 // Sizes of a cache and a batch over it.
 int check_sizes(const hcms_kv_cache *c, const hcms_kv_batch *b, int T) {
@@ -38,6 +39,8 @@ int check_sizes(const hcms_kv_cache *c, const hcms_kv_batch *b, int T) {
     // Tokens' places are counted in 32 bits, a chunk past the last one's too.
     if (static_cast<int64_t>(b->W) * c->page > INT32_MAX - 1023)
         return fail(HCMS_ERR_SHAPE, "W=%d pages of %d tokens: at most 2^31 - 1024 tokens", b->W, c->page);
+    if (static_cast<int64_t>(c->pages) * c->heads > kMostCache / c->page)
+        return fail(HCMS_ERR_SHAPE, "%d pages of %d heads and %d tokens: at most 2^48 together", c->pages, c->heads, c->page);
     // The grids' first axis, in threads.
     if (static_cast<int64_t>(T) + 2LL * b->B > (1 << 22))
         return fail(HCMS_ERR_SHAPE, "T=%d rows and B=%d sequences: at most 2^22 rows and half as many sequences", T, b->B);
@@ -74,6 +77,10 @@ int check_rows(const hcms_kv_rows *r, const char *name, int T, int heads, int d,
     if (T > 1 && r->token > hcms::kMostSpan / (T - 1))
         return fail(HCMS_ERR_SHAPE, "%d rows %lld elements apart span more than 2^60 elements", T,
                     static_cast<long long>(r->token));
+    const int64_t rest = hcms::kMostSpan - (T - 1) * r->token;
+    if (heads > 1 && r->head > rest / (heads - 1))
+        return fail(HCMS_ERR_SHAPE, "%d heads %lld elements apart in %d rows %lld apart span more than 2^60 elements",
+                    heads, static_cast<long long>(r->head), T, static_cast<long long>(r->token));
     if (!aligned(r->x, es)) return fail(HCMS_ERR_ALIGN, "%s must be aligned to its elements", name);
     *out = {name, r->x, ((T - 1) * r->token + (heads - 1) * r->head + d) * es};
     return HCMS_OK;

@@ -203,6 +203,27 @@ def test_rows_that_span_more_than_63_bits_are_refused(lib):
     assert b"span" in lib.hcms_last_error()
 
 
+def test_heads_that_span_more_than_63_bits_are_refused(lib):
+    def call(T, heads, token, head, n):
+        return lib.hcms_cache_attention(_cache(heads=n), _batch(), _rows(H, token=token, head=head), I, J, T, heads, 0.1, 0, 0,
+                                        0, None)
+
+    for args in ((1, 1 << 28, 64, 1 << 40, 2), (1, 1 << 29, 0, 1 << 33, 1), (1 << 20, 4, 1 << 40, 1 << 40, 2),
+                 (2, (1 << 20) + 2, 1 << 40, 1 << 40, 2)):
+        assert call(*args) == ESHAPE and b"span" in lib.hcms_last_error(), args
+    assert call(1, (1 << 20) + 1, 64, 1 << 40, 1) == EALIAS      # 2^60 to the last head: over the cache
+
+
+def test_caches_whose_bytes_pass_63_bits_are_refused(lib):
+    n = ctypes.c_int64()
+    for c in (_cache(pages=(1 << 31) - 1, heads=1 << 15, page=1 << 20), _cache(pages=1 << 30, heads=1 << 13, page=64)):
+        assert lib.hcms_cache_attention(c, _batch(), _rows(H), I, J, 5, 1 << 15, 0.1, 0, 0, 0, None) == ESHAPE
+        assert b"together" in lib.hcms_last_error()
+        assert lib.hcms_cache_attention_workspace(c, _batch(), 5, 1 << 15, 0, 0, ctypes.byref(n)) == ESHAPE
+        assert lib.hcms_append_kv(c, _batch(), _rows(H), _rows(I), None, None, 5, None, None, None, 0, None, 0, 0, 0,
+                                  None) == ESHAPE
+
+
 # ---------------------------------------------------------------------------
 # Refusals of the binding
 # ---------------------------------------------------------------------------
