@@ -238,25 +238,38 @@ std::pair<Tensor, Tensor> rms_norm_backward(const Tensor &dy, const Tensor &x, c
 // differentiable.
 void once() { TORCH_CHECK(!at::GradMode::is_enabled(), "these operators are differentiable once (create_graph)"); }
 
-// A backward pass under capture hands a leaf's gradient to the stream on which the leaf was
-// first used by a graph that is still alive.  If that is a stream outside the capture, the
-// wait for it ends the process: refused here, ahead of it.
-void check_captured_leaves(void *stream) {
+// The capture that a stream's work goes into, or 0.
+unsigned long long capture_of(hipStream_t stream) {
     hipStreamCaptureStatus status;
-    if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &status) != hipSuccess) (void)hipGetLastError();
-    else if (status == hipStreamCaptureStatusNone) return;
+    unsigned long long id = 0;
+    if (hipStreamGetCaptureInfo(stream, &status, &id) != hipSuccess) {   // the default stream, which is never captured
+        (void)hipGetLastError();
+        return 0;
+    }
+    return status == hipStreamCaptureStatusNone ? 0 : id;
+}
+
+// A backward pass under capture hands a gradient on to the stream of the node that takes it:
+// for a leaf, the one on which it was first used by a graph that is still alive.  If that is
+// a stream outside the capture, the wait for it ends the process: refused here, ahead of it.
+void check_captured_nodes(void *stream) {
+    const auto capture = capture_of(static_cast<hipStream_t>(stream));
+    if (!capture) return;
     std::vector<torch::autograd::Node *> todo{torch::autograd::get_current_node().get()};
     std::unordered_set<torch::autograd::Node *> seen;
-    const auto current = c10::hip::getCurrentHIPStream(c10::hip::current_device()).id();
+    const c10::Stream current = c10::hip::getCurrentHIPStream(c10::hip::current_device()).unwrap();
     while (!todo.empty()) {
         torch::autograd::Node *const node = todo.back();
         todo.pop_back();
         if (!node || !seen.insert(node).second) continue;
         for (const auto &edge : node->next_edges()) todo.push_back(edge.function.get());
-        const auto at = node->stream();
-        TORCH_CHECK(!at || at->id() == current,
-                    "gradients under capture: a leaf belongs to a graph that was made on another stream and is still "
-                    "alive; drop that graph before the capture");
+        const auto at = node->stream();   // autograd calls its devices CUDA ones
+        const auto own = [&] {
+            return c10::Stream(c10::Stream::UNSAFE, c10::Device(current.device_type(), at->device_index()), at->id());
+        };
+        TORCH_CHECK(!at || own() == current || capture_of(c10::hip::HIPStream(own()).stream()) == capture,
+                    "gradients under capture: a leaf or a step before belongs to a graph that was made on a stream outside "
+                    "the capture and is still alive; drop that graph before the capture");
     }
 }
 
@@ -651,7 +664,7 @@ struct QkNormRope : torch::autograd::Function<QkNormRope> {
             const MaybeTensor positions = maybe(saved[5]);
             const auto p = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
             void *const stream = stream_of(q);
-            check_captured_leaves(stream);
+            check_captured_nodes(stream);
             run([&] {
                 return hcms_qk_norm_rope_backward(
                     &grad[0], &grad[1], &in[0], &in[1], p(saved[2]), p(saved[3]), p(dw[0]), p(dw[1]),

@@ -244,8 +244,9 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, q_weight: torch.Tensor
 class QkNormRope:
     """Autograd over :func:`qk_norm_rope`: ``QkNormRope.apply(q, k, q_weight, k_weight,
     table, grid, axis_pairs, positions, layout, eps)`` returns (q, k), or q without
-    keys.  The inputs are kept for the backward, which may be captured into a graph where
-    no other autograd graph of the leaves, made on another stream, is alive."""
+    keys.  The inputs are kept for the backward, which may be captured into a graph, with
+    all of its streams, where no autograd graph of the leaves that was made on a stream
+    outside the capture is alive."""
 
     @staticmethod
     def apply(q, k, q_weight, k_weight, table, grid, axis_pairs, positions=None, layout="interleaved", eps=1e-6):

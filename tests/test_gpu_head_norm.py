@@ -327,3 +327,44 @@ def test_a_training_step_in_a_graph(hcms):
     assert flag.item() == 1.0
     for t in torch.autograd.grad(alive, leaves, (dq, dk)):
         assert torch.isfinite(t).all()
+
+
+def test_a_captured_training_step_on_two_streams(hcms):
+    """Queries and keys made on two streams of one capture, both directions, bit for bit the
+    eager step."""
+    S, H, Hk, d = 50, 4, 2, 64
+    xq, xk = _randn(1, S, H, d).cuda(), _randn(2, S, Hk, d).cuda()
+    leaves = [(1 + 0.3 * _randn(3 + i, *shape)).cuda().requires_grad_()
+              for i, shape in enumerate(((S, H, d), (S, Hk, d), (d,), (d,)))]
+    dq, dk, table = _randn(7, S, H, d).cuda(), _randn(8, S, Hk, d).cuda(), hcms.rope_table([S], [32])
+    side = torch.cuda.Stream()
+
+    def step():
+        a, b, qw, kw = leaves
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        with torch.cuda.stream(side):
+            k = xk * b
+        q = xq * a
+        here.wait_stream(side)
+        y = hcms.QkNormRope.apply(q, k, qw, kw, table, [S], [32], None, "half", EPS)
+        out = [q, k, *y, *torch.autograd.grad(y, leaves, (dq, dk))]
+        here.wait_stream(side)
+        return [t.detach() for t in out]
+
+    want = step()
+    torch.cuda.synchronize()
+    log("[graph] capture of two streams")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    log("[graph] replays")
+    for i in range(4):
+        xk.copy_(_randn(20 + i, S, Hk, d))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(bits(a), bits(b))
