@@ -64,6 +64,11 @@ constexpr float kNone = -__builtin_inff();
 // rescaled: probabilities stay below 2^8.
 constexpr float kHeadroom = 8.0f;
 constexpr float kMostSum = 256.0f;   // 2^kHeadroom, of a chunk's probabilities together
+// A probability's power of two is one multiply-add of its score, c score - c maximum, where
+// the maximum's product, rounded first, is up to this: off by 2^-13 at most.  Rows whose
+// maximum lies farther out take c (score - maximum), as that rounding would soon be all
+// there is.
+constexpr float kFar = 4096.0f;
 
 struct Args {
     KvCache cache;
@@ -422,7 +427,7 @@ __device__ inline unsigned not_finite_bytes(unsigned x) {
 // elements 32 b + 8 (l / 16) + 2 e + p in o[b][p][e].
 template <int D>
 struct State {
-    float m = kNone, limit = kNone, sum = 0.0f;   // sum: of the lane's own tokens
+    float m = kNone, limit = kNone, mc = 0.0f, sum = 0.0f;   // sum: of the lane's own tokens
     f32x4 o[D / 32][2] = {};
 };
 
@@ -460,17 +465,23 @@ __device__ inline void attend(const Args &a, const Raw<D> &raw, const bf16x8 (&q
     for (int i = 0; i < 4; ++i) tops[i] = larger(larger(s[i][0], s[i][1]), larger(s[i][2], s[i][3]));
     const float top = larger(larger(tops[0], tops[1]), larger(tops[2], tops[3]));
     if (__ballot(top > st.limit)) {
-        const float m = over_groups(fmaxf(top, st.m), true);
+        // Far rows' limit is none: they come here with each chunk of which they see something.
+        const float all = over_groups(fmaxf(top, st.m), true), m = all > st.limit ? all : st.m;
         const float by = st.m == kNone ? 0.0f : __builtin_amdgcn_exp2f((st.m - m) * c);
         st.sum *= by;
 #pragma unroll
         for (int b = 0; b < D / 32; ++b)
 #pragma unroll
             for (int p = 0; p < 2; ++p) st.o[b][p] *= by;
+        const bool near = __builtin_fabsf(m * c) <= kFar;
         st.m = m;
-        st.limit = m == kNone ? kNone : m + kHeadroom / c;
+        st.limit = near ? m + kHeadroom / c : kNone;
+        st.mc = near ? m * c : 0.0f;
+        const float from = near || m == kNone ? 0.0f : m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] -= from;
     }
-    const float mc = st.m == kNone ? 0.0f : st.m * c;
+    const float mc = st.mc;
     bf16x8 pr[2][NP];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -849,7 +860,8 @@ __device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &pa
     };
 
     const float c = a.c;
-    float m = kNone, mc = 0.0f, sum = 0.0f;
+    float m = kNone, sum = 0.0f;
+    float mc = __builtin_nanf("");   // m times c; NaN where there is none, or it is far
     f32x16 o[DT] = {};
     // Scores of chunk j.
     const auto scores = [&](int j, f32x16 (&s)[2]) {
@@ -877,15 +889,15 @@ __device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &pa
                 if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // else all comparisons' masks at once
             }
     };
-    // Probabilities against the running maximum, and the lane's sum of them.
-    const auto weights = [&](const f32x16 (&s)[2], bf16x8 (&pr)[4][NP]) {
+    // Probabilities of powers c (s - from) - off, and the lane's sum of them.
+    const auto weights = [&](const f32x16 (&s)[2], float from, float off, bf16x8 (&pr)[4][NP]) {
         float all = 0.0f;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ks / 2][8 * (ks % 2) + e], c, -mc));
+                x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ks / 2][8 * (ks % 2) + e] - from, c, -off));
                 all += x[e];
             }
             take_apart<NP>(x, pr[ks]);
@@ -917,8 +929,9 @@ __device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &pa
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] *= by;
         m = to;
-        mc = m == kNone ? 0.0f : m * c;
+        mc = __builtin_fabsf(m * c) <= kFar ? m * c : __builtin_nanf("");
     };
+    const auto far = [&] { return mc != mc; };
     // As in attend: values that are not finite make the rows NaN that see them, at the end
     // (bit dt: the elements of o[dt]).
     unsigned lost = 0;
@@ -952,23 +965,28 @@ __device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &pa
             if (mask) hide(j, s);
             if constexpr (NP == 1) {
                 // The maximum is raised, and the chunk's probabilities taken again, where their
-                // sum passes kMostSum, so that none is needed otherwise, and set by the first
-                // chunk of which a row sees something.
+                // sum passes kMostSum, so that none is needed otherwise, and where it is NaN:
+                // until a chunk of which the row sees something, and of far rows always.
                 bf16x8 pr[4][NP];
-                float all = weights(s, pr);
-                const bool high = of_halves(all, false) > kMostSum;
-                if (__ballot(high || m == kNone)) {
+                float all = weights(s, 0.0f, mc, pr);
+                const bool high = !(of_halves(all, false) <= kMostSum);
+                if (__ballot(high)) {
                     const float top = maximum(s);
-                    raise(high || m == kNone ? fmaxf(m, top) : m);
-                    all = weights(s, pr);
+                    raise(high ? fmaxf(m, top) : m);
+                    all = weights(s, far() && m != kNone ? m : 0.0f, far() ? 0.0f : mc, pr);
                 }
                 sum += all;
                 product(j, pr);
             } else {
                 const float top = maximum(s);
-                if (__ballot(m == kNone ? top > kNone : (top - m) * c > kHeadroom)) raise(fmaxf(m, top));
+                if (__ballot(m == kNone ? top > kNone : far() || (top - m) * c > kHeadroom)) {
+                    raise(fmaxf(m, top));
+                    const float from = far() && m != kNone ? m : 0.0f;
+#pragma unroll
+                    for (int mt = 0; mt < 2; ++mt) s[mt] -= from;
+                }
                 bf16x8 pr[4][NP];
-                sum += weights(s, pr);
+                sum += weights(s, 0.0f, far() ? 0.0f : mc, pr);
                 product(j, pr);
             }
             in_order<4 * DT, NP, 6>();
@@ -1241,9 +1259,10 @@ int64_t cache_attention_workspace(const KvCache &cache, const KvBatch &batch, in
 hipError_t launch_cache_attention(const KvCache &cache, const KvBatch &batch, const KvQueries &rows, void *workspace,
                                   int dtype, hipStream_t stream) {
     if (rows.T == 0 || batch.B == 0 || rows.H == 0) return hipSuccess;
-    // At least 2^-126, which makes exp2 of any finite score 1 as a scale of 0 does, and
-    // leaves masked scores at minus infinity.
-    const float c = std::max(std::fabs(rows.scale) * 1.44269504088896340736f, 1.17549435e-38f);
+    // At least 2^-149, which makes exp2 of any finite score 1 as a scale of 0 does, and
+    // leaves masked scores at minus infinity; at most the largest number, so that scores of
+    // 0 stay 0.
+    const float c = std::min(std::max(std::fabs(rows.scale) * 1.44269504088896340736f, 0x1p-149f), 0x1.fffffep127f);
     const Args a{cache, batch, rows, c, rows.H / cache.heads, 0, 0, 0, 0, false, nullptr, nullptr};
     const Plan p = plan_of(cache, batch, rows.T, rows.H, rows.window, dtype);
     float *w = static_cast<float *>(workspace);

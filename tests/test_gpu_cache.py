@@ -321,6 +321,52 @@ def test_scores_that_rise_and_fall_along_the_cache(hcms, order, rows, width):
         _check(got, q.to(dtype), b, dtype, 2.0, False, 0, f"order {order}")
 
 
+@pytest.mark.parametrize("rows,width", [(1, 0), (5, 8 * 64), (40, 0), (300, WIDE)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("power", [5, 12, 25, 40, 90, 118])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_of_any_size(hcms, rows, width, dtype, power, sign):
+    """Scores of halves up to 6, times 2^power and more, exact in fp32: a row's output is the
+    mean of the values of the 12 tokens with the largest one, as the next is 128 and more
+    below and its probability 0.  Theirs are equal, at most 2^-13 from 1 (in bf16: rounded to
+    1 in the sum over values), so sums and quotient are off by 32 roundings.  With a scale of
+    0 it is the mean of all, the powers of two off by 2^-21 and the sums as elsewhere."""
+    rng = np.random.default_rng(power + rows)
+    b = Batch((rows,), (700,), 1, 64, seed=rows, width=width)
+    size = rng.choice([0.5, 1.0, 2.0, 3.0], 700) if sign > 0 else rng.choice([1.5, 2.0, 3.0], 700)
+    top = rng.permutation(700)[:12]
+    size[top] = 6.0 if sign > 0 else 0.5
+    for p in range(700):
+        k = np.zeros(64)
+        k[0] = sign * size[p]
+        oc.store(b.cache, b.page_table[0, p // 64], p % 64, 0, k, rng.standard_normal(64))
+    q = torch.zeros(rows, 2, 64)
+    q[:, 0, 0], q[:, 1, 0] = 2.0 ** (power + 3), 2.0 ** (power + 2)
+    q = q.to(dtype)
+    V = b.read(0)[1][:, 0]
+    for scale in (1.0, 0.0):
+        got = _f64(hcms.cache_attention(q.cuda(), *b.gpu(hcms), scale=scale))
+        seen = V[top] if scale else V
+        want, mass = seen.mean(0), np.abs(seen).mean(0)
+        off = (32 * 2.0 ** -24 + (2.0 ** -13 if dtype == BF16 else 0) if scale else
+               2.0 ** -20 + (700 / 16 + 64) * 2.0 ** -24 + (2.0 ** -8 if dtype == BF16 else 0))
+        bound = ROUND[dtype] * np.abs(want) + mass * off * (1 + 2.0 ** -7)
+        worst = float((np.abs(got - want) / bound).max())
+        log(f"    rows={rows} {dtype} 2^{power} {sign} scale {scale}: worst error {worst:.3f} of its bound")
+        assert worst <= 1.0, (scale, worst)
+
+
+@pytest.mark.parametrize("rows,width", [(1, 0), (300, WIDE)])
+@pytest.mark.parametrize("scale", [3.4e38, -3.4e38, 1e-44])
+def test_the_largest_and_smallest_scales(hcms, rows, width, scale):
+    """Scores of zero, and others times the smallest scales, give the mean of the values."""
+    b = Batch((rows,), (700,), 2, 128, seed=9, width=width)
+    q = torch.zeros(rows, 4, 128) if abs(scale) > 1 else _randn(1, rows, 4, 128)
+    for dtype in (BF16, FP32):
+        got = hcms.cache_attention(q.to(dtype).cuda(), *b.gpu(hcms), scale=scale)
+        _check(got, q.to(dtype), b, dtype, float(np.float32(scale)), False, 0, f"scale {scale}")
+
+
 def test_strided_queries_out_and_rows_of_no_sequence(hcms):
     b = Batch((3, 5), (100, 65), 2, 128, seed=6)
     heads, d, extra = 6, 128, 4
