@@ -931,7 +931,10 @@ __device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &pa
         m = to;
         mc = __builtin_fabsf(m * c) <= kFar ? m * c : __builtin_nanf("");
     };
+    // What the powers of a row's probabilities are taken from (of far rows: all of m).
     const auto far = [&] { return mc != mc; };
+    const auto from = [&] { return far() && m != kNone ? m : 0.0f; };
+    const auto off = [&] { return far() ? 0.0f : mc; };
     // As in attend: values that are not finite make the rows NaN that see them, at the end
     // (bit dt: the elements of o[dt]).
     unsigned lost = 0;
@@ -973,7 +976,7 @@ __device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &pa
                 if (__ballot(high)) {
                     const float top = maximum(s);
                     raise(high ? fmaxf(m, top) : m);
-                    all = weights(s, far() && m != kNone ? m : 0.0f, far() ? 0.0f : mc, pr);
+                    all = weights(s, from(), off(), pr);
                 }
                 sum += all;
                 product(j, pr);
@@ -981,12 +984,13 @@ __device__ inline void many_rows(const Args &a, const Part<kPieceRows<T, D>> &pa
                 const float top = maximum(s);
                 if (__ballot(m == kNone ? top > kNone : far() || (top - m) * c > kHeadroom)) {
                     raise(fmaxf(m, top));
-                    const float from = far() && m != kNone ? m : 0.0f;
+                    if (__ballot(far())) {   // the scores are not needed again
 #pragma unroll
-                    for (int mt = 0; mt < 2; ++mt) s[mt] -= from;
+                        for (int mt = 0; mt < 2; ++mt) s[mt] -= from();
+                    }
                 }
                 bf16x8 pr[4][NP];
-                sum += weights(s, 0.0f, far() ? 0.0f : mc, pr);
+                sum += weights(s, 0.0f, off(), pr);
                 product(j, pr);
             }
             in_order<4 * DT, NP, 6>();
