@@ -19,14 +19,19 @@
 //   * many rows (a prompt's piece, a frame; bounded by the matrix units, whose LDS reads
 //     and exponentials take as long and overlap in part): tiles of 32 rows a wave.  A
 //     workgroup widens each chunk once into LDS, in the order of the operands, and all its
-//     waves read it there.  bf16, 128: 2 x 2048 rows of 40 heads over 16384 tokens 1215 us
-//     in all (1.06 PFLOP/s), 1560 of 5 heads over 56160 253 us (0.89: the last of 7 tiles
-//     has 24 of 256 rows).
+//     waves read it there.  bf16, 128: 2 x 2048 rows of 40 heads over 16384 tokens 1212 to
+//     1294 us in all, by card (1.06 to 1.00 PFLOP/s), 1560 of 5 heads over 56160 254 to 265
+//     (0.89 to 0.85: the last of 7 tiles has 24 of 256 rows); fp32, 1024 of 64 heads on 8
+//     key heads over 9216 872 us (1.0 PFLOP/s of the three products).
 // Widening is one instruction for two elements, exact in bf16.
 //
 // fp32 rows: Q and P are taken apart into three bf16 each, whose sum is exact, and
 // K and V are exact anyway, so the products are those of fp32.  bf16 rows: P is
-// rounded to bf16, 2^-8 relative at most, where its sum is not.
+// rounded to bf16, 2^-8 relative at most, where its sum is not.  That takes the output's
+// error in norm from the 1.66e-3 of its own rounding to 2.1e-3 to 2.35e-3; P in two parts,
+// which would save that, takes a third longer with many rows (1225 -> 1685 us, 254 -> 335)
+// and 2 to 12 % with few (one next token of 64 sequences 81.6 -> 83.3, 8 next tokens of 16
+// sequences of 8192 101 -> 110, a prompt of 64 behind 8192 52 -> 59).
 #include <algorithm>
 #include <cmath>
 
@@ -176,7 +181,9 @@ struct Work {
         // half as many: parts of tiles alike begin and end with groups, and a group's second
         // part costs about those units (12 sequences of 8 key heads of 128: 3840 tokens 25.7 us
         // in equal pieces and 22.8 in two groups a tile, 32768 92 and 102; of 5 heads 1560 rows
-        // over 32768 203 and 189, 1536 184 and 204).
+        // over 32768 203 and 189, 1536 184 and 204).  Many rows, bf16 and fp32, of 64 and 128,
+        // in 11 forms: at most 4 % slower than in equal pieces always, and than with 1.0, which
+        // takes up to 17 % longer (1536 rows of 5 heads over 32768 217 us for 185).
         constexpr double MORE = ROWS > kRows ? 0.45 : 1.0;
         const double room = a.groups, some = static_cast<double>(tiles), units = static_cast<double>(all);
         const double fit = min(units / a.least, room), even = some * floor(fit / some);
@@ -1185,7 +1192,10 @@ Plan plan_of(const KvCache &cache, const KvBatch &batch, int T, int H, int windo
     // beside others' next tokens, and enough of them for its start and its tiles of 128
     // or 256 rows, which the long sequences pay back first (8 key heads of 128, in both
     // kernels: 8192 tokens of 512 rows 50 and 81 us, of 1024 99 and 85; 32768 tokens of 256
-    // 88 and 111, of 512 159 and 137; 1024 tokens of 1024 24 and 46, of 4096 84 and 48).
+    // 88 and 111, of 512 159 and 137; 1024 tokens of 1024 24 and 46, of 4096 84 and 48).  Heads
+    // of 64 and fp32 turn at the same place: of 13 prompts each behind 1024, 8192 and 32768
+    // tokens, 64 rows a token, the rule takes the faster kernel or one 3 % behind, but for fp32,
+    // 128, 1024 tokens behind 1024 (216 us, 196 in the other).
     const int64_t n = chunks(kRows);
     const double beyond = static_cast<double>((static_cast<int64_t>(T) - batch.B) * H / kRows);   // tiles
     const bool pieces = (rows > static_cast<int64_t>(kFewRows) * batch.B || T > 8LL * batch.B) && T > batch.B &&

@@ -165,7 +165,7 @@ hipError_t launch_head_norm(const RopeSide &q, const RopeSide &k, const void *qw
                             int R, bool half, float eps, int dtype, hipStream_t stream);
 // Its backward: q and k as the forward read them, dq and dk the gradients of its
 // outputs (x) and of its inputs (y); dqw and dkw [d] (NULL: not wanted); partial:
-// head_norm_partials(S, heads of both sides) rows of 2 d floats.
+// head_norm_partials(S, heads of both sides) rows of d floats.
 int head_norm_partials(int64_t S, int64_t heads);
 hipError_t launch_head_norm_backward(const RopeSide &q, const RopeSide &k, const RopeSide &dq, const RopeSide &dk,
                                      const void *qw, const void *kw, bool w_f32, void *dqw, void *dkw, float *partial,

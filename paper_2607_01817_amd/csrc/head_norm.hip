@@ -11,9 +11,10 @@
 // and dx out.  LP lanes hold a head vector (8 elements each, in the layout of
 // halves 8 and their partners), so the sums are a few steps between lanes of a
 // row, and they go through a token's heads with its table entries and the
-// weights in registers.  dw is kept in registers over all the tokens of a lane,
-// then added over a workgroup's lanes through LDS and over the workgroups by a
-// second kernel, all in a fixed order.
+// weights in registers.  dw is kept in registers over all the tokens of a lane
+// (in fp32, chains of a few terms and tokens x heads / 2048 at most), then added
+// over a workgroup's lanes through LDS and over the workgroups by a second
+// kernel in fp64, all in a fixed order.
 //
 // bf16, heads of 128: 56160 tokens of 10 heads 61 us, 4.7 TB/s of x and y; 7800 of 80
 // heads 55 us, its backward 97, 4.9 TB/s, and the sum of dw 5.
@@ -63,9 +64,9 @@ struct Side {
     int64_t dy_token, dy_head;
     const void *w;
 };
-// 1 / sqrt(x) to an ulp: the hardware's with one step of Newton's, a quarter of the
-// instructions of an exact root and division.  The hardware's takes what is below 2^-126
-// as 0, so that goes in as 2^24 x.  0 gives infinity, and infinity 0.
+// 1 / sqrt(x) to an ulp: the hardware's with one step of Newton's, in fewer instructions
+// than an exact root and division.  The hardware's takes what is below 2^-126 as 0, so that
+// goes in as 2^24 x.  0 gives infinity, and infinity 0.
 __device__ inline float inverse_root(float x) {
     const bool small = x < 0x1p-126f;
     const float y = small ? x * 0x1p24f : x;
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(256) void head_norm_backward_kernel(Args a, float *
     }
     __syncthreads();
     for (int e = threadIdx.x; e < a.d; e += 256) {
-        double sum = 0.0;   // and in sum_partials_kernel: no length of a chain of sums shows
+        double sum = 0.0;   // and in sum_partials_kernel: fp32 are the lanes' own chains alone
         for (int i = 0; i < PER; ++i) sum += lds[i * a.d + e];
         row[e] = static_cast<float>(sum);
     }
@@ -378,7 +379,8 @@ __global__ __launch_bounds__(256) void head_norm_any_kernel(Args a, bool half, f
     __syncthreads();
     float *row = partial + (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * a.d;
     for (int e = threadIdx.x; e < a.d; e += 256)
-        row[e] = (lds[e] + lds[a.d + e]) + (lds[2 * a.d + e] + lds[3 * a.d + e]);
+        row[e] = static_cast<float>((static_cast<double>(lds[e]) + lds[a.d + e]) +
+                                    (static_cast<double>(lds[2 * a.d + e]) + lds[3 * a.d + e]));
 }
 
 // dw of both sides from the workgroups' rows of d, the queries' q_rows first: 16
