@@ -31,7 +31,9 @@
 // error in norm from the 1.66e-3 of its own rounding to 2.1e-3 to 2.35e-3; P in two parts,
 // which would save that, takes a third longer with many rows (1225 -> 1685 us, 254 -> 335)
 // and 2 to 12 % with few (one next token of 64 sequences 81.6 -> 83.3, 8 next tokens of 16
-// sequences of 8192 101 -> 110, a prompt of 64 behind 8192 52 -> 59).
+// sequences of 8192 101 -> 110, a prompt of 64 behind 8192 52 -> 59).  fp16 would hold
+// three bits more, but not those of probabilities below 2^-21 of the largest, which are all
+// that an element has whose other tokens' values are 0.
 #include <algorithm>
 #include <cmath>
 
