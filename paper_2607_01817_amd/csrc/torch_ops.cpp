@@ -238,15 +238,16 @@ std::pair<Tensor, Tensor> rms_norm_backward(const Tensor &dy, const Tensor &x, c
 // differentiable.
 void once() { TORCH_CHECK(!at::GradMode::is_enabled(), "these operators are differentiable once (create_graph)"); }
 
-// The capture that a stream's work goes into, or 0.
-unsigned long long capture_of(hipStream_t stream) {
+// The capture that a stream's work goes into, if it does.
+std::optional<unsigned long long> capture_of(hipStream_t stream) {
     hipStreamCaptureStatus status;
     unsigned long long id = 0;
     if (hipStreamGetCaptureInfo(stream, &status, &id) != hipSuccess) {   // the default stream, which is never captured
         (void)hipGetLastError();
-        return 0;
+        return std::nullopt;
     }
-    return status == hipStreamCaptureStatusNone ? 0 : id;
+    if (status == hipStreamCaptureStatusNone) return std::nullopt;
+    return id;
 }
 
 // A backward pass under capture hands a gradient on to the stream of the node that takes it:

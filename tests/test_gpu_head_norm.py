@@ -7,6 +7,10 @@ within 2^-17 of the magnitudes of their terms; the rotation's terms are both ele
 a pair; then the rounding of the storage type.  dw sums over tokens and heads in fp32, in
 a tree whose paths have at most S H / 512 + 100 steps, each 2^-24 of the magnitudes.
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -368,3 +372,30 @@ def test_a_captured_training_step_on_two_streams(hcms):
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(bits(a), bits(b))
+
+
+def test_the_first_capture_of_a_process_refuses_an_eager_graph_s_leaves():
+    """In a process of its own, whose first capture has the first of all ids."""
+    code = """
+import torch
+import paper_2607_01817_amd as hcms
+x, w = torch.randn(8, 2, 64, device="cuda", requires_grad=True), torch.ones(64, device="cuda", requires_grad=True)
+table, flag = hcms.rope_table([8], [32]), torch.zeros(1, device="cuda")
+alive = hcms.QkNormRope.apply(x, None, w, None, table, [8], [32])
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    flag.add_(1.0)
+    y = hcms.QkNormRope.apply(x, None, w, None, table, [8], [32])
+    try:
+        torch.autograd.grad(y, (x, w), torch.ones_like(y))
+    except RuntimeError as e:
+        assert "drop that graph" in str(e), e
+        flag.add_(1.0)
+graph.replay()
+torch.cuda.synchronize()
+assert flag.item() == 2.0
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100,
+                          cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert done.returncode == 0, done.stderr[-2000:]
